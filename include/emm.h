@@ -17,6 +17,8 @@
  *   emm_decode_attn_shared  the decode step reading pages that several requests share once (Section 3.3)
  *   emm_decode_step   scatter + decode attention of one step in one launch               (Section 2.2)
  *   emm_kv_pages_pack / emm_kv_pages_unpack  the two ends of a KV cache migration      (Appendix B.5)
+ *   emm_rope          rotary positions of q and k, before the scatter
+ * emm_fp8.h has the cache in 8 bits: quantised as it is written, read back, attended over.
  *
  * Conventions common to all calls
  *   - Every pointer marked "device" is memory of the current HIP device, owned by the caller; the
@@ -342,6 +344,70 @@ emm_status emm_kv_pages_pack(const void *k_cache, const void *v_cache, int32_t n
 emm_status emm_kv_pages_unpack(const void *staging, const int32_t *page_ids, int32_t n, void *k_cache,
                                void *v_cache, int32_t num_pages, int64_t page_bytes, uint32_t *checksums,
                                const uint32_t *expected, uint32_t *mismatches, void *hip_stream);
+
+/*
+ * Rotary positions.  A model whose attention takes positions by rotation turns q and k by them before k goes into
+ * the cache (emm_kv_scatter) and q into an attention call.  Frequency i < rotary_dim / 2 turns one pair of channels
+ * (a, b) of every head by the angle position * inv_freq[i]:
+ *   (a, b) -> factor * (a cos - b sin, b cos + a sin);     inverse: the angle's sign is changed, which is the
+ *   transpose of the rotation: it takes a gradient back through it, and for factor 1 undoes it
+ *   layout EMM_ROPE_HALF         a = channel i, b = channel i + rotary_dim / 2
+ *   layout EMM_ROPE_INTERLEAVED  a = channel 2 i, b = channel 2 i + 1
+ * Channels from rotary_dim on stay as they are.  Positions: with num_axes == 0 a token's place in its request,
+ * prefix_lens[r] + j.  With num_axes 1 .. 4 they are given, positions[axis][token], any int32 (images and videos
+ * have a position for each of time, height and width); the first sections[0] frequencies go by axis 0, the next
+ * sections[1] by axis 1 and so on, and the sections add up to rotary_dim / 2.
+ * Angles are taken in 64 bits and reduced to a turn before sine and cosine (in 32 bits position 10^6 alone would be
+ * 0.06 rad off); the rotation is in 32 bits, rounded once to the batch's dtype.
+ */
+typedef enum { EMM_ROPE_HALF = 0, EMM_ROPE_INTERLEAVED = 1 } emm_rope_layout;
+typedef struct {
+    int32_t layout;              /* emm_rope_layout                                                  */
+    int32_t rotary_dim;          /* a multiple of 16, 16 .. head_dim                                 */
+    int32_t num_axes;            /* 0: positions from the batch; 1 .. 4: as given                    */
+    int32_t inverse;             /* 0 or 1                                                           */
+    int32_t sections[4];         /* frequencies of each axis (num_axes of them count)                */
+    float factor;                /* of cosine and sine; 1 unless a scaling asks for another          */
+    int32_t reserved;            /* must be 0                                                        */
+    const double *inv_freq;      /* device [rotary_dim / 2], 8-byte aligned                          */
+    const int32_t *positions;    /* device [num_axes][T], or NULL where num_axes is 0                */
+} emm_rope_params;
+
+/*
+ * Rotates q [T][num_q_heads][head_dim] into q_out and k [T][num_kv_heads][head_dim] into k_out (either pair may be
+ * NULL).  token_stride: elements from a token's row to the next in q and in k, for views into the rows of one
+ * projection (a multiple of 16 bytes, at least a row); 0: q and k are packed.  q_out and k_out are always packed,
+ * and may be q and k themselves where those are; any other overlap is refused.  dtype EMM_BF16 or EMM_F32, head_dim
+ * 64 or 128.  Of the batch's arrays prefix_lens and cu_new_lens are read, and new_lens (rows of no request are left
+ * as they were), where num_axes is 0; with given positions none, and all T rows are turned.
+ */
+emm_status emm_rope(const emm_batch *batch, const emm_rope_params *rope, const void *q, const void *k,
+                    int64_t token_stride, void *q_out, void *k_out, void *hip_stream);
+
+/*
+ * The frequencies, in host memory: inv_freq[i] = base^(-2 i / rotary_dim), changed for contexts `scale` times as long
+ * as the model was trained on (original_len tokens) by one of the published ways:
+ *   EMM_ROPE_PLAIN   unchanged
+ *   EMM_ROPE_LINEAR  divided by scale (position interpolation)
+ *   EMM_ROPE_NTK     base * scale^(rotary_dim / (rotary_dim - 2)) in place of base (the lowest frequency is divided by
+ *                    scale, the highest stays)
+ *   EMM_ROPE_YARN    frequencies with more than `fast` turns in original_len tokens stay, those with fewer than `slow`
+ *                    are divided by scale, between them a linear ramp over i; *factor = 0.1 ln(scale) + 1
+ *                    (YaRN, arXiv 2309.00071)
+ *   EMM_ROPE_BANDS   the same ends, between them a linear ramp over the number of turns; *factor = 1
+ * fast > slow > 0 and original_len > 0 are needed by the last two only.  *factor is 1 for the others; NULL: not wanted.
+ */
+typedef enum { EMM_ROPE_PLAIN = 0, EMM_ROPE_LINEAR = 1, EMM_ROPE_NTK = 2, EMM_ROPE_YARN = 3, EMM_ROPE_BANDS = 4 } emm_rope_kind;
+typedef struct {
+    int32_t kind;                /* emm_rope_kind                                                    */
+    int32_t rotary_dim;          /* a multiple of 16, 16 .. 128                                      */
+    int32_t original_len;
+    int32_t reserved;            /* must be 0                                                        */
+    double base;                 /* > 1                                                              */
+    double scale;                /* >= 1                                                             */
+    double slow, fast;
+} emm_rope_scaling;
+emm_status emm_rope_inv_freq_host(const emm_rope_scaling *scaling, double *inv_freq, float *factor);
 
 /*
  * Host-side consistency check of a batch whose arrays are given as HOST copies (debug / tests).

@@ -1,4 +1,4 @@
-"""ctypes binding of the C-ABI library declared in ``include/emm.h``.
+"""ctypes binding of the C-ABI library declared in ``include/emm.h`` and ``include/emm_fp8.h``.
 
 Argument marshalling only: every function has the name and the meaning of the C entry point it
 calls, takes torch tensors that live on the GPU (PyTorch is used for device memory and streams,
@@ -26,7 +26,11 @@ EXPORTS = ["emm_kv_scatter", "emm_prefill_attn_workspace_size", "emm_prefill_att
            "emm_decode_attn_static", "emm_decode_attn_shared_workspace_size", "emm_decode_attn_shared", "emm_shared_prefix_plan_host",
            "emm_cross_attn_shared", "emm_decode_step", "emm_kv_pages_pack", "emm_kv_pages_unpack",
            "emm_prefill_shared_plan_host", "emm_prefill_attn_shared_workspace_size", "emm_prefill_attn_shared",
-           "emm_validate_batch_host", "emm_prefill_plan_host", "emm_status_string", "emm_version"]
+           "emm_validate_batch_host", "emm_prefill_plan_host", "emm_rope", "emm_rope_inv_freq_host", "emm_status_string", "emm_version"]
+FP8_EXPORTS = ["emm_kv_scatter_fp8", "emm_rope_kv_scatter_fp8", "emm_kv_gather_fp8", "emm_attn_fp8_workspace_size", "emm_prefill_attn_fp8",
+               "emm_cross_attn_fp8", "emm_decode_attn_fp8"]
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_KINDS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
 
 
 class EmmError(RuntimeError):
@@ -64,6 +68,21 @@ class emm_shared_prefix(ctypes.Structure):
                 ("max_own_tiles", ctypes.c_int32), ("max_unit_tiles", ctypes.c_int32), ("unit_first_req", ctypes.c_void_p),
                 ("unit_num_reqs", ctypes.c_void_p), ("unit_shared_len", ctypes.c_void_p), ("req_unit", ctypes.c_void_p),
                 ("req_shared_len", ctypes.c_void_p)]
+
+
+class emm_rope_params(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("sections", ctypes.c_int32 * 4), ("factor", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p)]
+
+
+class emm_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("original_len", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("base", ctypes.c_double), ("scale", ctypes.c_double), ("slow", ctypes.c_double), ("fast", ctypes.c_double)]
+
+
+class emm_fp8_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
 _lib = None
@@ -118,6 +137,18 @@ def load() -> ctypes.CDLL:
     lib.emm_validate_batch_host.argtypes = [bp, i32p, i32p, i32p, i32p, ctypes.c_int]
     lib.emm_prefill_plan_host.restype = ctypes.c_int
     lib.emm_prefill_plan_host.argtypes = [bp, i32p, ctypes.c_int, ctypes.POINTER(emm_prefill_plan)]
+    rp, cp, i64 = ctypes.POINTER(emm_rope_params), ctypes.POINTER(emm_fp8_cache), ctypes.c_int64
+    signatures = {"emm_rope": [bp, rp, vp, vp, i64, vp, vp, vp],
+                  "emm_rope_inv_freq_host": [ctypes.POINTER(emm_rope_scaling), ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_float)],
+                  "emm_kv_scatter_fp8": [bp, vp, vp, i64, cp, vp],
+                  "emm_rope_kv_scatter_fp8": [bp, rp, vp, vp, vp, i64, vp, cp, vp],
+                  "emm_kv_gather_fp8": [bp, cp, vp, vp, vp],
+                  "emm_attn_fp8_workspace_size": [bp, ctypes.POINTER(ctypes.c_size_t)]}
+    for name in ("emm_prefill_attn_fp8", "emm_cross_attn_fp8", "emm_decode_attn_fp8"):
+        signatures[name] = [bp, vp, cp, vp, vp, vp, ctypes.c_size_t, vp]
+    for name, args in signatures.items():
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = args
     lib.emm_status_string.restype = ctypes.c_char_p
     lib.emm_status_string.argtypes = [ctypes.c_int]
     lib.emm_version.restype = ctypes.c_int
@@ -350,6 +381,90 @@ def emm_kv_pages_unpack(staging, page_ids, n: int, k_cache, v_cache, num_pages: 
     _check(load().emm_kv_pages_unpack(_ptr(staging), _ptr(page_ids), n, _ptr(k_cache), _ptr(v_cache), num_pages,
                                       page_bytes, _ptr(checksums), _ptr(expected), _ptr(mismatches), _stream(stream)),
            "emm_kv_pages_unpack")
+
+
+def make_rope(inv_freq, *, rotary_dim: int, layout="half", factor: float = 1.0, inverse: bool = False, positions=None,
+              sections=None) -> emm_rope_params:
+    """Fill the descriptor.  inv_freq: float64 device tensor [rotary_dim / 2]; positions: int32 device tensor [axes][T], or
+    None for the tokens' places in their requests; sections: frequencies of each axis (default: one axis has them all).
+    The returned object keeps both tensors alive."""
+    axes = 0 if positions is None else int(positions.shape[0]) if positions.dim() == 2 else 1
+    parts = list(sections) if sections is not None and axes else [rotary_dim // 2] if axes == 1 else []
+    if len(parts) != axes:
+        raise ValueError("%d sections for %d axes of positions" % (len(parts), axes))
+    for what, t, kind in (("inv_freq", inv_freq, "torch.float64"), ("positions", positions, "torch.int32")):
+        if t is not None and (str(t.dtype) != kind or not t.is_contiguous()):
+            raise ValueError("%s is a contiguous %s tensor" % (what, kind))
+    if inv_freq is not None and inv_freq.numel() < rotary_dim // 2:
+        raise ValueError("inv_freq has %d of %d frequencies" % (inv_freq.numel(), rotary_dim // 2))
+    rope = emm_rope_params(ROPE_LAYOUTS.get(layout, layout), rotary_dim, axes, int(inverse), (ctypes.c_int32 * 4)(*(parts + [0] * 4)[:4]), factor, 0,
+                           _ptr(inv_freq), _ptr(positions))
+    rope._keepalive = (inv_freq, positions)
+    return rope
+
+
+def emm_rope_inv_freq_host(rotary_dim: int, base: float, kind="plain", scale: float = 1.0, original_len: int = 0, slow: float = 1.0,
+                           fast: float = 32.0):
+    """Returns (inv_freq: float64 array [rotary_dim / 2], factor)."""
+    inv, factor = np.zeros(max(rotary_dim // 2, 1), np.float64), ctypes.c_float(0.0)
+    s = emm_rope_scaling(ROPE_KINDS.get(kind, kind), rotary_dim, original_len, 0, base, scale, slow, fast)
+    _check(load().emm_rope_inv_freq_host(ctypes.byref(s), inv.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), ctypes.byref(factor)),
+           "emm_rope_inv_freq_host")
+    return inv, float(factor.value)
+
+
+def emm_rope(batch: emm_batch, rope: emm_rope_params, q, k, q_out, k_out, token_stride: int = 0, stream=None) -> None:
+    _check(load().emm_rope(ctypes.byref(batch), ctypes.byref(rope), _ptr(q), _ptr(k), token_stride, _ptr(q_out), _ptr(k_out), _stream(stream)),
+           "emm_rope")
+
+
+def make_fp8_cache(k, v, k_scale, v_scale) -> emm_fp8_cache:
+    """The pools: code tensors of any 8-bit type [num_pages][Hkv][page_size][d], scale bytes [num_pages][Hkv][page_size], which the
+    returned object keeps alive."""
+    for t in (k, v, k_scale, v_scale):
+        if t is not None and (t.element_size() != 1 or not t.is_contiguous()):
+            raise ValueError("the cache's pools are contiguous tensors of bytes")
+    cache = emm_fp8_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+    cache._keepalive = (k, v, k_scale, v_scale)
+    return cache
+
+
+def emm_kv_scatter_fp8(batch: emm_batch, k_new, v_new, cache: emm_fp8_cache, token_stride: int = 0, stream=None) -> None:
+    _check(load().emm_kv_scatter_fp8(ctypes.byref(batch), _ptr(k_new), _ptr(v_new), token_stride, ctypes.byref(cache), _stream(stream)),
+           "emm_kv_scatter_fp8")
+
+
+def emm_rope_kv_scatter_fp8(batch: emm_batch, rope: emm_rope_params, q, k_new, v_new, q_out, cache: emm_fp8_cache, token_stride: int = 0,
+                            stream=None) -> None:
+    _check(load().emm_rope_kv_scatter_fp8(ctypes.byref(batch), ctypes.byref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), token_stride, _ptr(q_out),
+                                          ctypes.byref(cache), _stream(stream)), "emm_rope_kv_scatter_fp8")
+
+
+def emm_kv_gather_fp8(batch: emm_batch, cache: emm_fp8_cache, k_out, v_out, stream=None) -> None:
+    _check(load().emm_kv_gather_fp8(ctypes.byref(batch), ctypes.byref(cache), _ptr(k_out), _ptr(v_out), _stream(stream)), "emm_kv_gather_fp8")
+
+
+def emm_attn_fp8_workspace_size(batch: emm_batch) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().emm_attn_fp8_workspace_size(ctypes.byref(batch), ctypes.byref(n)), "emm_attn_fp8_workspace_size")
+    return int(n.value)
+
+
+def _attn_fp8(name: str, batch, q, cache, out, lse, workspace, stream) -> None:
+    _check(getattr(load(), name)(ctypes.byref(batch), _ptr(q), ctypes.byref(cache), _ptr(out), _ptr(lse), _ptr(workspace), _bytes(workspace),
+                                 _stream(stream)), name)
+
+
+def emm_prefill_attn_fp8(batch: emm_batch, q, cache: emm_fp8_cache, out, lse=None, workspace=None, stream=None) -> None:
+    _attn_fp8("emm_prefill_attn_fp8", batch, q, cache, out, lse, workspace, stream)
+
+
+def emm_cross_attn_fp8(batch: emm_batch, q, cache: emm_fp8_cache, out, lse=None, workspace=None, stream=None) -> None:
+    _attn_fp8("emm_cross_attn_fp8", batch, q, cache, out, lse, workspace, stream)
+
+
+def emm_decode_attn_fp8(batch: emm_batch, q, cache: emm_fp8_cache, out, lse=None, workspace=None, stream=None) -> None:
+    _attn_fp8("emm_decode_attn_fp8", batch, q, cache, out, lse, workspace, stream)
 
 
 def emm_validate_batch_host(batch: emm_batch, page_table: np.ndarray, prefix_lens: np.ndarray,
