@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libemm.so")
 SOURCES = ["api.hip", "kv_scatter.hip", "attn_f32.hip", "attn_bf16.hip", "attn_bf16_decode.hip", "attn_merge.hip", "kv_migrate.hip", "prefix_cache.cpp",
-           "api_fp8.hip", "rope_rows.hip", "attn_fp8.hip"]
+           "api_fp8.hip", "rope_rows.hip", "attn_fp8.hip", "attn_fp8_tiles.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 instruction forms are switched off for every device translation unit
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

@@ -12,7 +12,7 @@
 // neighbouring channels of the 8 keys whose scores it holds (the accumulators of two score products, which are then
 // its part of the operand P^T as they are), pairs keys by byte permutes, and v_cvt_scalef32_pk_bf16_fp8 makes two bf16 of
 // a pair.  V's scales go into P (a power of two).
-#include "fp8_device.h"
+#include "attn_fp8_common.h"
 
 namespace emm {
 
@@ -20,15 +20,10 @@ namespace {
 
 using namespace fp8;
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int D = 128;
+constexpr int D = HEAD_DIM;
 constexpr int WAVES = 4;
 constexpr int TILE = 32;                                 // keys per step of a wave
 constexpr int ROWS = 16;
-constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
 
 // largest of the four lanes (l, l ^ 16, l ^ 32, l ^ 48) that hold a row
 __device__ inline float row_max(float x)
@@ -41,8 +36,6 @@ __device__ inline float row_sum(float x)
     x += __shfl_xor(x, 16);
     return x + __shfl_xor(x, 32);
 }
-
-__device__ inline float saturated(float x) { return x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f); }
 
 // q's operands of the score product: 32 channels of the lane's row
 struct QParts {
@@ -62,25 +55,17 @@ __device__ inline QParts split_q(const bf16x8 (&q)[4])
     most = max(most, (uint32_t)__shfl_xor((int)most, 32));
     QParts p;
     p.scale_high = scale_byte(most);
-    p.scale_low = p.scale_high - 4;
+    p.scale_low = p.scale_high + LOW_PART_SCALE;
     const float down = down_scale(p.scale_high);
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
-        float a[4], r[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = finite(x[4 * w + i]) ? x[4 * w + i] * down : __builtin_nanf("");
-        const uint32_t codes = pack4(saturated(a[0]), saturated(a[1]), saturated(a[2]), saturated(a[3]));
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(codes, true);
-        r[0] = saturated((a[0] - lo[0]) * 16.0f); r[1] = saturated((a[1] - lo[1]) * 16.0f);
-        r[2] = saturated((a[2] - hi[0]) * 16.0f); r[3] = saturated((a[3] - hi[1]) * 16.0f);
-        p.high[w] = (int)codes;
-        p.low[w] = (int)pack4(r[0], r[1], r[2], r[3]);
+        const float part[4] = {x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
+        const QCodes c = split4(part, down);
+        p.high[w] = (int)c.high;
+        p.low[w] = (int)c.low;
     }
     return p;
 }
-
-// a lane's bytes of V: 8 keys of 8 channels; which of them are NaN codes
-__device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
 template <bool CAUSAL>
 __global__ __launch_bounds__(64 * WAVES) void attn_fp8_rows_kernel(AttnFp8Args a)
@@ -261,10 +246,16 @@ __global__ __launch_bounds__(64 * WAVES) void attn_fp8_rows_kernel(AttnFp8Args a
 
 }  // namespace
 
-size_t attn_fp8_workspace_bytes(const BatchView&) { return 0; }
+// Few rows of a (request, KV head): their keys are split over the waves.  Many: rows over the waves, keys through LDS.
+namespace {
+bool few_rows(const BatchView& b) { return (long long)b.max_new_len * (b.num_q_heads / b.num_kv_heads) <= ROWS; }
+}  // namespace
+
+size_t attn_fp8_workspace_bytes(const BatchView& b) { return few_rows(b) ? 0 : attn_fp8_tiles_workspace_bytes(b); }
 
 hipError_t launch_attn_fp8(const AttnFp8Args& a, bool causal, hipStream_t stream)
 {
+    if (!few_rows(a.b)) return launch_attn_fp8_tiles(a, causal, stream);
     const int G = a.b.num_q_heads / a.b.num_kv_heads;
     const dim3 grid((unsigned)(((long long)a.b.max_new_len * G + ROWS - 1) / ROWS), (unsigned)a.b.num_kv_heads, (unsigned)a.b.num_reqs);
     if (causal) hipLaunchKernelGGL(attn_fp8_rows_kernel<true>, grid, dim3(64 * WAVES), 0, stream, a);

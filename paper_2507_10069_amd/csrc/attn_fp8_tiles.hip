@@ -1,0 +1,679 @@
+// Attention of many rows over the 8-bit cache: prompts and longer chunks (formulas: include/emm_fp8.h).
+//
+// Bound by the matrix pipe and the instructions around it.  Rows are (new token, query head of a KV group) pairs of one
+// (request, KV head), token-major; a workgroup of 8 waves takes 256 of them (a unit), a wave 32, and streams the keys
+// in tiles of 64, each fetched once for the workgroup:
+//   K     stays in 8 bits: global memory -> LDS (a ring of four tiles, fetched three ahead), 16-byte chunks placed so that the
+//         operand reads meet no bank twice (the hardware fixes where a lane's bytes land, so the lane picks what it fetches);
+//   V     goes to LDS as it is, and from there through the wave that fetched it, which makes it bf16 in its keys' scales
+//         (exact) and puts it into a ring of two tiles that the transposing reads take channels from;
+//   scale bytes travel with them.
+// S^T = K Q^T is v_mfma_scale_f32_32x32x64_f8f6f4: a key's scale byte is its row's block scale, and q comes as two 8-bit
+// parts (split4), so the scores are those of the bf16 q with half of K's LDS reads and none of its conversions.  A lane
+// has one row and 32 of a tile's keys; K's rows lie in LDS such that its weights, rounded to bf16, are the operand of
+// O^T += V^T P^T (v_mfma_f32_32x32x16_bf16) as they are.
+// Weights are exp2(S c - m) with a reference m that is the row's maximum over its first tile, and follows only where a
+// tile's weights sum to more than 2^20: any reference gives the same result, and the sum, which is taken before
+// the weights are used, tells in time.  So the loop takes no maxima.  Row sums are of the weights before they are
+// rounded (of the rounded ones they would be off by up to 2^-9 where few keys count).
+#include <type_traits>
+
+#include "attn_bf16_common.h"
+#include "attn_fp8_common.h"
+
+namespace emm {
+
+namespace {
+
+using namespace fp8;
+using bf16attn::lds_dma16;
+using bf16attn::pair_max;
+using bf16attn::pair_sum;
+using bf16attn::swap23;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int NW = 8;                                    // waves of a workgroup
+constexpr int BR = 32 * NW;                              // rows of a unit
+constexpr int BC = 64;                                   // keys of a tile
+constexpr int PLACES = 256;                              // workgroups that run at once: one on each compute unit
+constexpr int MAX_PARTS = 64;                            // pieces of a unit
+constexpr int MIN_TILES_ALONE = 2, MIN_TILES_BEHIND = 12;   // key tiles of a piece where no unit is whole, and behind whole ones
+constexpr float LAG_LIMIT = 1048576.f;                   // 2^20
+
+// LDS
+constexpr int K_TILE = BC * HEAD_DIM, V_TILE = BC * HEAD_DIM * 2, RAW_TILE = BC * HEAD_DIM;
+constexpr int K_AT = 0, V_AT = K_AT + 4 * K_TILE, RAW_AT = V_AT + 2 * V_TILE, S_AT = RAW_AT + 2 * RAW_TILE, FLAG_AT = S_AT + 4 * 128, SMEM = FLAG_AT + 64;
+constexpr int OUT_STRIDE = 272;                          // bytes between output rows on their way out
+static_assert(NW * 32 * OUT_STRIDE <= FLAG_AT, "output rows are staged over the rings");
+constexpr int FETCHES = 3;                               // of a wave for a tile: K, V, scales
+
+constexpr int RECORD_FLOATS = (64 + 2) * 64 * NW;        // of a piece: 64 accumulators of each thread in groups of four, then m and l
+
+// how the units of a batch are laid out over the grid
+struct Layout {
+    int units_max;          // units of the batch at most, rounded up to 8
+    int cut;                // 1: units behind the last full round of PLACES may be cut along the keys
+    int G;
+    Divisor by_G, by_kv_heads;
+};
+
+struct Unit {
+    int req, kvh, tile;     // req < 0: nothing to do
+    int new_len, prefix_len, cu_new;
+    int parts, part, slot;  // planned pieces of the unit, which one, and the unit's place among those that are cut
+};
+
+// Units in order: requests, in a request row tiles from the last (which sees the most keys) to the first, of a row tile the
+// KV heads; neighbouring workgroups run on neighbouring XCDs, so an XCD has the same few heads throughout and their K and V
+// go through its L2.  Whole rounds of PLACES units first; the rest, if few, are cut in as many pieces as fill the chip.
+// merge_slot >= 0: the unit in that slot instead.
+__device__ inline Unit plan_unit(const BatchView& b, const Layout& L, int wg, int merge_slot)
+{
+    Unit u;
+    u.req = -1;
+    const int lane = threadIdx.x & 63;
+    int total = 0;
+    int new_lane = 0, prefix_lane = 0, cu_lane = 0, incl = 0;
+    auto look = [&](int first) {                         // lane's request first + lane
+        const int r = min(first + lane, b.num_reqs - 1);
+        new_lane = b.new_lens[r];
+        prefix_lane = b.prefix_lens[r];
+        cu_lane = b.cu_new_lens[r];
+        const int n = first + lane < b.num_reqs ? clamp_new_len(b, new_lane, false) : 0;
+        incl = scan64((n * L.G + BR - 1) / BR);
+        return __builtin_amdgcn_readlane(incl, 63);
+    };
+    for (int first = 0; first < b.num_reqs; first += 64) total += look(first);
+    const int units = total * b.num_kv_heads;
+    const int full = L.cut ? units / PLACES * PLACES : units, rest = units - full;
+    const int stride = (rest + 7) & ~7;                  // pieces of a unit run on the XCD of the unit
+    u.parts = stride == 0 ? 1 : min(PLACES / stride, MAX_PARTS);
+    u.part = 0;
+    u.slot = 0;
+    int ordinal = wg;
+    if (merge_slot >= 0) {
+        if (merge_slot >= rest || u.parts < 2) return u;
+        u.slot = merge_slot;
+        ordinal = full + merge_slot;
+    } else if (wg >= full) {
+        if (stride == 0) return u;
+        u.part = (wg - full) / stride;
+        u.slot = wg - full - u.part * stride;
+        if (u.slot >= rest || u.part >= u.parts) return u;
+        ordinal = full + u.slot;
+    } else {
+        u.parts = 1;
+    }
+    if (ordinal >= units) return u;
+    const int nth = L.by_kv_heads.quotient(ordinal);     // row tile of the batch
+    u.kvh = ordinal - nth * b.num_kv_heads;
+    int before = 0;
+    for (int first = 0; first < b.num_reqs; first += 64) {
+        const int sum = b.num_reqs <= 64 ? total : look(first);
+        if (nth < before + sum) {
+            const unsigned long long hit = __builtin_amdgcn_ballot_w64(incl > nth - before);
+            const int at = __builtin_ctzll(hit);
+            u.req = first + at;
+            u.tile = __builtin_amdgcn_readlane(incl, at) - 1 - (nth - before);
+            u.new_len = __builtin_amdgcn_readlane(new_lane, at);
+            u.prefix_len = __builtin_amdgcn_readlane(prefix_lane, at);
+            u.cu_new = __builtin_amdgcn_readlane(cu_lane, at);
+            return u;
+        }
+        before += sum;
+    }
+    return u;
+}
+
+// a unit's rows and keys
+struct Extent {
+    int N, P, first_row, ctx, n_rows, row0, kv_len, n_tiles, pieces;
+};
+template <bool CAUSAL>
+__device__ inline Extent extent_of(const BatchView& b, const Layout& L, const Unit& u, bool alone)
+{
+    Extent e;
+    e.N = clamp_new_len(b, u.new_len, CAUSAL);
+    e.n_rows = e.N * L.G;
+    e.row0 = u.tile * BR;
+    e.P = clamp_prefix_len(b, u.prefix_len, CAUSAL ? e.N : 0);
+    e.first_row = clamp_first_row(b, u.cu_new, e.N);
+    e.ctx = CAUSAL ? e.P + e.N : e.P;
+    e.kv_len = CAUSAL ? e.P + L.by_G.quotient(min(e.row0 + BR, e.n_rows) - 1) + 1 : e.P;
+    e.n_tiles = (e.kv_len + BC - 1) / BC;
+    e.pieces = min(u.parts, max(1, e.n_tiles / (alone ? MIN_TILES_ALONE : MIN_TILES_BEHIND)));
+    return e;
+}
+
+__device__ inline void lds_dma4(const void* base, uint32_t byte_offset, uint32_t lds_byte_offset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_byte_offset), "v"(byte_offset), "s"(base) : "memory");
+}
+__device__ inline void pin(float& x) { asm volatile("" : "+v"(x)); }
+__device__ inline void pin(bf16x2& x)
+{
+    uint32_t u = __builtin_bit_cast(uint32_t, x);
+    asm volatile("" : "+v"(u));
+    x = __builtin_bit_cast(bf16x2, u);
+}
+template <int BEGIN, int END, class F>
+__device__ inline void static_for(F&& f)
+{
+    if constexpr (BEGIN < END) {
+        f(std::integral_constant<int, BEGIN>{});
+        static_for<BEGIN + 1, END>(f);
+    }
+}
+
+template <bool CAUSAL>
+__global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args a, Layout L)
+{
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[SMEM];
+    const BatchView& b = a.b;
+    const Unit u = plan_unit(b, L, blockIdx.x, -1);
+    if (u.req < 0) return;
+    const Extent e = extent_of<CAUSAL>(b, L, u, L.units_max <= PLACES);
+    if (e.row0 >= e.n_rows || u.part >= e.pieces) return;
+    const int t_begin = u.part * e.n_tiles / e.pieces, n_tiles = (u.part + 1) * e.n_tiles / e.pieces - t_begin;
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int l32 = lane & 31, h32 = lane >> 5;
+    const int wrow0 = e.row0 + wave * 32;
+    const bool active = wrow0 < e.n_rows;                    // a wave without rows fetches its share and meets the others
+    const int row = min(wrow0 + l32, e.n_rows - 1), tok = L.by_G.quotient(row);
+    const int limit = CAUSAL ? e.P + tok : e.P - 1;          // last key that the lane's row sees
+    const int wave_clear = CAUSAL ? (e.P + L.by_G.quotient(min(wrow0, e.n_rows - 1)) + 1) / BC : e.P / BC;    // tiles that all rows of the wave see whole,
+    const int unit_clear = CAUSAL ? (e.P + L.by_G.quotient(e.row0) + 1) / BC : e.P / BC;                      // and of the unit
+
+    // q, 64 channels a lane: 64 s + 32 h32 + 0 .. 31
+    i32x8 q_high[2], q_low[2];
+    int q_scale_high, q_scale_low;
+    {
+        const __bf16* qp = (const __bf16*)a.q + ((long long)(e.first_row + tok) * b.num_q_heads + u.kvh * L.G + row - tok * L.G) * HEAD_DIM + 32 * h32;
+        bf16x8 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = *(const bf16x8*)(qp + 64 * (i >> 2) + 8 * (i & 3));
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+            const float x = (float)v[i >> 3][i & 7];
+            most = max(most, finite(x) ? __float_as_uint(x) & 0x7fffffffu : 0u);
+        }
+        most = __float_as_uint(pair_max(__uint_as_float(most)));
+        q_scale_high = scale_byte(most);
+        q_scale_low = q_scale_high + LOW_PART_SCALE;
+        const float down = down_scale(q_scale_high);
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            const float x[4] = {(float)v[w >> 1][4 * (w & 1)], (float)v[w >> 1][4 * (w & 1) + 1], (float)v[w >> 1][4 * (w & 1) + 2], (float)v[w >> 1][4 * (w & 1) + 3]};
+            const QCodes c = split4(x, down);
+            q_high[w >> 3][w & 7] = (int)c.high;
+            q_low[w >> 3][w & 7] = (int)c.low;
+        }
+    }
+
+    // ---- fetches.  Wave w brings rows 8 w .. 8 w + 7 of a tile, of 16-key block 4 tile + w / 2 (1 KB of K and of V), and that block's
+    //      16 scale bytes of K (even waves) or V (odd).
+    const int32_t* __restrict__ pt = b.page_table + (long long)u.req * b.max_pages;
+    const int n_blocks = (e.ctx + 15) >> 4;
+    const uint32_t smem_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+    const int r16 = 8 * (wave & 1) + (lane >> 3);            // row in the block
+    // K: LDS row = block row with the key's bits 2 and 3 changed places; chunk c of row r lies at place c ^ (r / 2 mod 8)
+    const uint32_t k_src = swap23(r16) * HEAD_DIM + (((lane & 7) ^ ((r16 >> 1) & 7)) << 4);
+    const uint32_t v_src = (wave & 1) * 1024 + lane * 16;    // V: as it is
+    const unsigned char* scales = (wave & 1) ? a.pools.v_scale : a.pools.k_scale;
+    int block_ids = 0, ids_from = 0;                         // lane k: the wave's block of tile ids_from + k, in blocks of the pool
+    auto ask_blocks = [&](int from) {
+        const int blk = min(4 * (from + lane) + (wave >> 1), n_blocks - 1);
+        const int page = min(max(pt[blk >> b.page_shift], 0), b.num_pages - 1);
+        block_ids = ((page * b.num_kv_heads + u.kvh) << b.page_shift) + (blk & ((1 << b.page_shift) - 1));
+        ids_from = from;
+    };
+    auto block_of = [&](int t) { return (long long)__builtin_amdgcn_readlane(block_ids, t - ids_from); };
+    auto fetch_k = [&](int t, int slot) { lds_dma16(a.pools.k + block_of(t) * 2048, k_src, smem_base + K_AT + slot * K_TILE + wave * 1024); };
+    auto fetch_v = [&](int t, int slot) { lds_dma16(a.pools.v + block_of(t) * 2048, v_src, smem_base + RAW_AT + slot * RAW_TILE + wave * 1024); };
+    auto fetch_scales = [&](int t, int slot) {
+        const unsigned char* src = scales + block_of(t) * 16;
+        if (lane < 4) lds_dma4(src, lane * 4, smem_base + S_AT + slot * 128 + (wave & 1) * 64 + (wave >> 1) * 16);
+    };
+
+    // ---- V to bf16: 16 channels of a key per lane.  Keys behind the context hold anything: zeros in their place.  In tiles that not every
+    //      row sees whole, a NaN would reach rows that do not see it (0 * NaN): it becomes a zero too, and flags say that there was one.
+    const int v_key = 8 * wave + (lane >> 3);
+    const int v_wr = V_AT + v_key * 256 + (((2 * (lane & 7) + ((v_key)&1)) ^ ((v_key & 3) << 2)) << 4);     // the first of its two chunks, by turns
+    uint4 raw;
+    int raw_scale;
+    auto read_raw = [&](int raw_slot, int s_slot) {
+        raw = *(const uint4*)(smem + RAW_AT + raw_slot * RAW_TILE + wave * 1024 + lane * 16);
+        raw_scale = smem[S_AT + s_slot * 128 + 64 + v_key];
+    };
+    auto check_raw = [&](int t, int v_slot) {                // tiles from unit_clear on
+        if (t * BC + v_key >= e.ctx) {
+            raw = make_uint4(0, 0, 0, 0);
+            raw_scale = BIAS;
+        }
+        if constexpr (CAUSAL) {
+            const uint32_t n0 = nan_bytes(raw.x), n1 = nan_bytes(raw.y), n2 = nan_bytes(raw.z), n3 = nan_bytes(raw.w);
+            const bool any = __builtin_amdgcn_ballot_w64((n0 | n1 | n2 | n3) != 0) != 0;
+            if (any) raw = make_uint4(raw.x & ~((n0 >> 7) * 0xffu), raw.y & ~((n1 >> 7) * 0xffu), raw.z & ~((n2 >> 7) * 0xffu), raw.w & ~((n3 >> 7) * 0xffu));
+            if (lane == 0) smem[FLAG_AT + 8 * v_slot + wave] = any ? 1 : 0;
+        }
+    };
+    auto widen = [&](int half) -> uint4 {                    // 8 channels: the lower or upper half
+        const float s = up_scale(raw_scale);
+        const uint32_t w0 = half ? raw.z : raw.x, w1 = half ? raw.w : raw.y;
+        const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, true);
+        const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true);
+        return make_uint4(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1), __builtin_bit_cast(uint32_t, p2), __builtin_bit_cast(uint32_t, p3));
+    };
+    auto store_v = [&](int v_slot) {                         // (odd rows store their upper half first: no bank twice)
+        const uint4 lo = widen(0), hi = widen(1);
+        const bool odd = (v_key & 1) != 0;
+        const uint4 first = odd ? hi : lo, second = odd ? lo : hi;
+        *(uint4*)(smem + v_slot * V_TILE + v_wr) = first;
+        *(uint4*)(smem + v_slot * V_TILE + (v_wr ^ 16)) = second;
+    };
+
+    // which of the lane's 64 outputs meet a NaN of V: bit 4 (4 nb + v / 4) + v % 4.  Rare: from global memory, key by key.
+    unsigned long long poison = 0;
+    auto find_poison = [&](int t) {
+        for (int k = 0; k < BC; ++k) {
+            const int key = t * BC + k;
+            if (key >= e.ctx) break;
+            const int page = min(max(pt[(key >> 4) >> b.page_shift], 0), b.num_pages - 1);
+            const long long pool_row = ((((long long)page * b.num_kv_heads + u.kvh) << b.page_shift) + ((key >> 4) & ((1 << b.page_shift) - 1))) * 16 + (key & 15);
+            const uint32_t* codes = (const uint32_t*)(a.pools.v + pool_row * HEAD_DIM) + h32;
+            for (int c = 0; c < 16; ++c) {
+                const uint32_t n = nan_bytes(codes[2 * c]) >> 7;
+                const unsigned long long bits = (n | n >> 7 | n >> 14 | n >> 21) & 15u;
+                if (key <= limit) poison |= bits << (4 * c);
+            }
+        }
+    };
+
+    // ---- operands
+    const int k_rd = K_AT + l32 * HEAD_DIM + (((2 * h32) ^ ((l32 >> 1) & 7)) << 4);      // the other three chunks: ^ 16, ^ 64
+    const int ks_rd = S_AT + swap23(l32);
+    auto read_k = [&](int slot, int kb, int s) -> i32x8 {
+        const uint4 x = *(const uint4*)(smem + slot * K_TILE + kb * 32 * HEAD_DIM + (k_rd ^ (s << 6)));
+        const uint4 y = *(const uint4*)(smem + slot * K_TILE + kb * 32 * HEAD_DIM + (k_rd ^ (s << 6) ^ 16));
+        return i32x8{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
+    };
+    // within each 16 lanes, lane j gives the address of 4 channels of key k0 + j / 4 and gets keys k0 .. k0 + 3 of channel d0 + j
+    const int v_rd = V_AT + (8 * h32 + ((lane & 15) >> 2)) * 256 + ((4 * ((lane & 15) >> 2) + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) + (lane & 1) * 8;
+    auto read_v = [&](int slot, int k16, int nb) -> bf16x8 {     // keys 16 k16 .. + 15, channels 32 nb .. + 31
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        const unsigned char* src = smem + slot * V_TILE + 16 * k16 * 256 + (v_rd ^ (nb << 6));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src + 4 * 256));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const float c_log2 = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, b.softmax_scale * LOG2E)));
+
+    f32x16 o[4];
+    float m = 0.f, l = 0.f;
+#pragma unroll
+    for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[nb][v] = 0.f;
+
+    // register v of block kb is key 32 kb + 16 (v / 8) + 8 h32 + v % 8 of the tile
+    auto mask_tile = [&](int t, f32x16 (&s)[2]) {
+        const int last = limit - 8 * h32 - t * BC;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (32 * kb + 16 * (v >> 3) + (v & 7) > last) s[kb][v] = -INFINITY;
+    };
+    auto row_max = [&](const f32x16 (&s)[2]) -> float {
+        float x = s[0][0];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x = fmaxf(x, s[kb][v]);
+        return pair_max(x);
+    };
+    auto scores = [&](int slot, f32x16 (&s)[2]) {            // not interleaved: first and only tiles
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const int scale = smem[ks_rd + slot * 128 + 32 * kb];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const i32x8 kf = read_k(slot, kb, st);
+                s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, q_high[st], s[kb], 0, 0, 0, scale, 0, q_scale_high);
+                s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, q_low[st], s[kb], 0, 0, 0, scale, 0, q_scale_low);
+            }
+        }
+    };
+    // weights of a tile, packed, and their sum over the lane's keys
+    auto weights = [&](const f32x16 (&s)[2], uint32_t (&p)[16]) -> float {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            bf16x2 w;
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 3][2 * (i & 7)], c_log2, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[i >> 3][2 * (i & 7) + 1], c_log2, -m));
+            sum += x + y;
+            w[0] = (__bf16)x;
+            w[1] = (__bf16)y;
+            p[i] = __builtin_bit_cast(uint32_t, w);
+        }
+        return sum;
+    };
+    // the tile's weights have outgrown the reference: it becomes the row's maximum so far, and they are made again
+    auto raise = [&](const f32x16 (&s)[2], uint32_t (&p)[16]) -> float {
+        const float to = fmaxf(m, row_max(s) * c_log2), scale = __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= scale;
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[nb][v] *= scale;
+        return weights(s, p);
+    };
+    auto p_operand = [&](const uint32_t (&p)[16], int k16) -> bf16x8 {
+        return __builtin_bit_cast(bf16x8, u32x4{p[4 * k16], p[4 * k16 + 1], p[4 * k16 + 2], p[4 * k16 + 3]});
+    };
+    auto flagged = [&](int v_slot) -> bool {
+        typedef int i32x2 __attribute__((ext_vector_type(2)));
+        const i32x2 f = *(const i32x2*)(smem + FLAG_AT + 8 * v_slot);
+        return __builtin_amdgcn_readfirstlane(f[0] | f[1]) != 0;
+    };
+
+    if (n_tiles > 0) {
+        ask_blocks(t_begin);
+        fetch_k(t_begin, 0);
+        fetch_v(t_begin, 0);
+        fetch_scales(t_begin, 0);
+        if (n_tiles > 1) {
+            fetch_k(t_begin + 1, 1);
+            fetch_v(t_begin + 1, 1);
+            fetch_scales(t_begin + 1, 1);
+            fetch_k(t_begin + 2, 2);
+            fetch_scales(t_begin + 2, 2);
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0)
+        __syncthreads();
+        read_raw(0, 0);
+        if (t_begin >= unit_clear) check_raw(t_begin, 0);
+        store_v(0);
+        const int t_end = t_begin + n_tiles;
+        if (!active) {
+            for (int i = t_begin; i + 1 < t_end; ++i) {
+                const int R = (i - t_begin) & 3;
+                if (i + 3 - ids_from >= 64) ask_blocks(i + 2);
+                fetch_k(i + 3, (R + 3) & 3);
+                fetch_v(i + 2, R & 1);
+                fetch_scales(i + 3, (R + 3) & 3);
+                __builtin_amdgcn_s_waitcnt(0x0f70 | FETCHES);
+                __syncthreads();
+                read_raw((R + 1) & 1, (R + 1) & 3);
+                if (i + 1 >= unit_clear) check_raw(i + 1, (R + 1) & 1);
+                store_v((R + 1) & 1);
+            }
+            __syncthreads();
+        } else {
+            f32x16 sc[2][2];                                 // scores of tile i in sc[i & 1]
+            scores(0, sc[0]);
+            if (t_begin >= wave_clear) mask_tile(t_begin, sc[0]);
+            const float top = row_max(sc[0]) * c_log2;
+            m = top > -INFINITY ? top : 0.f;                 // (a row that sees none of a piece's keys: its weights are zeros)
+
+            // Iteration i: scores of tile i + 1 and the weights of tile i; then everybody's fetches for the next tiles are published;
+            // then the values of tile i, and V of tile i + 1 to bf16.
+            auto iteration = [&](int i, auto par) {
+                constexpr int R = decltype(par)::value;
+                constexpr int KS = (R + 1) & 3, VS = R & 1, VN = (R + 1) & 1;
+                f32x16 (&s_cur)[2] = sc[R & 1];
+                f32x16 (&s_nxt)[2] = sc[(R & 1) ^ 1];
+                uint32_t p[16];
+                float fa[16], fb[16], ea[16], eb[16], sum0 = 0.f, sum1 = 0.f;
+                const float ref = m;
+                // pair g: F F (scale, subtract), E E (exp2), A A (sums), C (round): a stream in which nothing follows what it depends on
+                auto softmax_op = [&](auto idx_c) {
+                    constexpr int idx = decltype(idx_c)::value, g = idx / 7, slot = idx % 7;
+                    if constexpr (slot == 0 && g < 16) {
+                        ea[g] = __builtin_amdgcn_exp2f(fa[g]);
+                        pin(ea[g]);
+                    } else if constexpr (slot == 1 && g < 16) {
+                        eb[g] = __builtin_amdgcn_exp2f(fb[g]);
+                        pin(eb[g]);
+                    } else if constexpr (slot == 2 && g >= 1) {
+                        bf16x2 w;
+                        w[0] = (__bf16)ea[g - 1];
+                        w[1] = (__bf16)eb[g - 1];
+                        pin(w);
+                        p[g - 1] = __builtin_bit_cast(uint32_t, w);
+                    } else if constexpr (slot == 3 && g + 1 < 16) {
+                        fa[g + 1] = fmaf(s_cur[(g + 1) >> 3][2 * ((g + 1) & 7)], c_log2, -ref);
+                        pin(fa[g + 1]);
+                    } else if constexpr (slot == 4 && g + 1 < 16) {
+                        fb[g + 1] = fmaf(s_cur[(g + 1) >> 3][2 * ((g + 1) & 7) + 1], c_log2, -ref);
+                        pin(fb[g + 1]);
+                    } else if constexpr (slot == 5 && g >= 1) {
+                        sum0 += ea[g - 1];
+                        pin(sum0);
+                    } else if constexpr (slot == 6 && g >= 1) {
+                        sum1 += eb[g - 1];
+                        pin(sum1);
+                    }
+                };
+                constexpr int OPS = 17 * 7;
+                fa[0] = fmaf(s_cur[0][0], c_log2, -ref);
+                fb[0] = fmaf(s_cur[0][1], c_log2, -ref);
+                const int scale0 = smem[ks_rd + KS * 128], scale1 = smem[ks_rd + KS * 128 + 32];
+                i32x8 kf[4];                                 // channels 0 .. 63 and 64 .. 127 of block 0, then of block 1
+                kf[0] = read_k(KS, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                static_for<0, 8>([&](auto kc) {
+                    constexpr int k = decltype(kc)::value, st = (k >> 1) & 1, kb = k >> 2;
+                    constexpr bool low = (k & 1) != 0;
+                    if constexpr (!low && k < 6) kf[(k >> 1) + 1] = read_k(KS, (k + 2) >> 2, ((k >> 1) + 1) & 1);
+                    if constexpr ((k & 3) == 0) {
+                        f32x16 zero;
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) zero[v] = 0.f;
+                        s_nxt[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[k >> 1], q_high[0], zero, 0, 0, 0, kb ? scale1 : scale0, 0, q_scale_high);
+                    } else {
+                        s_nxt[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[k >> 1], low ? q_low[st] : q_high[st], s_nxt[kb], 0, 0, 0, kb ? scale1 : scale0, 0,
+                                                                                    low ? q_scale_low : q_scale_high);
+                    }
+                    static_for<(k * OPS) / 8, ((k + 1) * OPS) / 8>(softmax_op);
+                    if constexpr (k == 1) fetch_k(i + 3, (R + 3) & 3);
+                    if constexpr (k == 2) fetch_v(i + 2, R & 1);
+                    if constexpr (k == 3) fetch_scales(i + 3, (R + 3) & 3);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                float sum = sum0 + sum1;
+                if (__builtin_amdgcn_ballot_w64(sum > LAG_LIMIT) != 0) {
+                    // both lanes of a row decide alike
+                    if (pair_max(sum) > LAG_LIMIT) sum = raise(s_cur, p);
+                }
+                l += sum;
+                __builtin_amdgcn_s_waitcnt(0x0f70 | FETCHES);        // all fetches but this iteration's have landed
+                __syncthreads();
+                __builtin_amdgcn_sched_barrier(0);
+                read_raw(VN, KS);
+                bf16x8 vf[16 + 2];
+                vf[0] = read_v(VS, 0, 0);
+                vf[1] = read_v(VS, 0, 1);
+                if (CAUSAL && i >= unit_clear) {
+                    if (flagged(VS)) find_poison(i);
+                }
+                if (i + 1 >= unit_clear) check_raw(i + 1, VN);
+                __builtin_amdgcn_sched_barrier(0);
+                static_for<0, 16>([&](auto kc) {
+                    constexpr int k = decltype(kc)::value;
+                    if constexpr (k + 2 < 16) vf[k + 2] = read_v(VS, (k + 2) >> 2, (k + 2) & 3);
+                    o[k & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k], p_operand(p, k >> 2), o[k & 3], 0, 0, 0);
+                    if constexpr (k == 4) store_v(VN);
+                    if constexpr (k == 8) {
+                        if (i + 1 >= wave_clear) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            mask_tile(i + 1, s_nxt);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            };
+            int i = t_begin;
+            for (;;) {
+                if (i + 6 - ids_from >= 64) ask_blocks(i + 2);       // tiles i + 2 .. i + 6 may be fetched in this trip
+                if (i + 1 >= t_end) break;
+                iteration(i, std::integral_constant<int, 0>{});
+                if (i + 2 >= t_end) break;
+                iteration(i + 1, std::integral_constant<int, 1>{});
+                if (i + 3 >= t_end) break;
+                iteration(i + 2, std::integral_constant<int, 2>{});
+                if (i + 4 >= t_end) break;
+                iteration(i + 3, std::integral_constant<int, 3>{});
+                i += 4;
+            }
+            // the last tile
+            const int odd = (n_tiles - 1) & 1;
+            uint32_t p[16];
+            float sum = odd ? weights(sc[1], p) : weights(sc[0], p);
+            if (__builtin_amdgcn_ballot_w64(sum > LAG_LIMIT) != 0) {
+                if (pair_max(sum) > LAG_LIMIT) sum = odd ? raise(sc[1], p) : raise(sc[0], p);
+            }
+            l += sum;
+            __syncthreads();
+            if (CAUSAL && t_end - 1 >= unit_clear) {
+                if (flagged(odd)) find_poison(t_end - 1);
+            }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) o[k & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(odd, k >> 2, k & 3), p_operand(p, k >> 2), o[k & 3], 0, 0, 0);
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);                  // the last fetches have landed, and
+        __syncthreads();                                     // all are past their reads: the rings are free
+    }
+    if (!active) return;
+    if (CAUSAL && __builtin_amdgcn_ballot_w64(poison != 0) != 0) {
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if ((poison >> (16 * nb + v)) & 1) o[nb][v] = __builtin_nanf("");
+    }
+    const float l_row = pair_sum(l);
+    if (e.pieces > 1) {
+        float* rec = (float*)a.workspace + (long long)(u.slot * u.parts + u.part) * RECORD_FLOATS;
+#pragma unroll
+        for (int g = 0; g < 16; ++g)
+            *(f32x4*)(rec + (g * 64 * NW + tid) * 4) = f32x4{o[g >> 2][4 * (g & 3)], o[g >> 2][4 * (g & 3) + 1], o[g >> 2][4 * (g & 3) + 2], o[g >> 2][4 * (g & 3) + 3]};
+        *(f32x2*)(rec + 64 * 64 * NW + 2 * tid) = f32x2{l_row == 0.f ? -INFINITY : m, l_row};
+        return;
+    }
+    // rows go out through LDS, so that a store writes four whole rows
+    const float inv = l_row == 0.f ? 0.f : 1.0f / l_row;
+    unsigned char* stage = smem + wave * (32 * OUT_STRIDE);
+#pragma unroll
+    for (int g = 0; g < 16; ++g) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = (__bf16)(o[g >> 2][4 * (g & 3) + k] * inv);
+        *(bf16x4*)(stage + l32 * OUT_STRIDE + 2 * (32 * (g >> 2) + 8 * (g & 3) + 4 * h32)) = w;
+    }
+    auto place_of = [&](int r) -> long long {
+        const int t = L.by_G.quotient(r);
+        return (long long)(e.first_row + t) * b.num_q_heads + u.kvh * L.G + r - t * L.G;
+    };
+    if (a.lse != nullptr && h32 == 0 && wrow0 + l32 < e.n_rows) a.lse[place_of(wrow0 + l32)] = l_row == 0.f ? -INFINITY : (m + log2f(l_row)) * LN2;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int r = 4 * j + (lane >> 4);
+        if (wrow0 + r < e.n_rows)
+            *(uint4*)((__bf16*)a.out + place_of(wrow0 + r) * HEAD_DIM + (lane & 15) * 8) = *(const uint4*)(stage + r * OUT_STRIDE + (lane & 15) * 16);
+    }
+}
+
+// the pieces of the units that were cut: a workgroup per unit and wave of rows, a thread for a quarter of a lane's accumulators
+template <bool CAUSAL>
+__global__ __launch_bounds__(256) void attn_fp8_merge_tiles_kernel(AttnFp8Args a, Layout L)
+{
+    const BatchView& b = a.b;
+    const Unit u = plan_unit(b, L, 0, blockIdx.x / NW);
+    if (u.req < 0) return;
+    const Extent e = extent_of<CAUSAL>(b, L, u, L.units_max <= PLACES);
+    const int wave = blockIdx.x % NW, lane = threadIdx.x & 63, nb = threadIdx.x >> 6;
+    const int row = e.row0 + 32 * wave + (lane & 31);
+    if (e.pieces < 2 || e.row0 + 32 * wave >= e.n_rows) return;
+    const float* rec = (const float*)a.workspace + (long long)(u.slot * u.parts) * RECORD_FLOATS;
+    const int col = 64 * wave + lane;
+    float top = -INFINITY;
+    for (int p = 0; p < e.pieces; ++p) top = fmaxf(top, rec[(long long)p * RECORD_FLOATS + 64 * 64 * NW + 2 * col]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    f32x4 acc[4] = {};
+    float sum = 0.f;
+    for (int p = 0; p < e.pieces; ++p) {
+        const float* one = rec + (long long)p * RECORD_FLOATS;
+        const f32x2 ml = *(const f32x2*)(one + 64 * 64 * NW + 2 * col);
+        const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
+        sum = fmaf(ml[1], f, sum);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 x = *(const f32x4*)(one + ((4 * nb + g) * 64 * NW + col) * 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[g][k] = fmaf(x[k], f, acc[g][k]);
+        }
+    }
+    if (row >= e.n_rows) return;
+    const int t = L.by_G.quotient(row);
+    const long long place = (long long)(e.first_row + t) * b.num_q_heads + u.kvh * L.G + row - t * L.G;
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = (__bf16)(acc[g][k] * inv);
+        *(bf16x4*)((__bf16*)a.out + place * HEAD_DIM + 32 * nb + 8 * g + 4 * (lane >> 5)) = w;
+    }
+    if (a.lse != nullptr && threadIdx.x < 32) a.lse[place] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
+}
+
+Layout layout_of(const BatchView& b)
+{
+    Layout L;
+    L.G = b.num_q_heads / b.num_kv_heads;
+    L.by_G = divisor_of(L.G);
+    L.by_kv_heads = divisor_of(b.num_kv_heads);
+    const long long longest = ((long long)b.max_new_len * L.G + BR - 1) / BR;
+    const long long most = (long long)b.total_new_tokens * L.G / BR + b.num_reqs;
+    const bool equal = (long long)b.max_new_len * b.num_reqs == b.total_new_tokens;
+    const long long row_tiles = equal ? longest * b.num_reqs : longest * b.num_reqs < most ? longest * b.num_reqs : most;
+    const long long units = row_tiles * b.num_kv_heads;
+    L.units_max = (int)((units + 7) / 8 * 8);
+    // behind whole rounds only long pieces pay; where all units run at once any do
+    const long long tiles = ((long long)b.max_pages * b.page_size + BC - 1) / BC;
+    L.cut = tiles >= 2 * (L.units_max <= PLACES ? MIN_TILES_ALONE : MIN_TILES_BEHIND) && !(equal && (units + 7) / 8 * 8 % PLACES > PLACES / 2);
+    return L;
+}
+
+}  // namespace
+
+size_t attn_fp8_tiles_workspace_bytes(const BatchView& b)
+{
+    return layout_of(b).cut ? (size_t)PLACES * RECORD_FLOATS * sizeof(float) : 0;
+}
+
+hipError_t launch_attn_fp8_tiles(const AttnFp8Args& a, bool causal, hipStream_t stream)
+{
+    const Layout L = layout_of(a.b);
+    const dim3 grid((unsigned)(L.units_max + (L.cut ? PLACES : 0))), block(64 * NW);
+    if (causal) hipLaunchKernelGGL(attn_fp8_tiles_kernel<true>, grid, block, 0, stream, a, L);
+    else hipLaunchKernelGGL(attn_fp8_tiles_kernel<false>, grid, block, 0, stream, a, L);
+    if (L.cut) {
+        const int slots = L.units_max < PLACES / 2 ? L.units_max : PLACES / 2;
+        if (causal) hipLaunchKernelGGL(attn_fp8_merge_tiles_kernel<true>, dim3(slots * NW), dim3(256), 0, stream, a, L);
+        else hipLaunchKernelGGL(attn_fp8_merge_tiles_kernel<false>, dim3(slots * NW), dim3(256), 0, stream, a, L);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace emm

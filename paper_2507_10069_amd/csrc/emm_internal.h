@@ -179,6 +179,8 @@ struct AttnFp8Args {
     void* workspace;
 };
 size_t attn_fp8_workspace_bytes(const BatchView& b);
+size_t attn_fp8_tiles_workspace_bytes(const BatchView& b);
+hipError_t launch_attn_fp8_tiles(const AttnFp8Args& a, bool causal, hipStream_t stream);
 hipError_t launch_attn_fp8(const AttnFp8Args& a, bool causal, hipStream_t stream);
 
 }  // namespace emm
