@@ -18,6 +18,7 @@
 // its part of the operand P^T as they are), pairs keys by byte permutes, and v_cvt_scalef32_pk_bf16_fp8 makes two bf16 of
 // a pair.  V's scales go into P (a power of two).
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_fp8_common.h"
 
@@ -28,48 +29,34 @@ namespace {
 using namespace fp8;
 
 constexpr int D = HEAD_DIM;
-constexpr int WAVES = 4;
+constexpr int WAVES = 4;                                 // of a workgroup; a compute unit holds two
+constexpr int SUMS = 8 / WAVES;
 constexpr int TILE = 32;                                 // keys per step of a wave
 constexpr int ROWS = 16;
-constexpr int LEAST_TILES = 4;                           // of a part: one for each wave
-constexpr int WORKGROUPS = 1024;                         // four on each compute unit
+constexpr int OUT_STRIDE = D + 8;                        // bf16 values between output rows in LDS
+constexpr int LEAST_TILES = WAVES;                       // of a part: one for each wave
+constexpr int WORKGROUPS = 512;                          // two on each compute unit
+constexpr int MANY_RECORDS = 16;                         // of a pair
+constexpr int STREAM_TILES = 12000;                      // 96 MiB of codes: from here on a call does not fit the last-level cache next to others
+constexpr int MOST_COMPARED = 512;                       // requests among which shared pages are looked for
 
-// largest of the four lanes (l, l ^ 16, l ^ 32, l ^ 48) that hold a row
-__device__ inline float row_max(float x)
-{
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ inline float row_sum(float x)
-{
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
-}
+// of the four lanes (l, l ^ 16, l ^ 32, l ^ 48) that hold a row
+__device__ inline float row_max(float x) { return max32(max16(x)); }
+__device__ inline float row_sum(float x) { return sum32(sum16(x)); }
 
 // q's operands of the score product: 32 channels of the lane's row
 struct QParts {
     i32x8 high, low;
     int scale_high, scale_low;                           // scale bytes
 };
-__device__ inline QParts split_q(const bf16x8 (&q)[4])
+__device__ inline QParts split_q(const uint32_t (&pairs)[16])
 {
-    float x[32];
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        x[i] = (float)q[i >> 3][i & 7];
-        most = max(most, finite(x[i]) ? __float_as_uint(x[i]) & 0x7fffffffu : 0u);
-    }
-    most = max(most, (uint32_t)__shfl_xor((int)most, 16));
-    most = max(most, (uint32_t)__shfl_xor((int)most, 32));
     QParts p;
-    p.scale_high = scale_byte(most);
-    p.scale_low = p.scale_high + LOW_PART_SCALE;
-    const float down = down_scale(p.scale_high);
+    p.scale_high = q_scale_byte(__float_as_uint(row_max(__uint_as_float(most_of(pairs)))));
+    p.scale_low = p.scale_high == 0xff ? 0xff : p.scale_high + LOW_PART_SCALE;
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
-        const float part[4] = {x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
-        const QCodes c = split4(part, down);
+        const QCodes c = split4(pairs[2 * w], pairs[2 * w + 1], p.scale_high);
         p.high[w] = (int)c.high;
         p.low[w] = (int)c.low;
     }
@@ -78,15 +65,15 @@ __device__ inline QParts split_q(const bf16x8 (&q)[4])
 
 // how the batch's tiles are dealt
 struct RowsLayout {
-    int G, workgroups, least;                            // least: tiles of a part
-    Divisor by_G, by_kv_heads;
+    int G, workgroups;
+    Divisor by_G, by_kv_heads, by_workgroups;
 };
 
 // a request's rows and keys, and where its tiles lie in the line (of one KV head; heads follow each other)
 struct Request {
     int r, N, P, first_row;
     int tiles;                                           // per KV head
-    long long before;                                    // tiles per KV head of the requests before it
+    int before;                                          // tiles per KV head of the requests before it
 };
 
 // What the wave's lanes see of 64 requests at a time.  (A request without queries has no tiles; one with queries and no keys has
@@ -95,7 +82,7 @@ template <bool CAUSAL>
 struct Line {
     const BatchView& b;
     int lane, N, P, cu, tiles, incl, first;
-    long long total;
+    int total;                                           // (the whole line is below 2^31 tiles: see launch_attn_fp8)
 
     __device__ int look(int from)                        // returns the tiles of the 64
     {
@@ -114,7 +101,7 @@ struct Line {
     {
         for (int from = 0; from < b.num_reqs; from += 64) total += look(from);
     }
-    __device__ Request take(int at, long long before_chunk) const
+    __device__ Request take(int at, int before_chunk) const
     {
         Request q;
         q.r = first + at;
@@ -126,118 +113,200 @@ struct Line {
         return q;
     }
     // the request that holds tile x of the line of one head, x < total
-    __device__ Request holding(long long x)
+    __device__ Request holding(int x)
     {
-        long long before = 0;
+        int before = 0;
         for (int from = 0;; from += 64) {
-            const int sum = b.num_reqs <= 64 ? (int)total : look(from);
+            const int sum = b.num_reqs <= 64 ? total : look(from);
             if (x < before + sum || from + 64 >= b.num_reqs)
-                return take(__builtin_ctzll(__builtin_amdgcn_ballot_w64(incl > (int)(x - before)) | 1ull << 63), before);
+                return take(__builtin_ctzll(__builtin_amdgcn_ballot_w64(incl > x - before) | 1ull << 63), before);
             before += sum;
         }
     }
     __device__ Request request(int r)
     {
-        long long before = 0;
+        int before = 0;
         for (int from = 0;; from += 64) {
-            const int sum = b.num_reqs <= 64 ? (int)total : look(from);
+            const int sum = b.num_reqs <= 64 ? total : look(from);
             if (r < from + 64) return take(r - from, before);
             before += sum;
         }
     }
 };
 
-__device__ inline int part_tiles(const RowsLayout& L, long long all) { return (int)max((long long)L.least, (all + L.workgroups - 1) / L.workgroups); }
+__device__ inline int part_tiles(const RowsLayout& L, int all) { return max(LEAST_TILES, L.by_workgroups.quotient(all - 1) + 1); }
+// x / d for d > 0, 0 <= x < 2^31 and a quotient below 2^22: by the reciprocal, which is off by less than one whole
+__device__ inline int small_quotient(int x, int d)
+{
+    const int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));
+    const int rest = x - q * d;
+    return rest < 0 ? q - 1 : rest >= d ? q + 1 : q;
+}
 
-// A record: RT * 16 rows of 128 values, then (reference, sum) of each.  Workgroup w has two: of the pair its part begins in, of the pair
+// a row's place among the packed (token, head) rows
+__device__ inline long long place_of(const BatchView& b, const RowsLayout& L, const Request& rq, int kvh, int row)
+{
+    const int tok = L.by_G.quotient(row);
+    return (long long)(rq.first_row + tok) * b.num_q_heads + kvh * L.G + row - tok * L.G;
+}
+
+// A record: RT * 16 rows of 128 values in the order of the accumulators, then (reference, sum) of each.  Workgroup w has two: of the pair its part begins in, of the pair
 // that it ends in.
 template <int RT> constexpr int RECORD_FLOATS = RT * ROWS * (D + 2);
 
+// 16 bytes or 8 of a row of codes, with the non-temporal hint or without
+template <class T, bool STREAM>
+__device__ inline T fetch(const unsigned char* base, uint32_t offset)
+{
+    typedef uint32_t V __attribute__((ext_vector_type(sizeof(T) / 4)));
+    const V* p = (const V*)(base + offset);
+    if constexpr (STREAM) return __builtin_bit_cast(T, __builtin_nontemporal_load(p));
+    else return __builtin_bit_cast(T, *p);
+}
+
+// a part of a pair: the pair's tiles t0 .. t1 - 1
+struct Segment {
+    Request rq;
+    int kvh, t0, t1, n_rows, ctx;
+};
+
 template <bool CAUSAL, int RT>
-__global__ __launch_bounds__(64 * WAVES) void attn_fp8_rows_kernel(AttnFp8Args a, RowsLayout L)
+__global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Args a, RowsLayout L)
 {
     const BatchView& b = a.b;
-    __shared__ float part_o[WAVES][ROWS][D + 4];
-    __shared__ float part_m[WAVES][ROWS], part_l[WAVES][ROWS];
+    __shared__ f32x4 part_o[WAVES][ROWS * D / 4];
+    __shared__ f32x2 part_ml[WAVES][ROWS];
     Line<CAUSAL> line(b);
-    const long long all = line.total * b.num_kv_heads;
+    const int all = line.total * b.num_kv_heads;
+    if (all == 0) return;
     const int share = part_tiles(L, all);
-    long long x = (long long)blockIdx.x * share;
-    const long long x_end = min(x + share, all);
+    int x = (int)min((long long)blockIdx.x * share, (long long)all);
+    const int x_end = x + min(share, all - x);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int n16 = lane & 15, g = lane >> 4;
     const float c = b.softmax_scale * LOG2E;
-    bool first_segment = true;
-    while (x < x_end) {
-        const Request rq = line.holding(x / b.num_kv_heads);
-        const long long off = x - rq.before * b.num_kv_heads;
-        if (off < 0 || off >= (long long)rq.tiles * b.num_kv_heads) return;      // (lengths that change meanwhile)
-        const int kvh = (int)(off / rq.tiles), t0 = (int)(off - (long long)kvh * rq.tiles);
-        const int t1 = (int)min((long long)rq.tiles, t0 + (x_end - x));
-        x += t1 - t0;
-        const int n_rows = min(rq.N * L.G, RT * ROWS);
-        const int ctx = CAUSAL ? rq.P + rq.N : rq.P;                     // slots that hold tokens
-        const int all_see = CAUSAL ? rq.P + 1 : rq.P;                    // keys that every row sees
-        const int last_block = max(((ctx + 15) >> 4) - 1, 0);
 
-        QParts q[RT];
-        int limit[RT];                                                   // last key that the lane's row sees
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const int row = min(rt * ROWS + n16, n_rows - 1), tok = L.by_G.quotient(row);
-            limit[rt] = CAUSAL ? rq.P + tok : rq.P - 1;
-            const __bf16* qp = (const __bf16*)a.q + ((long long)(rq.first_row + tok) * b.num_q_heads + kvh * L.G + row - tok * L.G) * D;
-            // channels 16 g .. + 15 and 64 + 16 g .. + 15, of q and of K alike
-            bf16x8 qv[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) qv[i] = *(const bf16x8*)(qp + 64 * (i >> 1) + 16 * g + 8 * (i & 1));
-            q[rt] = split_q(qv);
+    // the segment that begins at x; x moves behind it.  t1 == t0: none.
+    auto next_segment = [&]() -> Segment {
+        Segment s = {};
+        if (x >= x_end) return s;
+        s.rq = line.holding(L.by_kv_heads.quotient(x));
+        const int off = x - s.rq.before * b.num_kv_heads;
+        if (off < 0 || s.rq.tiles <= 0) return s;                        // (lengths that change meanwhile)
+        s.kvh = min(small_quotient(off, s.rq.tiles), b.num_kv_heads - 1);
+        s.t0 = off - s.kvh * s.rq.tiles;
+        s.t1 = max(min(s.rq.tiles, s.t0 + (x_end - x)), s.t0);
+        s.n_rows = min(s.rq.N * L.G, RT * ROWS);
+        s.ctx = CAUSAL ? s.rq.P + s.rq.N : s.rq.P;                       // slots that hold tokens
+        x += s.t1 - s.t0;
+        return s;
+    };
+    // lane 2 j + k: block k of the wave's j-th tile from `from` on, in 16-key blocks of the pool
+    auto ask_ids = [&](const Segment& s, int from) -> int {
+        const int blk = min(2 * (from + WAVES * (lane >> 1)) + (lane & 1), max(((s.ctx + 15) >> 4) - 1, 0));
+        const int page = min(max(b.page_table[(long long)s.rq.r * b.max_pages + (blk >> b.page_shift)], 0), b.num_pages - 1);
+        return ((page * b.num_kv_heads + s.kvh) << b.page_shift) + (blk & ((1 << b.page_shift) - 1));
+    };
+    // Are K and V of the segment to go past the caches?  Not where all of a call fits them, nor where another request holds the same
+    // pages: what the first brings in serves the others.
+    auto streamed = [&](const Segment& s) -> bool {
+        if (all < STREAM_TILES || s.t0 >= s.t1) return false;
+        const int entry = min((2 * s.t0) >> b.page_shift, b.max_pages - 1);
+        const int mine = b.page_table[(long long)s.rq.r * b.max_pages + entry];
+        bool shared = false;
+        for (int from = 0; from < min(b.num_reqs, MOST_COMPARED); from += 64) {
+            const int r = min(from + lane, b.num_reqs - 1);
+            shared |= r != s.rq.r && b.page_table[(long long)r * b.max_pages + entry] == mine;
         }
-        const int32_t* __restrict__ pt = b.page_table + (long long)rq.r * b.max_pages;
+        return __builtin_amdgcn_ballot_w64(shared) == 0;
+    };
+    // q's rows: channels 16 g .. + 15 and 64 + 16 g .. + 15, of q and of K alike
+    auto ask_q = [&](const Segment& s, int rt, uint32_t (&pairs)[16]) {
+        const __bf16* qp = (const __bf16*)a.q + place_of(b, L, s.rq, s.kvh, min(rt * ROWS + n16, s.n_rows - 1)) * D;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 w = *(const uint4*)(qp + 64 * (i >> 1) + 16 * g + 8 * (i & 1));
+            pairs[4 * i] = w.x; pairs[4 * i + 1] = w.y; pairs[4 * i + 2] = w.z; pairs[4 * i + 3] = w.w;
+        }
+    };
+    struct Tile {
+        uint4 k[4];
+        uint2 v[8];                                                      // of key 4 g + i of block 0, then of block 1: channels 8 n16 .. + 7
+        uint32_t v_scale[2];
+        int k_scale[2];
+    };
+    const uint32_t k_at = n16 * D + 16 * g, v_at = 4 * g * D + 8 * n16;
+    auto load_as = [&](int ids, int nth, auto streamed, Tile& to) {
+        constexpr bool STREAM = decltype(streamed)::value;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const long long at = (long long)__builtin_amdgcn_readlane(ids, 2 * (nth & 31) + k) * 16;     // row of the pool
+            const unsigned char *kp = a.pools.k + at * D, *vp = a.pools.v + at * D;
+            to.k[2 * k] = fetch<uint4, STREAM>(kp, k_at);
+            to.k[2 * k + 1] = fetch<uint4, STREAM>(kp, k_at + 64);
+            to.k_scale[k] = (a.pools.k_scale + at)[(uint32_t)n16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to.v[4 * k + i] = fetch<uint2, STREAM>(vp, v_at + i * D);
+            to.v_scale[k] = *(const uint32_t*)(a.pools.v_scale + at + (uint32_t)(4 * g));
+        }
+    };
+    auto load = [&](int ids, int nth, bool stream, Tile& to) {
+        if (stream) {
+            asm volatile("" ::: "memory");                               // (the two ways are one load without a hint to the optimiser otherwise)
+            load_as(ids, nth, std::true_type{}, to);
+            asm volatile("" ::: "memory");
+        } else {
+            load_as(ids, nth, std::false_type{}, to);
+        }
+    };
+
+    constexpr bool AHEAD = RT == 1;                                      // one tile is computed, one travels (32 rows leave no registers for that)
+    Tile even, odd;
+    Segment now = next_segment();
+    if (now.t0 >= now.t1) return;
+    int ids = ask_ids(now, now.t0 + wave);
+    uint32_t pairs[RT][16];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) ask_q(now, rt, pairs[rt]);
+    bool stream = streamed(now);
+    if (AHEAD && now.t0 + wave < now.t1) load(ids, 0, stream, even);
+    for (bool first_segment = true;; first_segment = false) {
+        const int all_see = CAUSAL ? now.rq.P + 1 : now.rq.P;            // keys that every row sees
+        int limit[RT];                                                   // last key that the lane's row sees
+        QParts q[RT];
         float m[RT], l[RT];
         f32x4 o[RT][8];                                                  // channels 32 g + 8 v + i of the row, in o[i][v]
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
+            limit[rt] = CAUSAL ? now.rq.P + L.by_G.quotient(min(rt * ROWS + n16, now.n_rows - 1)) : now.rq.P - 1;
+            q[rt] = split_q(pairs[rt]);
             m[rt] = -INFINITY;
             l[rt] = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[rt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        // lane 2 j + k: block k of the wave's j-th tile from `ids_from` on, in 16-key blocks of the pool
-        int ids = 0;
-        auto ask_ids = [&](int from) {
-            const int blk = min(2 * (from + WAVES * (lane >> 1)) + (lane & 1), last_block);
-            const int page = min(max(pt[blk >> b.page_shift], 0), b.num_pages - 1);
-            ids = ((page * b.num_kv_heads + kvh) << b.page_shift) + (blk & ((1 << b.page_shift) - 1));
-        };
-        int nth = 0;
-        for (int t = t0 + wave; t < t1; t += WAVES, ++nth) {
-            if ((nth & 31) == 0) ask_ids(t);
-            uint4 kc[4];
-            uint2 v[8];
-            uint32_t vs[2];
-            int ks[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const long long at = (long long)__builtin_amdgcn_readlane(ids, 2 * (nth & 31) + k) * 16;     // row of the pool
-                const unsigned char* kp = a.pools.k + at * D + n16 * D + 16 * g;
-                kc[2 * k] = *(const uint4*)kp;
-                kc[2 * k + 1] = *(const uint4*)(kp + 64);
-                ks[k] = (a.pools.k_scale + at)[n16];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[4 * k + i] = *(const uint2*)(a.pools.v + at * D + (4 * g + i) * D + 8 * n16);
-                vs[k] = *(const uint32_t*)(a.pools.v_scale + at + 4 * g);
-            }
+        // what the next segment begins with travels over this one's tiles
+        const Segment then = next_segment();
+        const bool more = then.t0 < then.t1;
+        int then_ids = 0;
+        if (more) {
+            then_ids = ask_ids(then, then.t0 + wave);
+            if (AHEAD) ask_q(then, 0, pairs[0]);
+        }
+
+        auto compute = [&](int t, Tile& tile) {
+            uint2 (&v)[8] = tile.v;
+            uint32_t (&vs)[2] = tile.v_scale;
             f32x4 s[RT][2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const i32x8 kf = {(int)kc[2 * k].x, (int)kc[2 * k].y, (int)kc[2 * k].z, (int)kc[2 * k].w, (int)kc[2 * k + 1].x, (int)kc[2 * k + 1].y, (int)kc[2 * k + 1].z,
-                                  (int)kc[2 * k + 1].w};
+                const uint4 k0 = tile.k[2 * k], k1 = tile.k[2 * k + 1];
+                const i32x8 kf = {(int)k0.x, (int)k0.y, (int)k0.z, (int)k0.w, (int)k1.x, (int)k1.y, (int)k1.z, (int)k1.w};
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     s[rt][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    s[rt][k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, q[rt].high, s[rt][k], 0, 0, 0, ks[k], 0, q[rt].scale_high);
-                    s[rt][k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, q[rt].low, s[rt][k], 0, 0, 0, ks[k], 0, q[rt].scale_low);
+                    s[rt][k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, q[rt].high, s[rt][k], 0, 0, 0, tile.k_scale[k], 0, q[rt].scale_high);
+                    s[rt][k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, q[rt].low, s[rt][k], 0, 0, 0, tile.k_scale[k], 0, q[rt].scale_low);
                 }
             }
             const int key0 = t * TILE + 4 * g;                           // key of score (k, i): key0 + 16 k + i
@@ -252,7 +321,7 @@ __global__ __launch_bounds__(64 * WAVES) void attn_fp8_rows_kernel(AttnFp8Args a
 #pragma unroll
                         for (int rt = 0; rt < RT; ++rt)
                             if (key > limit[rt]) s[rt][k][i] = -INFINITY;
-                        if (key >= ctx) {                                // whatever lies there must not meet a weight of zero
+                        if (key >= now.ctx) {                            // whatever lies there must not meet a weight of zero
                             v[4 * k + i] = make_uint2(0, 0);
                             vs[k] = (vs[k] & ~(0xffu << (8 * i))) | (uint32_t)BIAS << (8 * i);
                         }
@@ -303,150 +372,217 @@ __global__ __launch_bounds__(64 * WAVES) void attn_fp8_rows_kernel(AttnFp8Args a
                     add(i, __builtin_bit_cast(bf16x8, w));
                 }
             };
-            auto values = [&](int i, bf16x8 vf) {
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) o[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rt], o[rt][i], 0, 0, 0);
-            };
-            if (masked && __builtin_amdgcn_ballot_w64(nans != 0) != 0) {
+            bf16x8 sees[RT];
+            uint2 marks[8];
+            const bool some_nan = masked && __builtin_amdgcn_ballot_w64(nans != 0) != 0;
+            if (some_nan) {
                 // A NaN in V of a key that only some of the rows see: a weight of zero does not keep it out.  It is taken out, and the rows
                 // that see such a key get it afterwards, by a product of which is what.
-                uint2 marks[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint32_t nx = nan_bytes(v[i].x) >> 7, ny = nan_bytes(v[i].y) >> 7;    // 1 in each byte that is a NaN
                     marks[i] = make_uint2(nx * 0x38u, ny * 0x38u);                              // the code of 1.0
                     v[i] = make_uint2(v[i].x & ~(nx * 0xffu), v[i].y & ~(ny * 0xffu));
-                }
-                product(values);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    v[k] = marks[k];
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) p[rt][k] = key0 + 16 * (k >> 2) + (k & 3) <= limit[rt] ? (__bf16)1.0f : (__bf16)0.0f;
+                    for (int rt = 0; rt < RT; ++rt) sees[rt][i] = key0 + 16 * (i >> 2) + (i & 3) <= limit[rt] ? (__bf16)1.0f : (__bf16)0.0f;
                 }
+            }
+            product([&](int i, bf16x8 vf) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) o[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rt], o[rt][i], 0, 0, 0);
+            });
+            if (some_nan) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = marks[i];
                 product([&](int i, bf16x8 vf) {
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
-                        const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rt], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                        const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, sees[rt], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             if (hit[k] > 0.f) o[rt][i][k] = __builtin_nanf("");
                     }
                 });
-            } else {
-                product(values);
+            }
+        };
+        int nth = 0;
+        auto step = [&](int t, Tile& tile, Tile& next) {                 // tile t; the one after it is asked for first
+            if (t + WAVES < now.t1) {
+                ++nth;
+                if ((nth & 31) == 0) ids = ask_ids(now, t + WAVES);
+                load(ids, nth, stream, next);
+            }
+            compute(t, tile);
+        };
+        if constexpr (AHEAD) {
+            for (int t = now.t0 + wave; t < now.t1; t += 2 * WAVES) {
+                step(t, even, odd);
+                if (t + WAVES < now.t1) step(t + WAVES, odd, even);
+            }
+        } else {
+            for (int t = now.t0 + wave; t < now.t1; t += WAVES, ++nth) {
+                if (nth > 0 && (nth & 31) == 0) ids = ask_ids(now, t);
+                load(ids, nth, stream, even);
+                compute(t, even);
             }
         }
-        // the waves' parts of 16 rows at a time, 8 channels of a row per thread
-        const bool whole = t0 == 0 && t1 == rq.tiles;
+        if (more) {
+            ids = then_ids;
+            stream = streamed(then);
+            if (AHEAD && then.t0 + wave < then.t1) load(ids, 0, stream, even);
+        }
+
+        // The waves' parts, 16 rows at a time, in the order of the accumulators: four of them, channels 32 g + 8 k + i for k = 0 .. 3, are
+        // the 16 bytes at place i * 64 + lane.  A thread adds up SUMS places, its own and those that far behind.
+        const bool whole = now.t0 == 0 && now.t1 == now.rq.tiles;
         float* rec = (float*)a.workspace + (2ll * blockIdx.x + (first_segment ? 0 : 1)) * RECORD_FLOATS<RT>;
-        first_segment = false;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            if (rt * ROWS >= n_rows) break;                              // (the same for all waves)
+            if (rt * ROWS >= now.n_rows) break;                          // (the same for all waves)
             __syncthreads();
             const float l_row = row_sum(l[rt]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) part_o[wave][n16][32 * g + 8 * k + i] = o[rt][i][k];
-            if (g == 0) {
-                part_m[wave][n16] = m[rt];
-                part_l[wave][n16] = l_row;
-            }
+            for (int i = 0; i < 8; ++i) part_o[wave][i * 64 + lane] = o[rt][i];
+            if (g == 0) part_ml[wave][n16] = f32x2{m[rt], l_row};
             __syncthreads();
-            const int in_rows = threadIdx.x >> 4, ch = (threadIdx.x & 15) * 8, row = rt * ROWS + in_rows;
-            if (row >= n_rows) continue;
-            float top = -INFINITY, sum = 0.f, acc[8] = {};
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) top = fmaxf(top, part_m[w][in_rows]);
-            const float ref = top == -INFINITY ? 0.f : top;
+            float top = -INFINITY, sum = 0.f;
+            f32x2 ml[WAVES];
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
-                const float f = __builtin_amdgcn_exp2f(part_m[w][in_rows] - ref);
-                sum = fmaf(part_l[w][in_rows], f, sum);
+                ml[w] = part_ml[w][n16];
+                top = fmaxf(top, ml[w][0]);
+            }
+            const float ref = top == -INFINITY ? 0.f : top;
+            f32x4 acc[SUMS] = {};
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] = fmaf(part_o[w][in_rows][ch + i], f, acc[i]);
+            for (int w = 0; w < WAVES; ++w) {
+                const float f = __builtin_amdgcn_exp2f(ml[w][0] - ref);
+                sum = fmaf(ml[w][1], f, sum);
+#pragma unroll
+                for (int h = 0; h < SUMS; ++h) {
+                    const f32x4 part = part_o[w][threadIdx.x + 64 * WAVES * h];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[h][k] = fmaf(part[k], f, acc[h][k]);
+                }
             }
             if (!whole) {
-                *(f32x4*)(rec + row * D + ch) = f32x4{acc[0], acc[1], acc[2], acc[3]};
-                *(f32x4*)(rec + row * D + ch + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
-                if ((threadIdx.x & 15) == 0) *(f32x2*)(rec + RT * ROWS * D + 2 * row) = f32x2{top, sum};
+#pragma unroll
+                for (int h = 0; h < SUMS; ++h) *(f32x4*)(rec + (rt * 512 + threadIdx.x + 64 * WAVES * h) * 4) = acc[h];
+                if (threadIdx.x < ROWS) *(f32x2*)(rec + RT * ROWS * D + 2 * (rt * ROWS + threadIdx.x)) = f32x2{top, sum};
                 continue;
             }
-            const int tok = L.by_G.quotient(row);
-            const long long dst = (long long)(rq.first_row + tok) * b.num_q_heads + kvh * L.G + row - tok * L.G;
+            // finished: rows in order again, through LDS
             const float inv = sum == 0.f ? 0.f : 1.0f / sum;             // no key at all: a row of zeros
-            bf16x8 res;
+            __syncthreads();
+            __bf16* rows = (__bf16*)part_o;                              // [16][OUT_STRIDE]
 #pragma unroll
-            for (int i = 0; i < 8; ++i) res[i] = (__bf16)(acc[i] * inv);
-            *(bf16x8*)((__bf16*)a.out + dst * D + ch) = res;
-            if (a.lse != nullptr && (threadIdx.x & 15) == 0) a.lse[dst] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
+            for (int h = 0; h < SUMS; ++h)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) rows[n16 * OUT_STRIDE + 32 * g + 8 * k + wave + WAVES * h] = (__bf16)(acc[h][k] * inv);
+            __syncthreads();
+            const int out_row = threadIdx.x >> 4;
+            if (threadIdx.x < 16 * ROWS && rt * ROWS + out_row < now.n_rows)
+                *(uint4*)((__bf16*)a.out + place_of(b, L, now.rq, now.kvh, rt * ROWS + out_row) * D + 8 * n16) = *(const uint4*)(rows + out_row * OUT_STRIDE + 8 * n16);
+            if (a.lse != nullptr && threadIdx.x < ROWS && rt * ROWS + n16 < now.n_rows)
+                a.lse[place_of(b, L, now.rq, now.kvh, rt * ROWS + n16)] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
         }
+        if (!more) return;
+        if (!AHEAD) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) ask_q(then, rt, pairs[rt]);
+        }
+        now = then;
     }
 }
 
-// The records of a row of a pair that several workgroups had parts of.  Half a wave takes a record at a time, 4 channels a lane.
-template <bool CAUSAL, int RT>
-__global__ __launch_bounds__(64 * WAVES) void attn_fp8_merge_rows_kernel(AttnFp8Args a, RowsLayout L, int rows_most)
+// The records of a pair that several workgroups had parts of: a workgroup for 32 channels (a lane group of the records) of 16 rows,
+// 128 threads of it a record at a time.
+template <bool CAUSAL, int RT, int THREADS>
+__global__ __launch_bounds__(THREADS) void attn_fp8_merge_rows_kernel(AttnFp8Args a, RowsLayout L)
 {
+    constexpr int TEAMS = THREADS / 128, AT_ONCE = 8;
     const BatchView& b = a.b;
-    const int row = blockIdx.x % rows_most, pair = blockIdx.x / rows_most;
+    const int g = blockIdx.x & 3, rt = RT == 1 ? 0 : (blockIdx.x >> 2) & 1, pair = blockIdx.x >> (RT == 1 ? 2 : 3);
     const int r = L.by_kv_heads.quotient(pair), kvh = pair - r * b.num_kv_heads;
     Line<CAUSAL> line(b);
-    const long long all = line.total * b.num_kv_heads;
+    const int all = line.total * b.num_kv_heads;
+    if (all == 0) return;
     const int share = part_tiles(L, all);
     const Request rq = line.request(r);
-    if (row >= rq.N * L.G || rq.tiles == 0) return;
-    const long long x = rq.before * b.num_kv_heads + (long long)kvh * rq.tiles;
-    const int w0 = (int)(x / share), w1 = (int)((x + rq.tiles - 1) / share);
+    const int n_rows = min(rq.N * L.G, RT * ROWS);
+    if (rt * ROWS >= n_rows || rq.tiles == 0) return;
+    const int x = rq.before * b.num_kv_heads + kvh * rq.tiles;
+    const int w0 = small_quotient(x, share), w1 = small_quotient(x + rq.tiles - 1, share);
     if (w0 == w1) return;                                                // done where it was
-    __shared__ float part[2 * WAVES][D + 4];
-    __shared__ float part_l[2 * WAVES];
-    const int lane = threadIdx.x & 63, half = threadIdx.x >> 5, ch = (threadIdx.x & 31) * 4;
+    __shared__ f32x4 part[TEAMS][128];
+    __shared__ f32x2 part_ml[TEAMS][ROWS];
+    __shared__ __bf16 rows[ROWS][40];
+    const int team = threadIdx.x >> 7, in_team = threadIdx.x & 127, i = in_team >> 4, n16 = threadIdx.x & 15;
     // the first workgroup's record is its last pair's, unless the pair is where its part begins; of the others it is the first
-    auto record = [&](int w) { return (const float*)a.workspace + (2ll * w + (w == w0 && x != (long long)w0 * share ? 1 : 0)) * RECORD_FLOATS<RT>; };
-    float top = -INFINITY;
-    for (int w = w0 + lane; w <= w1; w += 64) top = fmaxf(top, record(w)[RT * ROWS * D + 2 * row]);
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
-    const float ref = top == -INFINITY ? 0.f : top;
+    auto record = [&](int w) { return (const float*)a.workspace + (2ll * w + (w == w0 && x != w0 * share ? 1 : 0)) * RECORD_FLOATS<RT>; };
+    const int ml_at = RT * ROWS * D + 2 * (rt * ROWS + n16), v_at = (rt * 512 + i * 64 + 16 * g + n16) * 4;
+    float top = -INFINITY, sum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-#pragma unroll 4
-    for (int w = w0 + half; w <= w1; w += 2 * WAVES) {
-        const float* rec = record(w);
-        const f32x4 v = *(const f32x4*)(rec + row * D + ch);
-        const f32x2 ml = *(const f32x2*)(rec + RT * ROWS * D + 2 * row);
+    // what there is in terms of a larger reference, and more of it
+    auto raise = [&](float to) -> float {
+        const float ref = to == -INFINITY ? 0.f : to, f = __builtin_amdgcn_exp2f(top - ref);
+        top = to;
+        sum *= f;
+        acc *= f;
+        return ref;
+    };
+    auto take = [&](f32x4 v, float ref, f32x2 ml) {
         const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
         sum = fmaf(ml[1], f, sum);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = fmaf(v[i], f, acc[i]);
+        for (int k = 0; k < 4; ++k) acc[k] = fmaf(v[k], f, acc[k]);
+    };
+    for (int from = w0 + team; from <= w1; from += TEAMS * AT_ONCE) {
+        f32x4 v[AT_ONCE];
+        f32x2 ml[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const float* rec = record(min(from + TEAMS * u, w1));
+            v[u] = *(const f32x4*)(rec + v_at);
+            ml[u] = *(const f32x2*)(rec + ml_at);
+        }
+        float most = top;
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (from + TEAMS * u <= w1) most = fmaxf(most, ml[u][0]);
+        const float ref = raise(most);
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (from + TEAMS * u <= w1) take(v[u], ref, ml[u]);
     }
-    *(f32x4*)&part[half][ch] = acc;
-    if ((threadIdx.x & 31) == 0) part_l[half] = sum;
+    if (team > 0) {
+        part[team][in_team] = acc;
+        if (i == 0) part_ml[team][n16] = f32x2{top, sum};
+    }
     __syncthreads();
-    if (threadIdx.x >= 32) return;
-    sum = 0.f;
-    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (team == 0) {
+        float most = top;
 #pragma unroll
-    for (int i = 0; i < 2 * WAVES; ++i) {
-        sum += part_l[i];
-        acc += *(const f32x4*)&part[i][ch];
+        for (int w = 1; w < TEAMS; ++w) most = fmaxf(most, part_ml[w][n16][0]);
+        const float ref = raise(most);
+#pragma unroll
+        for (int w = 1; w < TEAMS; ++w) take(part[w][in_team], ref, part_ml[w][n16]);
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) rows[n16][8 * k + i] = (__bf16)(acc[k] * inv);
+        if (a.lse != nullptr && g == 0 && i == 0 && rt * ROWS + n16 < n_rows)
+            a.lse[place_of(b, L, rq, kvh, rt * ROWS + n16)] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
     }
-    const int tok = L.by_G.quotient(row);
-    const long long dst = (long long)(rq.first_row + tok) * b.num_q_heads + kvh * L.G + row - tok * L.G;
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    bf16x4 res;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) res[i] = (__bf16)(acc[i] * inv);
-    *(bf16x4*)((__bf16*)a.out + dst * D + ch) = res;
-    if (a.lse != nullptr && threadIdx.x == 0) a.lse[dst] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
+    __syncthreads();
+    const int out_row = threadIdx.x >> 2, at = 8 * (threadIdx.x & 3);
+    if (threadIdx.x < 64 && rt * ROWS + out_row < n_rows)
+        *(uint4*)((__bf16*)a.out + place_of(b, L, rq, kvh, rt * ROWS + out_row) * D + 32 * g + at) = *(const uint4*)&rows[out_row][at];
 }
 
 constexpr int MOST_ROWS = 2 * ROWS;
 long long rows_of(const BatchView& b) { return (long long)b.max_new_len * (b.num_q_heads / b.num_kv_heads); }
+// tiles that the page table could hold
+long long line_of(const BatchView& b) { return ((long long)b.max_pages * b.page_size + TILE - 1) / TILE * b.num_reqs * b.num_kv_heads; }
 
 RowsLayout layout_of(const BatchView& b)
 {
@@ -454,10 +590,9 @@ RowsLayout layout_of(const BatchView& b)
     L.G = b.num_q_heads / b.num_kv_heads;
     L.by_G = divisor_of(L.G);
     L.by_kv_heads = divisor_of(b.num_kv_heads);
-    L.least = LEAST_TILES;
     // no more workgroups than the page table can hold work for
-    const long long tiles = ((long long)b.max_pages * b.page_size + TILE - 1) / TILE, all = tiles * b.num_reqs * b.num_kv_heads;
-    L.workgroups = (int)std::min<long long>(WORKGROUPS, (all + L.least - 1) / L.least);
+    L.workgroups = (int)std::max<long long>(std::min<long long>(WORKGROUPS, (line_of(b) + LEAST_TILES - 1) / LEAST_TILES), 1);
+    L.by_workgroups = divisor_of(L.workgroups);
     return L;
 }
 size_t rows_workspace_bytes(const BatchView& b) { return 2 * (size_t)layout_of(b).workgroups * (rows_of(b) <= ROWS ? RECORD_FLOATS<1> : RECORD_FLOATS<2>) * sizeof(float); }
@@ -466,25 +601,32 @@ template <bool CAUSAL, int RT>
 hipError_t launch_rows(const AttnFp8Args& a, hipStream_t stream)
 {
     const RowsLayout L = layout_of(a.b);
-    const int rows = (int)rows_of(a.b);
     hipLaunchKernelGGL((attn_fp8_rows_kernel<CAUSAL, RT>), dim3(L.workgroups), dim3(64 * WAVES), 0, stream, a, L);
-    if (L.workgroups > 1)
-        hipLaunchKernelGGL((attn_fp8_merge_rows_kernel<CAUSAL, RT>), dim3((unsigned)a.b.num_reqs * a.b.num_kv_heads * rows), dim3(64 * WAVES), 0, stream, a, L, rows);
+    // few pairs have many records each: more of them at a time
+    const long long pairs = (long long)a.b.num_reqs * a.b.num_kv_heads;
+    const dim3 grid((unsigned)(pairs * 4 * RT));
+    if (L.workgroups > MANY_RECORDS * pairs) hipLaunchKernelGGL((attn_fp8_merge_rows_kernel<CAUSAL, RT, 1024>), grid, dim3(1024), 0, stream, a, L);
+    else if (L.workgroups > 1) hipLaunchKernelGGL((attn_fp8_merge_rows_kernel<CAUSAL, RT, 256>), grid, dim3(256), 0, stream, a, L);
     return hipGetLastError();
 }
 
 }  // namespace
 
 // Few rows of a (request, KV head): their keys are split over the chip.  Many: rows over the waves, keys through LDS.
+// (Tables so wide that the line could pass 2^31 tiles, a terabyte of cache or pages shared by thousands, go the second way.)
+namespace {
+bool few_rows(const BatchView& b) { return rows_of(b) <= MOST_ROWS && line_of(b) < (1ll << 31) - (1 << 20); }
+}  // namespace
+
 size_t attn_fp8_workspace_bytes(const BatchView& b)
 {
     if (b.num_reqs == 0 || b.total_new_tokens == 0) return 0;
-    return rows_of(b) <= MOST_ROWS ? rows_workspace_bytes(b) : attn_fp8_tiles_workspace_bytes(b);
+    return few_rows(b) ? rows_workspace_bytes(b) : attn_fp8_tiles_workspace_bytes(b);
 }
 
 hipError_t launch_attn_fp8(const AttnFp8Args& a, bool causal, hipStream_t stream)
 {
-    if (rows_of(a.b) > MOST_ROWS) return launch_attn_fp8_tiles(a, causal, stream);
+    if (!few_rows(a.b)) return launch_attn_fp8_tiles(a, causal, stream);
     if (rows_of(a.b) <= ROWS) return causal ? launch_rows<true, 1>(a, stream) : launch_rows<false, 1>(a, stream);
     return causal ? launch_rows<true, 2>(a, stream) : launch_rows<false, 2>(a, stream);
 }

@@ -27,8 +27,6 @@ namespace {
 
 using namespace fp8;
 using bf16attn::lds_dma16;
-using bf16attn::pair_max;
-using bf16attn::pair_sum;
 using bf16attn::swap23;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -190,23 +188,18 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     int q_scale_high, q_scale_low;
     {
         const __bf16* qp = (const __bf16*)a.q + ((long long)(e.first_row + tok) * b.num_q_heads + u.kvh * L.G + row - tok * L.G) * HEAD_DIM + 32 * h32;
-        bf16x8 v[8];
+        uint32_t pairs[32];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = *(const bf16x8*)(qp + 64 * (i >> 2) + 8 * (i & 3));
-        uint32_t most = 0;
-#pragma unroll
-        for (int i = 0; i < 64; ++i) {
-            const float x = (float)v[i >> 3][i & 7];
-            most = max(most, finite(x) ? __float_as_uint(x) & 0x7fffffffu : 0u);
+        for (int i = 0; i < 8; ++i) {
+            const uint4 x = *(const uint4*)(qp + 64 * (i >> 2) + 8 * (i & 3));
+            pairs[4 * i] = x.x; pairs[4 * i + 1] = x.y; pairs[4 * i + 2] = x.z; pairs[4 * i + 3] = x.w;
         }
-        most = __float_as_uint(pair_max(__uint_as_float(most)));
-        q_scale_high = scale_byte(most);
-        q_scale_low = q_scale_high + LOW_PART_SCALE;
-        const float down = down_scale(q_scale_high);
+        const uint32_t most = __float_as_uint(max32(__uint_as_float(most_of(pairs))));
+        q_scale_high = q_scale_byte(most);
+        q_scale_low = q_scale_high == 0xff ? 0xff : q_scale_high + LOW_PART_SCALE;
 #pragma unroll
         for (int w = 0; w < 16; ++w) {
-            const float x[4] = {(float)v[w >> 1][4 * (w & 1)], (float)v[w >> 1][4 * (w & 1) + 1], (float)v[w >> 1][4 * (w & 1) + 2], (float)v[w >> 1][4 * (w & 1) + 3]};
-            const QCodes c = split4(x, down);
+            const QCodes c = split4(pairs[2 * w], pairs[2 * w + 1], q_scale_high);
             q_high[w >> 3][w & 7] = (int)c.high;
             q_low[w >> 3][w & 7] = (int)c.low;
         }
@@ -332,7 +325,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int v = 0; v < 16; ++v) x = fmaxf(x, s[kb][v]);
-        return pair_max(x);
+        return max32(x);
     };
     auto scores = [&](int slot, f32x16 (&s)[2]) {            // not interleaved: first and only tiles
 #pragma unroll
@@ -489,7 +482,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
                 float sum = sum0 + sum1;
                 if (__builtin_amdgcn_ballot_w64(sum > LAG_LIMIT) != 0) {
                     // both lanes of a row decide alike
-                    if (pair_max(sum) > LAG_LIMIT) sum = raise(s_cur, p);
+                    if (max32(sum) > LAG_LIMIT) sum = raise(s_cur, p);
                 }
                 l += sum;
                 __builtin_amdgcn_s_waitcnt(0x0f70 | FETCHES);        // all fetches but this iteration's have landed
@@ -537,7 +530,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
             uint32_t p[16];
             float sum = odd ? weights(sc[1], p) : weights(sc[0], p);
             if (__builtin_amdgcn_ballot_w64(sum > LAG_LIMIT) != 0) {
-                if (pair_max(sum) > LAG_LIMIT) sum = odd ? raise(sc[1], p) : raise(sc[0], p);
+                if (max32(sum) > LAG_LIMIT) sum = odd ? raise(sc[1], p) : raise(sc[0], p);
             }
             l += sum;
             __syncthreads();
@@ -558,7 +551,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
             for (int v = 0; v < 16; ++v)
                 if ((poison >> (16 * nb + v)) & 1) o[nb][v] = __builtin_nanf("");
     }
-    const float l_row = pair_sum(l);
+    const float l_row = sum32(l);
     if (e.pieces > 1) {
         float* rec = (float*)a.workspace + (long long)(u.slot * u.parts + u.part) * RECORD_FLOATS;
 #pragma unroll
