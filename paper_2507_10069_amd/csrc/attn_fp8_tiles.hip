@@ -35,8 +35,9 @@ constexpr int BR = 32 * NW;                              // rows of a unit
 constexpr int BC = 64;                                   // keys of a tile
 constexpr int PLACES = 256;                              // workgroups that run at once: one on each compute unit
 constexpr int MAX_PARTS = 64;                            // pieces of a unit
-constexpr int MIN_TILES_ALONE = 2, MIN_TILES_BEHIND = 12;   // key tiles of a piece where no unit is whole, and behind whole ones
+constexpr int MIN_TILES_ALONE = 2, MIN_TILES_BEHIND = 4;    // key tiles of a piece where no unit is whole, and behind whole ones
 constexpr float LAG_LIMIT = 1048576.f;                   // 2^20
+constexpr int QK_OPS = 80;                               // of a tile's 119 softmax instructions beside the score products
 
 // LDS
 constexpr int K_TILE = BC * HEAD_DIM, V_TILE = BC * HEAD_DIM * 2, RAW_TILE = BC * HEAD_DIM;
@@ -84,7 +85,7 @@ __device__ inline Unit plan_unit(const BatchView& b, const Layout& L, int wg, in
     for (int first = 0; first < b.num_reqs; first += 64) total += look(first);
     const int units = total * b.num_kv_heads;
     const int full = L.cut ? units / PLACES * PLACES : units, rest = units - full;
-    const int stride = (rest + 7) & ~7;                  // pieces of a unit run on the XCD of the unit
+    const int stride = rest;
     u.parts = stride == 0 ? 1 : min(PLACES / stride, MAX_PARTS);
     u.part = 0;
     u.slot = 0;
@@ -233,7 +234,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     // ---- V to bf16: 16 channels of a key per lane.  Keys behind the context hold anything: zeros in their place.  In tiles that not every
     //      row sees whole, a NaN would reach rows that do not see it (0 * NaN): it becomes a zero too, and flags say that there was one.
     const int v_key = 8 * wave + (lane >> 3);
-    const int v_wr = V_AT + v_key * 256 + (((2 * (lane & 7) + ((v_key)&1)) ^ ((v_key & 3) << 2)) << 4);     // the first of its two chunks, by turns
+    // V tile: chunk c of 16 bytes of key k lies at place c ^ 4 (k mod 4) ^ (k mod 2): neither the transposing reads nor these stores meet a bank twice
+    const int v_wr = V_AT + v_key * 256 + (((2 * (lane & 7)) ^ ((v_key & 3) << 2) ^ (v_key & 1)) << 4);
     uint4 raw;
     int raw_scale;
     auto read_raw = [&](int raw_slot, int s_slot) {
@@ -259,12 +261,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
         const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true);
         return make_uint4(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1), __builtin_bit_cast(uint32_t, p2), __builtin_bit_cast(uint32_t, p3));
     };
-    auto store_v = [&](int v_slot) {                         // (odd rows store their upper half first: no bank twice)
-        const uint4 lo = widen(0), hi = widen(1);
-        const bool odd = (v_key & 1) != 0;
-        const uint4 first = odd ? hi : lo, second = odd ? lo : hi;
-        *(uint4*)(smem + v_slot * V_TILE + v_wr) = first;
-        *(uint4*)(smem + v_slot * V_TILE + (v_wr ^ 16)) = second;
+    auto store_v = [&](int v_slot) {
+        *(uint4*)(smem + v_slot * V_TILE + v_wr) = widen(0);
+        *(uint4*)(smem + v_slot * V_TILE + (v_wr ^ 16)) = widen(1);
     };
 
     // which of the lane's 64 outputs meet a NaN of V: bit 4 (4 nb + v / 4) + v % 4.  Rare: from global memory, key by key.
@@ -293,7 +292,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
         return i32x8{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
     };
     // within each 16 lanes, lane j gives the address of 4 channels of key k0 + j / 4 and gets keys k0 .. k0 + 3 of channel d0 + j
-    const int v_rd = V_AT + (8 * h32 + ((lane & 15) >> 2)) * 256 + ((4 * ((lane & 15) >> 2) + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) + (lane & 1) * 8;
+    const int v_rd = V_AT + (8 * h32 + ((lane & 15) >> 2)) * 256 + ((4 * ((lane & 15) >> 2) + 2 * ((lane >> 4) & 1) + (((lane & 3) >> 1) ^ ((lane >> 2) & 1))) << 4) + (lane & 1) * 8;
     auto read_v = [&](int slot, int k16, int nb) -> bf16x8 {     // keys 16 k16 .. + 15, channels 32 nb .. + 31
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         const unsigned char* src = smem + slot * V_TILE + 16 * k16 * 256 + (v_rd ^ (nb << 6));
@@ -341,13 +340,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
             }
         }
     };
-    // weights of a tile, packed, and their sum over the lane's keys
-    auto weights = [&](const f32x16 (&s)[2], uint32_t (&p)[16]) -> float {
+    // weights of half a tile (32 keys), packed, and their sum over the lane's keys
+    auto weights = [&](const f32x16& s, uint32_t* p) -> float {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 8; ++i) {
             bf16x2 w;
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 3][2 * (i & 7)], c_log2, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[i >> 3][2 * (i & 7) + 1], c_log2, -m));
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[2 * i], c_log2, -m)), y = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], c_log2, -m));
             sum += x + y;
             w[0] = (__bf16)x;
             w[1] = (__bf16)y;
@@ -355,18 +354,29 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
         }
         return sum;
     };
-    // the tile's weights have outgrown the reference: it becomes the row's maximum so far, and they are made again
-    auto raise = [&](const f32x16 (&s)[2], uint32_t (&p)[16]) -> float {
-        const float to = fmaxf(m, row_max(s) * c_log2), scale = __builtin_amdgcn_exp2f(m - to);
-        m = to;
-        l *= scale;
+    // The weights of a half, which sum to `sum`, are about to be used: where they have outgrown the reference it becomes the row's
+    // maximum so far, and they are made again; and where it has changed since they were made from `ref`.
+    auto settle = [&](const f32x16& s, uint32_t* p, float sum, float ref) {
+        const bool grown = sum > LAG_LIMIT;
+        if (__builtin_amdgcn_ballot_w64(grown || m != ref) != 0) {
+            // (both lanes of a row decide alike)
+            if (max32(sum) > LAG_LIMIT) {
+                float top = s[0];
 #pragma unroll
-        for (int nb = 0; nb < 4; ++nb)
+                for (int v = 1; v < 16; ++v) top = fmaxf(top, s[v]);
+                const float to = fmaxf(m, max32(top) * c_log2), scale = __builtin_amdgcn_exp2f(m - to);
+                m = to;
+                l *= scale;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) o[nb][v] *= scale;
-        return weights(s, p);
+                for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) o[nb][v] *= scale;
+            }
+            if (m != ref) sum = weights(s, p);
+        }
+        l += sum;
     };
-    auto p_operand = [&](const uint32_t (&p)[16], int k16) -> bf16x8 {
+    auto p_operand = [&](const uint32_t* p, int k16) -> bf16x8 {
         return __builtin_bit_cast(bf16x8, u32x4{p[4 * k16], p[4 * k16 + 1], p[4 * k16 + 2], p[4 * k16 + 3]});
     };
     auto flagged = [&](int v_slot) -> bool {
@@ -422,7 +432,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
                 f32x16 (&s_cur)[2] = sc[R & 1];
                 f32x16 (&s_nxt)[2] = sc[(R & 1) ^ 1];
                 uint32_t p[16];
-                float fa[16], fb[16], ea[16], eb[16], sum0 = 0.f, sum1 = 0.f;
+                float fa[16], fb[16], ea[16], eb[16], sums[4] = {};
                 const float ref = m;
                 // pair g: F F (scale, subtract), E E (exp2), A A (sums), C (round): a stream in which nothing follows what it depends on
                 auto softmax_op = [&](auto idx_c) {
@@ -446,14 +456,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
                         fb[g + 1] = fmaf(s_cur[(g + 1) >> 3][2 * ((g + 1) & 7) + 1], c_log2, -ref);
                         pin(fb[g + 1]);
                     } else if constexpr (slot == 5 && g >= 1) {
-                        sum0 += ea[g - 1];
-                        pin(sum0);
+                        sums[2 * ((g - 1) >> 3)] += ea[g - 1];
+                        pin(sums[2 * ((g - 1) >> 3)]);
                     } else if constexpr (slot == 6 && g >= 1) {
-                        sum1 += eb[g - 1];
-                        pin(sum1);
+                        sums[2 * ((g - 1) >> 3) + 1] += eb[g - 1];
+                        pin(sums[2 * ((g - 1) >> 3) + 1]);
                     }
                 };
-                constexpr int OPS = 17 * 7;
+                constexpr int OPS = 17 * 7, OPS_HERE = QK_OPS;   // (pairs 0 .. 7, the first half, are done after 63)
                 fa[0] = fmaf(s_cur[0][0], c_log2, -ref);
                 fb[0] = fmaf(s_cur[0][1], c_log2, -ref);
                 const int scale0 = smem[ks_rd + KS * 128], scale1 = smem[ks_rd + KS * 128 + 32];
@@ -473,18 +483,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
                         s_nxt[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[k >> 1], low ? q_low[st] : q_high[st], s_nxt[kb], 0, 0, 0, kb ? scale1 : scale0, 0,
                                                                                     low ? q_scale_low : q_scale_high);
                     }
-                    static_for<(k * OPS) / 8, ((k + 1) * OPS) / 8>(softmax_op);
+                    static_for<(k * OPS_HERE) / 8, ((k + 1) * OPS_HERE) / 8>(softmax_op);
                     if constexpr (k == 1) fetch_k(i + 3, (R + 3) & 3);
                     if constexpr (k == 2) fetch_v(i + 2, R & 1);
                     if constexpr (k == 3) fetch_scales(i + 3, (R + 3) & 3);
                     __builtin_amdgcn_sched_barrier(0);
                 });
-                float sum = sum0 + sum1;
-                if (__builtin_amdgcn_ballot_w64(sum > LAG_LIMIT) != 0) {
-                    // both lanes of a row decide alike
-                    if (max32(sum) > LAG_LIMIT) sum = raise(s_cur, p);
-                }
-                l += sum;
+                settle(s_cur[0], p, sums[0] + sums[1], ref);
                 __builtin_amdgcn_s_waitcnt(0x0f70 | FETCHES);        // all fetches but this iteration's have landed
                 __syncthreads();
                 __builtin_amdgcn_sched_barrier(0);
@@ -500,9 +505,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
                 static_for<0, 16>([&](auto kc) {
                     constexpr int k = decltype(kc)::value;
                     if constexpr (k + 2 < 16) vf[k + 2] = read_v(VS, (k + 2) >> 2, (k + 2) & 3);
-                    o[k & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k], p_operand(p, k >> 2), o[k & 3], 0, 0, 0);
-                    if constexpr (k == 4) store_v(VN);
                     if constexpr (k == 8) {
+                        settle(s_cur[1], p + 8, sums[2] + sums[3], ref);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    o[k & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k], p_operand(p, k >> 2), o[k & 3], 0, 0, 0);
+                    if constexpr (k < 8) static_for<OPS_HERE + (k * (OPS - OPS_HERE)) / 8, OPS_HERE + ((k + 1) * (OPS - OPS_HERE)) / 8>(softmax_op);
+                    if constexpr (k == 10) store_v(VN);
+                    if constexpr (k == 12) {
                         if (i + 1 >= wave_clear) {
                             __builtin_amdgcn_sched_barrier(0);
                             mask_tile(i + 1, s_nxt);
@@ -525,20 +535,22 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
                 iteration(i + 3, std::integral_constant<int, 3>{});
                 i += 4;
             }
-            // the last tile
+            // the last tile, a half at a time: the first half's values are taken before the second half may raise the reference
             const int odd = (n_tiles - 1) & 1;
-            uint32_t p[16];
-            float sum = odd ? weights(sc[1], p) : weights(sc[0], p);
-            if (__builtin_amdgcn_ballot_w64(sum > LAG_LIMIT) != 0) {
-                if (max32(sum) > LAG_LIMIT) sum = odd ? raise(sc[1], p) : raise(sc[0], p);
-            }
-            l += sum;
             __syncthreads();
             if (CAUSAL && t_end - 1 >= unit_clear) {
                 if (flagged(odd)) find_poison(t_end - 1);
             }
 #pragma unroll
-            for (int k = 0; k < 16; ++k) o[k & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(odd, k >> 2, k & 3), p_operand(p, k >> 2), o[k & 3], 0, 0, 0);
+            for (int h = 0; h < 2; ++h) {
+                uint32_t p[8];
+                const float ref = m;
+                if (odd) settle(sc[1][h], p, weights(sc[1][h], p), ref);
+                else settle(sc[0][h], p, weights(sc[0][h], p), ref);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    o[k & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(odd, 2 * h + (k >> 2), k & 3), p_operand(p, k >> 2), o[k & 3], 0, 0, 0);
+            }
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);                  // the last fetches have landed, and
         __syncthreads();                                     // all are past their reads: the rings are free
@@ -585,49 +597,88 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     }
 }
 
-// the pieces of the units that were cut: a workgroup per unit and wave of rows, a thread for a quarter of a lane's accumulators
+// The pieces of the units that were cut: a workgroup per unit, wave of rows and block of 32 channels; its four waves take the
+// pieces in turn, four at a time.
 template <bool CAUSAL>
 __global__ __launch_bounds__(256) void attn_fp8_merge_tiles_kernel(AttnFp8Args a, Layout L)
 {
+    constexpr int TEAMS = 4, AT_ONCE = 4;
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     const BatchView& b = a.b;
-    const Unit u = plan_unit(b, L, 0, blockIdx.x / NW);
+    const Unit u = plan_unit(b, L, 0, blockIdx.x / (4 * NW));
     if (u.req < 0) return;
     const Extent e = extent_of<CAUSAL>(b, L, u, L.units_max <= PLACES);
-    const int wave = blockIdx.x % NW, lane = threadIdx.x & 63, nb = threadIdx.x >> 6;
+    const int wave = (blockIdx.x >> 2) % NW, nb = blockIdx.x & 3, lane = threadIdx.x & 63, team = threadIdx.x >> 6;
     const int row = e.row0 + 32 * wave + (lane & 31);
     if (e.pieces < 2 || e.row0 + 32 * wave >= e.n_rows) return;
+    __shared__ f32x4 part[TEAMS][4][64];
+    __shared__ f32x2 part_ml[TEAMS][64];
     const float* rec = (const float*)a.workspace + (long long)(u.slot * u.parts) * RECORD_FLOATS;
     const int col = 64 * wave + lane;
-    float top = -INFINITY;
-    for (int p = 0; p < e.pieces; ++p) top = fmaxf(top, rec[(long long)p * RECORD_FLOATS + 64 * 64 * NW + 2 * col]);
-    const float ref = top == -INFINITY ? 0.f : top;
     f32x4 acc[4] = {};
-    float sum = 0.f;
-    for (int p = 0; p < e.pieces; ++p) {
-        const float* one = rec + (long long)p * RECORD_FLOATS;
-        const f32x2 ml = *(const f32x2*)(one + 64 * 64 * NW + 2 * col);
+    float top = -INFINITY, sum = 0.f;
+    auto raise = [&](float to) -> float {                    // what there is in terms of a larger reference
+        const float ref = to == -INFINITY ? 0.f : to, f = __builtin_amdgcn_exp2f(top - ref);
+        top = to;
+        sum *= f;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) acc[g] *= f;
+        return ref;
+    };
+    auto take = [&](const f32x4 (&x)[4], f32x2 ml, float ref) {
         const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
         sum = fmaf(ml[1], f, sum);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4 x = *(const f32x4*)(one + ((4 * nb + g) * 64 * NW + col) * 4);
+        for (int g = 0; g < 4; ++g)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) acc[g][k] = fmaf(x[k], f, acc[g][k]);
+            for (int k = 0; k < 4; ++k) acc[g][k] = fmaf(x[g][k], f, acc[g][k]);
+    };
+    for (int from = team; from < e.pieces; from += TEAMS * AT_ONCE) {
+        f32x4 x[AT_ONCE][4];
+        f32x2 ml[AT_ONCE];
+#pragma unroll
+        for (int p = 0; p < AT_ONCE; ++p) {
+            const float* one = rec + (long long)min(from + TEAMS * p, e.pieces - 1) * RECORD_FLOATS;
+            ml[p] = *(const f32x2*)(one + 64 * 64 * NW + 2 * col);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) x[p][g] = *(const f32x4*)(one + ((4 * nb + g) * 64 * NW + col) * 4);
         }
+        float most = top;
+#pragma unroll
+        for (int p = 0; p < AT_ONCE; ++p)
+            if (from + TEAMS * p < e.pieces) most = fmaxf(most, ml[p][0]);
+        const float ref = raise(most);
+#pragma unroll
+        for (int p = 0; p < AT_ONCE; ++p)
+            if (from + TEAMS * p < e.pieces) take(x[p], ml[p], ref);
     }
-    if (row >= e.n_rows) return;
+    if (team > 0) {
+        part_ml[team][lane] = f32x2{top, sum};
+#pragma unroll
+        for (int g = 0; g < 4; ++g) part[team][g][lane] = acc[g];
+    }
+    __syncthreads();
+    if (team > 0 || row >= e.n_rows) return;
+    float most = top;
+#pragma unroll
+    for (int w = 1; w < TEAMS; ++w) most = fmaxf(most, part_ml[w][lane][0]);
+    const float ref = raise(most);
+#pragma unroll
+    for (int w = 1; w < TEAMS; ++w) {
+        const f32x4 x[4] = {part[w][0][lane], part[w][1][lane], part[w][2][lane], part[w][3][lane]};
+        take(x, part_ml[w][lane], ref);
+    }
     const int t = L.by_G.quotient(row);
     const long long place = (long long)(e.first_row + t) * b.num_q_heads + u.kvh * L.G + row - t * L.G;
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
         bf16x4 w;
 #pragma unroll
         for (int k = 0; k < 4; ++k) w[k] = (__bf16)(acc[g][k] * inv);
         *(bf16x4*)((__bf16*)a.out + place * HEAD_DIM + 32 * nb + 8 * g + 4 * (lane >> 5)) = w;
     }
-    if (a.lse != nullptr && threadIdx.x < 32) a.lse[place] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
+    if (a.lse != nullptr && nb == 0 && lane < 32) a.lse[place] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
 }
 
 Layout layout_of(const BatchView& b)
@@ -663,8 +714,8 @@ hipError_t launch_attn_fp8_tiles(const AttnFp8Args& a, bool causal, hipStream_t 
     else hipLaunchKernelGGL(attn_fp8_tiles_kernel<false>, grid, block, 0, stream, a, L);
     if (L.cut) {
         const int slots = L.units_max < PLACES / 2 ? L.units_max : PLACES / 2;
-        if (causal) hipLaunchKernelGGL(attn_fp8_merge_tiles_kernel<true>, dim3(slots * NW), dim3(256), 0, stream, a, L);
-        else hipLaunchKernelGGL(attn_fp8_merge_tiles_kernel<false>, dim3(slots * NW), dim3(256), 0, stream, a, L);
+        if (causal) hipLaunchKernelGGL(attn_fp8_merge_tiles_kernel<true>, dim3(slots * NW * 4), dim3(256), 0, stream, a, L);
+        else hipLaunchKernelGGL(attn_fp8_merge_tiles_kernel<false>, dim3(slots * NW * 4), dim3(256), 0, stream, a, L);
     }
     return hipGetLastError();
 }
