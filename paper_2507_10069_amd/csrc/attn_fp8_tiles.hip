@@ -184,28 +184,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     const int wave_clear = CAUSAL ? (e.P + L.by_G.quotient(min(wrow0, e.n_rows - 1)) + 1) / BC : e.P / BC;    // tiles that all rows of the wave see whole,
     const int unit_clear = CAUSAL ? (e.P + L.by_G.quotient(e.row0) + 1) / BC : e.P / BC;                      // and of the unit
 
-    // q, 64 channels a lane: 64 s + 32 h32 + 0 .. 31
-    i32x8 q_high[2], q_low[2];
-    int q_scale_high, q_scale_low;
-    {
-        const __bf16* qp = (const __bf16*)a.q + ((long long)(e.first_row + tok) * b.num_q_heads + u.kvh * L.G + row - tok * L.G) * HEAD_DIM + 32 * h32;
-        uint32_t pairs[32];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint4 x = *(const uint4*)(qp + 64 * (i >> 2) + 8 * (i & 3));
-            pairs[4 * i] = x.x; pairs[4 * i + 1] = x.y; pairs[4 * i + 2] = x.z; pairs[4 * i + 3] = x.w;
-        }
-        const uint32_t most = __float_as_uint(max32(__uint_as_float(most_of(pairs))));
-        q_scale_high = q_scale_byte(most);
-        q_scale_low = q_scale_high == 0xff ? 0xff : q_scale_high + LOW_PART_SCALE;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) {
-            const QCodes c = split4(pairs[2 * w], pairs[2 * w + 1], q_scale_high);
-            q_high[w >> 3][w & 7] = (int)c.high;
-            q_low[w >> 3][w & 7] = (int)c.low;
-        }
-    }
-
     // ---- fetches.  Wave w brings rows 8 w .. 8 w + 7 of a tile, of 16-key block 4 tile + w / 2 (1 KB of K and of V), and that block's
     //      16 scale bytes of K (even waves) or V (odd).
     const int32_t* __restrict__ pt = b.page_table + (long long)u.req * b.max_pages;
@@ -222,6 +200,30 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
         const int page = min(max(pt[blk >> b.page_shift], 0), b.num_pages - 1);
         block_ids = ((page * b.num_kv_heads + u.kvh) << b.page_shift) + (blk & ((1 << b.page_shift) - 1));
         ids_from = from;
+    };
+    if (n_tiles > 0) ask_blocks(t_begin);
+    // q's rows travel with the block ids; 64 channels a lane: 64 s + 32 h32 + 0 .. 31
+    uint32_t pairs[32];
+    {
+        const __bf16* qp = (const __bf16*)a.q + ((long long)(e.first_row + tok) * b.num_q_heads + u.kvh * L.G + row - tok * L.G) * HEAD_DIM + 32 * h32;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint4 x = *(const uint4*)(qp + 64 * (i >> 2) + 8 * (i & 3));
+            pairs[4 * i] = x.x; pairs[4 * i + 1] = x.y; pairs[4 * i + 2] = x.z; pairs[4 * i + 3] = x.w;
+        }
+    }
+    i32x8 q_high[2], q_low[2];
+    int q_scale_high = 0, q_scale_low = 0;
+    auto split_q = [&]() {
+        const uint32_t most = __float_as_uint(max32(__uint_as_float(most_of(pairs))));
+        q_scale_high = q_scale_byte(most);
+        q_scale_low = q_scale_high == 0xff ? 0xff : q_scale_high + LOW_PART_SCALE;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            const QCodes c = split4(pairs[2 * w], pairs[2 * w + 1], q_scale_high);
+            q_high[w >> 3][w & 7] = (int)c.high;
+            q_low[w >> 3][w & 7] = (int)c.low;
+        }
     };
     auto block_of = [&](int t) { return (long long)__builtin_amdgcn_readlane(block_ids, t - ids_from); };
     auto fetch_k = [&](int t, int slot) { lds_dma16(a.pools.k + block_of(t) * 2048, k_src, smem_base + K_AT + slot * K_TILE + wave * 1024); };
@@ -386,7 +388,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     };
 
     if (n_tiles > 0) {
-        ask_blocks(t_begin);
+        // (q is waited for here, before the fetches: behind them it would be waited for with them)
+        __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) asm volatile("" : "+v"(pairs[i]));
         fetch_k(t_begin, 0);
         fetch_v(t_begin, 0);
         fetch_scales(t_begin, 0);
@@ -397,6 +402,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
             fetch_k(t_begin + 2, 2);
             fetch_scales(t_begin + 2, 2);
         }
+        if (active) split_q();
         __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0)
         __syncthreads();
         read_raw(0, 0);
