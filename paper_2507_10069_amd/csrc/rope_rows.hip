@@ -14,12 +14,15 @@ namespace {
 using namespace fp8;
 
 constexpr int WAVES = 4;
+constexpr int MANY_TOKENS = 8192;                        // one for each wave that the chip holds
+constexpr int MOST_SPLIT = 4096;                         // waves: half of what the chip holds at once
 
-template <typename T> struct Row8;                       // eight neighbouring channels in memory and in 32 bits
+template <typename T> struct Row8;                       // eight neighbouring channels: as they lie in memory, and in 32 bits
 template <> struct Row8<__bf16> {
-    static __device__ void load(const __bf16* p, float (&x)[8])
+    typedef bf16x8 Raw;
+    static __device__ Raw load(const __bf16* p) { return *(const bf16x8*)p; }
+    static __device__ void widen(const Raw& v, float (&x)[8])
     {
-        const bf16x8 v = *(const bf16x8*)p;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
     }
@@ -33,11 +36,12 @@ template <> struct Row8<__bf16> {
     static __device__ float rounded(float x) { return (float)(__bf16)x; }
 };
 template <> struct Row8<float> {
-    static __device__ void load(const float* p, float (&x)[8])
+    struct Raw { float4 a, b; };
+    static __device__ Raw load(const float* p) { return {*(const float4*)p, *(const float4*)(p + 4)}; }
+    static __device__ void widen(const Raw& v, float (&x)[8])
     {
-        const float4 a = *(const float4*)p, c = *(const float4*)(p + 4);
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = c.x; x[5] = c.y; x[6] = c.z; x[7] = c.w;
+        x[0] = v.a.x; x[1] = v.a.y; x[2] = v.a.z; x[3] = v.a.w;
+        x[4] = v.b.x; x[5] = v.b.y; x[6] = v.b.z; x[7] = v.b.w;
     }
     static __device__ void store(float* p, const float (&x)[8])
     {
@@ -58,6 +62,10 @@ __device__ inline float2 turn_of(const RopeView& r, int i, long long position)
     return make_float2(c * r.factor, s * r.sine_factor);
 }
 
+// A pair's two values.  What is fused is written out, so that the kernels with and without the cache round alike.
+__device__ inline float turned_a(float a, float b, float2 cs) { return fmaf(a, cs.x, -(b * cs.y)); }
+__device__ inline float turned_b(float a, float b, float2 cs) { return fmaf(b, cs.x, a * cs.y); }
+
 template <int LANES>                                     // largest of the 4 or 8 lanes that hold a row
 __device__ inline uint32_t row_most(uint32_t x)
 {
@@ -68,7 +76,7 @@ __device__ inline uint32_t row_most(uint32_t x)
 }
 
 // rows of a token: K heads, then (QUANT) V heads, then q heads
-template <typename T, int D, bool QUANT>
+template <typename T, int D, bool QUANT, bool ROPE>
 __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, RopeView rope, NewRows rows, Fp8Pools pools, int splits)
 {
     constexpr int UNITS = D / 16, ROWS = 64 / UNITS;
@@ -78,15 +86,46 @@ __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, Rope
     const int t = (int)(item / splits), part = (int)(item - (long long)t * splits);
     if (t >= b.total_new_tokens) return;
 
+    const int n_k = rows.k != nullptr ? b.num_kv_heads : 0, n_v = QUANT ? b.num_kv_heads : 0, n_q = rows.q != nullptr ? b.num_q_heads : 0;
+    const int n_rows = n_k + n_v + n_q, u = lane % UNITS;
+    const bool unit_turns = ROPE && u < rope.rotary_dim / 16;
+    // a pass: 16 channels of one of the ROWS rows from `base` on, in two eights at a0 and a1
+    struct Place {
+        int head, a0, a1;
+        bool valid, is_k, is_v, turned;
+    };
+    auto place_in = [&](int base) -> Place {
+        Place p;
+        const int row = base + lane / UNITS;
+        p.valid = row < n_rows;
+        p.is_k = row < n_k;
+        p.is_v = !p.is_k && row < n_k + n_v;
+        p.head = p.is_k ? row : p.is_v ? row - n_k : row - n_k - n_v;
+        p.turned = unit_turns && !p.is_v;
+        const bool apart = p.turned && !rope.interleaved;
+        p.a0 = apart ? 8 * u : 16 * u;
+        p.a1 = apart ? rope.rotary_dim / 2 + 8 * u : 16 * u + 8;
+        return p;
+    };
+    typename Row8<T>::Raw raw0 = {}, raw1 = {};
+    auto ask = [&](const Place& p) {
+        if (p.valid) {
+            const T* src = (p.is_k ? (const T*)rows.k + t * rows.k_stride : p.is_v ? (const T*)rows.v + t * rows.v_stride : (const T*)rows.q + t * rows.q_stride) + p.head * D;
+            raw0 = Row8<T>::load(src + p.a0);
+            raw1 = Row8<T>::load(src + p.a1);
+        }
+    };
+    ask(place_in(part * ROWS));                          // travels while it is worked out where it goes and how far it turns
+
     TokenPlace place = {0, -1};
     long long row0 = -1;
-    const bool from_batch = rope.rotary_dim > 0 && rope.num_axes == 0;
+    const bool from_batch = ROPE && rope.num_axes == 0;
     if (QUANT || from_batch) {
         place = place_of_token(b, t);
         if (place.slot < 0) return;                      // a row of no request stays as it was
     }
     if (QUANT) row0 = pool_row(b, place);
-    if (lane < rope.rotary_dim / 2) {
+    if (ROPE && lane < rope.rotary_dim / 2) {
         long long position = place.slot;
         if (!from_batch) {
             const int axis = (lane >= rope.ends[0] ? 1 : 0) + (lane >= rope.ends[1] ? 1 : 0) + (lane >= rope.ends[2] ? 1 : 0);
@@ -97,43 +136,35 @@ __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, Rope
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 
-    const int n_k = rows.k != nullptr ? b.num_kv_heads : 0, n_v = QUANT ? b.num_kv_heads : 0, n_q = rows.q != nullptr ? b.num_q_heads : 0;
-    const int n_rows = n_k + n_v + n_q, u = lane % UNITS;
     float2 cs[8] = {};
-    const bool unit_turns = u < rope.rotary_dim / 16;
     if (unit_turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) cs[i] = turns[wave][8 * u + i];
     }
     for (int base = part * ROWS; base < n_rows; base += splits * ROWS) {
-        const int row = base + lane / UNITS;
-        const bool valid = row < n_rows, is_k = row < n_k, is_v = !is_k && row < n_k + n_v;
-        const int head = is_k ? row : is_v ? row - n_k : row - n_k - n_v;
-        const bool turned = unit_turns && !is_v;
-        const bool apart = turned && !rope.interleaved;
-        const int a0 = apart ? 8 * u : 16 * u, a1 = apart ? rope.rotary_dim / 2 + 8 * u : 16 * u + 8;
-        float x[8] = {}, y[8] = {};
-        if (valid) {
-            const T* src = (is_k ? (const T*)rows.k + t * rows.k_stride : is_v ? (const T*)rows.v + t * rows.v_stride : (const T*)rows.q + t * rows.q_stride) + head * D;
-            Row8<T>::load(src + a0, x);
-            Row8<T>::load(src + a1, y);
-        }
+        const Place p = place_in(base);
+        const bool valid = p.valid, is_k = p.is_k, is_v = p.is_v, turned = p.turned;
+        const int head = p.head, a0 = p.a0, a1 = p.a1;
+        if (base != part * ROWS) ask(p);
+        float x[8], y[8];
+        Row8<T>::widen(raw0, x);
+        Row8<T>::widen(raw1, y);
         if (turned) {
             if (rope.interleaved) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float a = x[2 * i], c = x[2 * i + 1], d = y[2 * i], e = y[2 * i + 1];
-                    x[2 * i] = a * cs[i].x - c * cs[i].y;
-                    x[2 * i + 1] = c * cs[i].x + a * cs[i].y;
-                    y[2 * i] = d * cs[4 + i].x - e * cs[4 + i].y;
-                    y[2 * i + 1] = e * cs[4 + i].x + d * cs[4 + i].y;
+                    x[2 * i] = turned_a(a, c, cs[i]);
+                    x[2 * i + 1] = turned_b(a, c, cs[i]);
+                    y[2 * i] = turned_a(d, e, cs[4 + i]);
+                    y[2 * i + 1] = turned_b(d, e, cs[4 + i]);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float a = x[i], c = y[i];
-                    x[i] = a * cs[i].x - c * cs[i].y;
-                    y[i] = c * cs[i].x + a * cs[i].y;
+                    x[i] = turned_a(a, c, cs[i]);
+                    y[i] = turned_b(a, c, cs[i]);
                 }
             }
         }
@@ -170,10 +201,10 @@ __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, Rope
 }
 
 // 16 codes to the batch's dtype, exact
-__device__ inline void widen16(const uint4 c, int byte, __bf16* dst)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ inline void widen16(const u32x4 w, int byte, __bf16* dst)
 {
     const float scale = up_scale(byte);
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
     bf16x2 v[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -185,10 +216,9 @@ __device__ inline void widen16(const uint4 c, int byte, __bf16* dst)
         *(uint4*)(dst + 8 * i) = make_uint4(__builtin_bit_cast(uint32_t, v[4 * i]), __builtin_bit_cast(uint32_t, v[4 * i + 1]),
                                             __builtin_bit_cast(uint32_t, v[4 * i + 2]), __builtin_bit_cast(uint32_t, v[4 * i + 3]));
 }
-__device__ inline void widen16(const uint4 c, int byte, float* dst)
+__device__ inline void widen16(const u32x4 w, int byte, float* dst)
 {
     const float scale = up_scale(byte);
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i], scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i], scale, true);
@@ -196,41 +226,59 @@ __device__ inline void widen16(const uint4 c, int byte, float* dst)
     }
 }
 
-template <typename T, int D>
+// TOKENS: slots of a wave, whose rows travel together
+template <typename T, int D, int TOKENS>
 __global__ __launch_bounds__(64 * WAVES) void kv_gather_fp8_kernel(BatchView b, Fp8Pools pools, T* __restrict__ k_out, T* __restrict__ v_out)
 {
     constexpr int UNITS = D / 16, ROWS = 64 / UNITS;
-    const int t = blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (t >= b.total_new_tokens) return;
-    const long long row0 = pool_row(b, place_of_token(b, t));
-    if (row0 < 0) return;
+    const int t0 = (blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * TOKENS, lane = threadIdx.x & 63;
+    if (t0 >= b.total_new_tokens) return;
+    long long row0[TOKENS];
+#pragma unroll
+    for (int i = 0; i < TOKENS; ++i) row0[i] = t0 + i < b.total_new_tokens ? pool_row(b, place_of_token(b, t0 + i)) : -1;
     const int u = lane % UNITS;
     for (int row = lane / UNITS; row < 2 * b.num_kv_heads; row += ROWS) {
         const bool is_k = row < b.num_kv_heads;
         const int head = is_k ? row : row - b.num_kv_heads;
-        const long long at = row0 + (long long)head * b.page_size;
-        const uint4 codes = *(const uint4*)((is_k ? pools.k : pools.v) + at * D + 16 * u);
-        const int byte = (is_k ? pools.k_scale : pools.v_scale)[at];
-        widen16(codes, byte, (is_k ? k_out : v_out) + ((long long)t * b.num_kv_heads + head) * D + 16 * u);
+        u32x4 codes[TOKENS];
+        int byte[TOKENS];
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) {
+            const long long at = max(row0[i], 0ll) + (long long)head * b.page_size;
+            const u32x4* from = (const u32x4*)((is_k ? pools.k : pools.v) + at * D + 16 * u);
+            if constexpr (TOKENS > 1) codes[i] = __builtin_nontemporal_load(from);       // read once: other lines stay in the caches
+            else codes[i] = *from;
+            byte[i] = (is_k ? pools.k_scale : pools.v_scale)[at];
+        }
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i)
+            if (row0[i] >= 0) widen16(codes[i], byte[i], (is_k ? k_out : v_out) + ((long long)(t0 + i) * b.num_kv_heads + head) * D + 16 * u);
     }
 }
 
 template <typename T, int D>
 hipError_t launch_rows(const BatchView& b, const RopeView& rope, const NewRows& rows, const Fp8Pools* pools, hipStream_t stream)
 {
-    constexpr int splits = 1;
+    // Few tokens: a wave for each pass over a token's rows, which takes its turns by itself; many: a wave for a token.
+    const int heads = (rows.k != nullptr ? b.num_kv_heads : 0) + (pools != nullptr ? b.num_kv_heads : 0) + (rows.q != nullptr ? b.num_q_heads : 0);
+    const int passes = (heads * (D / 16) + 63) / 64;
+    const int splits = (long long)b.total_new_tokens * passes <= MOST_SPLIT ? passes : 1;
     const long long items = (long long)b.total_new_tokens * splits;
     const dim3 grid((unsigned)((items + WAVES - 1) / WAVES)), block(64 * WAVES);
-    if (pools != nullptr) hipLaunchKernelGGL((rope_rows_kernel<T, D, true>), grid, block, 0, stream, b, rope, rows, *pools, splits);
-    else hipLaunchKernelGGL((rope_rows_kernel<T, D, false>), grid, block, 0, stream, b, rope, rows, Fp8Pools{}, splits);
+    if (pools == nullptr) hipLaunchKernelGGL((rope_rows_kernel<T, D, false, true>), grid, block, 0, stream, b, rope, rows, Fp8Pools{}, splits);
+    else if (rope.rotary_dim > 0) hipLaunchKernelGGL((rope_rows_kernel<T, D, true, true>), grid, block, 0, stream, b, rope, rows, *pools, splits);
+    else hipLaunchKernelGGL((rope_rows_kernel<T, D, true, false>), grid, block, 0, stream, b, rope, rows, *pools, splits);
     return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch_gather(const BatchView& b, const Fp8Pools& pools, void* k_out, void* v_out, hipStream_t stream)
 {
-    hipLaunchKernelGGL((kv_gather_fp8_kernel<T, D>), dim3((unsigned)(((long long)b.total_new_tokens + WAVES - 1) / WAVES)), dim3(64 * WAVES), 0, stream, b, pools,
-                       (T*)k_out, (T*)v_out);
+    auto grid = [&](int tokens) { return dim3((unsigned)(((long long)b.total_new_tokens + WAVES * tokens - 1) / (WAVES * tokens))); };
+    if (b.total_new_tokens < MANY_TOKENS)
+        hipLaunchKernelGGL((kv_gather_fp8_kernel<T, D, 1>), grid(1), dim3(64 * WAVES), 0, stream, b, pools, (T*)k_out, (T*)v_out);
+    else
+        hipLaunchKernelGGL((kv_gather_fp8_kernel<T, D, 2>), grid(2), dim3(64 * WAVES), 0, stream, b, pools, (T*)k_out, (T*)v_out);
     return hipGetLastError();
 }
 
