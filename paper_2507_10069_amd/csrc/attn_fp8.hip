@@ -36,6 +36,7 @@ constexpr int ROWS = 16;
 constexpr int OUT_STRIDE = D + 8;                        // bf16 values between output rows in LDS
 constexpr int LEAST_TILES = WAVES;                       // of a part: one for each wave
 constexpr int WORKGROUPS = 512;                          // two on each compute unit
+constexpr int ALONE = 256;                               // so many parts have a compute unit to themselves
 constexpr int MANY_RECORDS = 16;                         // of a pair
 constexpr int STREAM_TILES = 12000;                      // 96 MiB of codes: from here on a call does not fit the last-level cache next to others
 constexpr int MOST_COMPARED = 512;                       // requests among which shared pages are looked for
@@ -134,11 +135,16 @@ struct Line {
     }
 };
 
-__device__ inline int part_tiles(const RowsLayout& L, int all) { return max(LEAST_TILES, L.by_workgroups.quotient(all - 1) + 1); }
-// x / d for d > 0, 0 <= x < 2^31 and a quotient below 2^22: by the reciprocal, which is off by less than one whole
+// Tiles of a part: equal shares for all workgroups, but not too short ones.  (Parts of four tiles where each has a compute unit to itself, of eight
+// at least else: one context of 1500 tokens 11.4 us with 4 and 12.4 with 8, 8 of 2000 15.0 and 13.6, one of 16000 17.6 and 15.0.)
+__device__ inline int part_tiles(const RowsLayout& L, int all)
+{
+    return max(all <= LEAST_TILES * ALONE ? LEAST_TILES : 2 * LEAST_TILES, L.by_workgroups.quotient(all - 1) + 1);
+}
+// x / d, the same in all lanes, for d > 0, 0 <= x < 2^31 and a quotient below 2^20: by the reciprocal, which is off by less than one whole
 __device__ inline int small_quotient(int x, int d)
 {
-    const int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));
+    const int q = __builtin_amdgcn_readfirstlane((int)((float)x * __builtin_amdgcn_rcpf((float)d)));
     const int rest = x - q * d;
     return rest < 0 ? q - 1 : rest >= d ? q + 1 : q;
 }
