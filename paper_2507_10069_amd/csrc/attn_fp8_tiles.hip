@@ -16,6 +16,7 @@
 // tile's weights sum to more than 2^20: any reference gives the same result, and the sum, which is taken before
 // the weights are used, tells in time.  So the loop takes no maxima.  Row sums are of the weights before they are
 // rounded (of the rounded ones they would be off by up to 2^-9 where few keys count).
+#include <algorithm>
 #include <type_traits>
 
 #include "attn_bf16_common.h"
@@ -47,6 +48,9 @@ static_assert(NW * 32 * OUT_STRIDE <= FLAG_AT, "output rows are staged over the 
 constexpr int FETCHES = 3;                               // of a wave for a tile: K, V, scales
 
 constexpr int RECORD_FLOATS = (64 + 2) * 64 * NW;        // of a piece: 64 accumulators of each thread in groups of four, then m and l
+constexpr int TEAMS = 4;                                 // waves of the merge,
+constexpr int MERGERS = 1024;                            // and its workgroups at most
+constexpr int FEW_UNITS = 8;                             // units that give the merge too little to do with 32 channels at a time
 
 // how the units of a batch are laid out over the grid
 struct Layout {
@@ -65,15 +69,15 @@ struct Unit {
 // Units in order: requests, in a request row tiles from the last (which sees the most keys) to the first, of a row tile the
 // KV heads; neighbouring workgroups run on neighbouring XCDs, so an XCD has the same few heads throughout and their K and V
 // go through its L2.  Whole rounds of PLACES units first; the rest, if few, are cut in as many pieces as fill the chip.
-// merge_slot >= 0: the unit in that slot instead.
-__device__ inline Unit plan_unit(const BatchView& b, const Layout& L, int wg, int merge_slot)
-{
-    Unit u;
-    u.req = -1;
-    const int lane = threadIdx.x & 63;
-    int total = 0;
-    int new_lane = 0, prefix_lane = 0, cu_lane = 0, incl = 0;
-    auto look = [&](int first) {                         // lane's request first + lane
+struct Plan {
+    const BatchView& b;
+    const Layout& L;
+    int lane, new_lane, prefix_lane, cu_lane, incl;      // of the 64 requests looked at
+    int total;                                           // row tiles of the batch
+    int units, full, rest, parts;                        // full: units in whole rounds; rest: those behind, in so many pieces each
+
+    __device__ int look(int first)                       // lane's request first + lane; returns the row tiles of the 64
+    {
         const int r = min(first + lane, b.num_reqs - 1);
         new_lane = b.new_lens[r];
         prefix_lane = b.prefix_lens[r];
@@ -81,48 +85,51 @@ __device__ inline Unit plan_unit(const BatchView& b, const Layout& L, int wg, in
         const int n = first + lane < b.num_reqs ? clamp_new_len(b, new_lane, false) : 0;
         incl = scan64((n * L.G + BR - 1) / BR);
         return __builtin_amdgcn_readlane(incl, 63);
-    };
-    for (int first = 0; first < b.num_reqs; first += 64) total += look(first);
-    const int units = total * b.num_kv_heads;
-    const int full = L.cut ? units / PLACES * PLACES : units, rest = units - full;
-    const int stride = rest;
-    u.parts = stride == 0 ? 1 : min(PLACES / stride, MAX_PARTS);
-    u.part = 0;
-    u.slot = 0;
-    int ordinal = wg;
-    if (merge_slot >= 0) {
-        if (merge_slot >= rest || u.parts < 2) return u;
-        u.slot = merge_slot;
-        ordinal = full + merge_slot;
-    } else if (wg >= full) {
-        if (stride == 0) return u;
-        u.part = (wg - full) / stride;
-        u.slot = wg - full - u.part * stride;
-        if (u.slot >= rest || u.part >= u.parts) return u;
-        ordinal = full + u.slot;
-    } else {
-        u.parts = 1;
     }
-    if (ordinal >= units) return u;
-    const int nth = L.by_kv_heads.quotient(ordinal);     // row tile of the batch
-    u.kvh = ordinal - nth * b.num_kv_heads;
-    int before = 0;
-    for (int first = 0; first < b.num_reqs; first += 64) {
-        const int sum = b.num_reqs <= 64 ? total : look(first);
-        if (nth < before + sum) {
-            const unsigned long long hit = __builtin_amdgcn_ballot_w64(incl > nth - before);
-            const int at = __builtin_ctzll(hit);
-            u.req = first + at;
-            u.tile = __builtin_amdgcn_readlane(incl, at) - 1 - (nth - before);
-            u.new_len = __builtin_amdgcn_readlane(new_lane, at);
-            u.prefix_len = __builtin_amdgcn_readlane(prefix_lane, at);
-            u.cu_new = __builtin_amdgcn_readlane(cu_lane, at);
-            return u;
+    __device__ Plan(const BatchView& batch, const Layout& layout) : b(batch), L(layout), lane(threadIdx.x & 63), total(0)
+    {
+        for (int first = 0; first < b.num_reqs; first += 64) total += look(first);
+        units = total * b.num_kv_heads;
+        full = L.cut ? units / PLACES * PLACES : units;
+        rest = units - full;
+        parts = rest == 0 ? 1 : min(PLACES / rest, MAX_PARTS);
+    }
+    __device__ Unit unit(int ordinal)
+    {
+        Unit u;
+        u.req = -1;
+        u.parts = ordinal < full ? 1 : parts;
+        u.part = 0;
+        u.slot = ordinal - full;
+        if (ordinal >= units) return u;
+        const int nth = L.by_kv_heads.quotient(ordinal); // row tile of the batch
+        u.kvh = ordinal - nth * b.num_kv_heads;
+        int before = 0;
+        for (int first = 0; first < b.num_reqs; first += 64) {
+            const int sum = b.num_reqs <= 64 ? total : look(first);
+            if (nth < before + sum) {
+                const unsigned long long hit = __builtin_amdgcn_ballot_w64(incl > nth - before);
+                const int at = __builtin_ctzll(hit);
+                u.req = first + at;
+                u.tile = __builtin_amdgcn_readlane(incl, at) - 1 - (nth - before);
+                u.new_len = __builtin_amdgcn_readlane(new_lane, at);
+                u.prefix_len = __builtin_amdgcn_readlane(prefix_lane, at);
+                u.cu_new = __builtin_amdgcn_readlane(cu_lane, at);
+                return u;
+            }
+            before += sum;
         }
-        before += sum;
+        return u;
     }
-    return u;
-}
+    __device__ Unit of_workgroup(int wg)
+    {
+        if (wg < full || rest == 0) return unit(wg);
+        const int part = (wg - full) / rest;
+        Unit u = unit(part < parts ? wg - part * rest : units);
+        u.part = part;
+        return u;
+    }
+};
 
 // a unit's rows and keys
 struct Extent {
@@ -169,7 +176,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
 {
     __shared__ __attribute__((aligned(1024))) unsigned char smem[SMEM];
     const BatchView& b = a.b;
-    const Unit u = plan_unit(b, L, blockIdx.x, -1);
+    const Unit u = Plan(b, L).of_workgroup(blockIdx.x);
     if (u.req < 0) return;
     const Extent e = extent_of<CAUSAL>(b, L, u, L.units_max <= PLACES);
     if (e.row0 >= e.n_rows || u.part >= e.pieces) return;
@@ -603,88 +610,98 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     }
 }
 
-// The pieces of the units that were cut: a workgroup per unit, wave of rows and block of 32 channels; its four waves take the
-// pieces in turn, four at a time.
-template <bool CAUSAL>
-__global__ __launch_bounds__(256) void attn_fp8_merge_tiles_kernel(AttnFp8Args a, Layout L)
+// The pieces of the units that were cut.  A piece of work is 32 rows of a unit (a wave's) and 4 GROUPS channels of each half of
+// the lanes; a workgroup's waves take the unit's records in turn, AT_ONCE of them on the way, and are added up through LDS.
+template <bool CAUSAL, int GROUPS, int AT_ONCE>
+__global__ __launch_bounds__(64 * TEAMS) void attn_fp8_merge_tiles_kernel(AttnFp8Args a, Layout L)
 {
-    constexpr int TEAMS = 4, AT_ONCE = 4;
+    constexpr int BLOCKS = 16 / GROUPS;
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     const BatchView& b = a.b;
-    const Unit u = plan_unit(b, L, 0, blockIdx.x / (4 * NW));
-    if (u.req < 0) return;
-    const Extent e = extent_of<CAUSAL>(b, L, u, L.units_max <= PLACES);
-    const int wave = (blockIdx.x >> 2) % NW, nb = blockIdx.x & 3, lane = threadIdx.x & 63, team = threadIdx.x >> 6;
-    const int row = e.row0 + 32 * wave + (lane & 31);
-    if (e.pieces < 2 || e.row0 + 32 * wave >= e.n_rows) return;
-    __shared__ f32x4 part[TEAMS][4][64];
+    __shared__ f32x4 part[TEAMS][GROUPS][64];
     __shared__ f32x2 part_ml[TEAMS][64];
-    const float* rec = (const float*)a.workspace + (long long)(u.slot * u.parts) * RECORD_FLOATS;
-    const int col = 64 * wave + lane;
-    f32x4 acc[4] = {};
-    float top = -INFINITY, sum = 0.f;
-    auto raise = [&](float to) -> float {                    // what there is in terms of a larger reference
-        const float ref = to == -INFINITY ? 0.f : to, f = __builtin_amdgcn_exp2f(top - ref);
-        top = to;
-        sum *= f;
+    const int lane = threadIdx.x & 63, team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Plan plan(b, L);
+    if (plan.parts < 2) return;
+    for (int work = blockIdx.x; work < plan.rest * (NW * BLOCKS); work += gridDim.x) {
+        const Unit u = plan.unit(plan.full + work / (NW * BLOCKS));
+        const Extent e = extent_of<CAUSAL>(b, L, u, L.units_max <= PLACES);
+        const int wave = work / BLOCKS % NW, block = work % BLOCKS;
+        const int row = e.row0 + 32 * wave + (lane & 31);
+        if (e.pieces < 2 || e.row0 + 32 * wave >= e.n_rows) continue;
+        const float* rec = (const float*)a.workspace + (long long)(u.slot * u.parts) * RECORD_FLOATS;
+        const int col = 64 * wave + lane;
+        f32x4 acc[GROUPS] = {};
+        float top = -INFINITY, sum = 0.f;
+        auto raise = [&](float to) -> float {                // what there is in terms of a larger reference
+            const float ref = to == -INFINITY ? 0.f : to, f = __builtin_amdgcn_exp2f(top - ref);
+            top = to;
+            sum *= f;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) acc[g] *= f;
-        return ref;
-    };
-    auto take = [&](const f32x4 (&x)[4], f32x2 ml, float ref) {
-        const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
-        sum = fmaf(ml[1], f, sum);
+            for (int g = 0; g < GROUPS; ++g) acc[g] *= f;
+            return ref;
+        };
+        auto take = [&](const f32x4 (&x)[GROUPS], f32x2 ml, float ref) {
+            const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
+            sum = fmaf(ml[1], f, sum);
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+            for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) acc[g][k] = fmaf(x[g][k], f, acc[g][k]);
-    };
-    for (int from = team; from < e.pieces; from += TEAMS * AT_ONCE) {
-        f32x4 x[AT_ONCE][4];
-        f32x2 ml[AT_ONCE];
+                for (int k = 0; k < 4; ++k) acc[g][k] = fmaf(x[g][k], f, acc[g][k]);
+        };
+        for (int from = team; from < e.pieces; from += TEAMS * AT_ONCE) {
+            f32x4 x[AT_ONCE][GROUPS];
+            f32x2 ml[AT_ONCE];
 #pragma unroll
-        for (int p = 0; p < AT_ONCE; ++p) {
-            const float* one = rec + (long long)min(from + TEAMS * p, e.pieces - 1) * RECORD_FLOATS;
-            ml[p] = *(const f32x2*)(one + 64 * 64 * NW + 2 * col);
+            for (int p = 0; p < AT_ONCE; ++p) {
+                if (p > 0 && from + TEAMS * p >= e.pieces) break;
+                const float* one = rec + (long long)(from + TEAMS * p) * RECORD_FLOATS;
+                ml[p] = *(const f32x2*)(one + 64 * 64 * NW + 2 * col);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) x[p][g] = *(const f32x4*)(one + ((4 * nb + g) * 64 * NW + col) * 4);
+                for (int g = 0; g < GROUPS; ++g) x[p][g] = *(const f32x4*)(one + ((GROUPS * block + g) * 64 * NW + col) * 4);
+            }
+            float most = top;
+#pragma unroll
+            for (int p = 0; p < AT_ONCE; ++p)
+                if (from + TEAMS * p < e.pieces) most = fmaxf(most, ml[p][0]);
+            const float ref = raise(most);
+#pragma unroll
+            for (int p = 0; p < AT_ONCE; ++p)
+                if (from + TEAMS * p < e.pieces) take(x[p], ml[p], ref);
         }
+        __syncthreads();                                     // the last piece of work's sums have been read
+        if (team > 0) {
+            part_ml[team][lane] = f32x2{top, sum};
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) part[team][g][lane] = acc[g];
+        }
+        __syncthreads();
+        if (team > 0) continue;
         float most = top;
 #pragma unroll
-        for (int p = 0; p < AT_ONCE; ++p)
-            if (from + TEAMS * p < e.pieces) most = fmaxf(most, ml[p][0]);
+        for (int w = 1; w < TEAMS; ++w) most = fmaxf(most, part_ml[w][lane][0]);
         const float ref = raise(most);
 #pragma unroll
-        for (int p = 0; p < AT_ONCE; ++p)
-            if (from + TEAMS * p < e.pieces) take(x[p], ml[p], ref);
+        for (int w = 1; w < TEAMS; ++w) {
+            f32x4 x[GROUPS];
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) x[g] = part[w][g][lane];
+            take(x, part_ml[w][lane], ref);
+        }
+        if (row < e.n_rows) {
+            const int t = L.by_G.quotient(row);
+            const long long place = (long long)(e.first_row + t) * b.num_q_heads + u.kvh * L.G + row - t * L.G;
+            const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                bf16x4 w;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = (__bf16)(acc[g][k] * inv);
+                *(bf16x4*)((__bf16*)a.out + place * HEAD_DIM + 8 * (GROUPS * block + g) + 4 * (lane >> 5)) = w;
+            }
+            if (a.lse != nullptr && block == 0 && lane < 32) a.lse[place] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
+        }
     }
-    if (team > 0) {
-        part_ml[team][lane] = f32x2{top, sum};
-#pragma unroll
-        for (int g = 0; g < 4; ++g) part[team][g][lane] = acc[g];
-    }
-    __syncthreads();
-    if (team > 0 || row >= e.n_rows) return;
-    float most = top;
-#pragma unroll
-    for (int w = 1; w < TEAMS; ++w) most = fmaxf(most, part_ml[w][lane][0]);
-    const float ref = raise(most);
-#pragma unroll
-    for (int w = 1; w < TEAMS; ++w) {
-        const f32x4 x[4] = {part[w][0][lane], part[w][1][lane], part[w][2][lane], part[w][3][lane]};
-        take(x, part_ml[w][lane], ref);
-    }
-    const int t = L.by_G.quotient(row);
-    const long long place = (long long)(e.first_row + t) * b.num_q_heads + u.kvh * L.G + row - t * L.G;
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        bf16x4 w;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = (__bf16)(acc[g][k] * inv);
-        *(bf16x4*)((__bf16*)a.out + place * HEAD_DIM + 32 * nb + 8 * g + 4 * (lane >> 5)) = w;
-    }
-    if (a.lse != nullptr && nb == 0 && lane < 32) a.lse[place] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
 }
 
 Layout layout_of(const BatchView& b)
@@ -705,6 +722,13 @@ Layout layout_of(const BatchView& b)
     return L;
 }
 
+template <bool CAUSAL, int GROUPS, int AT_ONCE>
+void merge(const AttnFp8Args& a, const Layout& L, hipStream_t stream)
+{
+    const int most = std::min(L.units_max, PLACES / 2) * (NW * 16 / GROUPS);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(attn_fp8_merge_tiles_kernel<CAUSAL, GROUPS, AT_ONCE>), dim3(std::min(most, MERGERS)), dim3(64 * TEAMS), 0, stream, a, L);
+}
+
 }  // namespace
 
 size_t attn_fp8_tiles_workspace_bytes(const BatchView& b)
@@ -719,9 +743,10 @@ hipError_t launch_attn_fp8_tiles(const AttnFp8Args& a, bool causal, hipStream_t 
     if (causal) hipLaunchKernelGGL(attn_fp8_tiles_kernel<true>, grid, block, 0, stream, a, L);
     else hipLaunchKernelGGL(attn_fp8_tiles_kernel<false>, grid, block, 0, stream, a, L);
     if (L.cut) {
-        const int slots = L.units_max < PLACES / 2 ? L.units_max : PLACES / 2;
-        if (causal) hipLaunchKernelGGL(attn_fp8_merge_tiles_kernel<true>, dim3(slots * NW * 4), dim3(256), 0, stream, a, L);
-        else hipLaunchKernelGGL(attn_fp8_merge_tiles_kernel<false>, dim3(slots * NW * 4), dim3(256), 0, stream, a, L);
+        // 32 channels at a time, or 16 with twice the records on the way where few units would leave compute units without work (8 tokens
+        // behind 16 k: 17.9 and 19.5 us; 8 images' chunks 65.2 and 64.6, 16 short ones 52.8 and 49.4)
+        if (L.units_max <= FEW_UNITS) causal ? merge<true, 2, 8>(a, L, stream) : merge<false, 2, 8>(a, L, stream);
+        else causal ? merge<true, 4, 4>(a, L, stream) : merge<false, 4, 4>(a, L, stream);
     }
     return hipGetLastError();
 }
