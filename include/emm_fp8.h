@@ -17,6 +17,9 @@
  * pools' are fixed.  Slots that hold no token may hold any bits.  emm_kv_pages_pack / emm_kv_pages_unpack move pages
  * of the code pools (page_bytes = num_kv_heads * page_size * head_dim) and, in a call of their own, of the scale pools
  * (num_kv_heads * page_size) as they are.
+ *
+ * Limits of these calls and of emm_rope (beyond them EMM_ERR_UNSUPPORTED): 2^25 tokens and 2^30 (token, head) rows in
+ * a batch, 4096 heads, 2^30 slots in a row of the page table; for the attention, 2^20 (request, KV head) pairs.
  */
 #ifndef EMM_FP8_H
 #define EMM_FP8_H
@@ -60,10 +63,10 @@ emm_status emm_kv_gather_fp8(const emm_batch *batch, const emm_fp8_cache *cache,
 /*
  * emm_prefill_attn, emm_cross_attn and emm_decode_attn over such a cache: the attention of the values that it stands
  * for, for any number of new tokens per request (emm_decode_attn_fp8: at most one, else EMM_ERR_INVALID_ARG).
- * EMM_BF16 with head_dim 128.  Arguments and results as there.  Codes meet q on the matrix pipe without loss (q
- * goes in as the sum of two 8-bit parts, which holds all of a bf16's significand); scores, softmax statistics and sums
- * are in 32 bits; softmax weights are rounded to bf16 for the value product.  A NaN in V reaches only rows that see
- * its slot.  Results are run-to-run bitwise deterministic.
+ * EMM_BF16 with head_dim 128.  Arguments and results as there.  Codes meet q on the matrix pipe as they are; q goes in
+ * as the sum of two 8-bit parts, which holds a bf16 whole down to 2^-13 of its row's largest value and smaller ones to
+ * within 2^-21 of that; scores, softmax statistics and sums are in 32 bits; softmax weights are rounded to bf16 for the
+ * value product.  A NaN in V reaches only rows that see its slot.  Results are run-to-run bitwise deterministic.
  *   workspace  device scratch of at least emm_attn_fp8_workspace_size bytes, 16-byte aligned (may be NULL if that is
  *              0), the same size for all three calls; contents need no initialisation and mean nothing afterwards.
  *              Calls that may overlap must not share one.

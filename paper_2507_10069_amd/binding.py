@@ -74,6 +74,7 @@ class emm_rope_params(ctypes.Structure):
     _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("inverse", ctypes.c_int32),
                 ("sections", ctypes.c_int32 * 4), ("factor", ctypes.c_float), ("reserved", ctypes.c_int32),
                 ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p)]
+    _tokens = None                                       # that positions has, where make_rope was given one
 
 
 class emm_rope_scaling(ctypes.Structure):
@@ -400,7 +401,13 @@ def make_rope(inv_freq, *, rotary_dim: int, layout="half", factor: float = 1.0, 
     rope = emm_rope_params(ROPE_LAYOUTS.get(layout, layout), rotary_dim, axes, int(inverse), (ctypes.c_int32 * 4)(*(parts + [0] * 4)[:4]), factor, 0,
                            _ptr(inv_freq), _ptr(positions))
     rope._keepalive = (inv_freq, positions)
+    rope._tokens = None if positions is None else positions.numel() // axes
     return rope
+
+
+def _check_positions(batch: emm_batch, rope: emm_rope_params) -> None:
+    if rope._tokens is not None and rope._tokens != batch.total_new_tokens:
+        raise ValueError("positions of %d tokens, a batch of %d" % (rope._tokens, batch.total_new_tokens))
 
 
 def emm_rope_inv_freq_host(rotary_dim: int, base: float, kind="plain", scale: float = 1.0, original_len: int = 0, slow: float = 1.0,
@@ -414,6 +421,7 @@ def emm_rope_inv_freq_host(rotary_dim: int, base: float, kind="plain", scale: fl
 
 
 def emm_rope(batch: emm_batch, rope: emm_rope_params, q, k, q_out, k_out, token_stride: int = 0, stream=None) -> None:
+    _check_positions(batch, rope)
     _check(load().emm_rope(ctypes.byref(batch), ctypes.byref(rope), _ptr(q), _ptr(k), token_stride, _ptr(q_out), _ptr(k_out), _stream(stream)),
            "emm_rope")
 
@@ -436,6 +444,7 @@ def emm_kv_scatter_fp8(batch: emm_batch, k_new, v_new, cache: emm_fp8_cache, tok
 
 def emm_rope_kv_scatter_fp8(batch: emm_batch, rope: emm_rope_params, q, k_new, v_new, q_out, cache: emm_fp8_cache, token_stride: int = 0,
                             stream=None) -> None:
+    _check_positions(batch, rope)
     _check(load().emm_rope_kv_scatter_fp8(ctypes.byref(batch), ctypes.byref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), token_stride, _ptr(q_out),
                                           ctypes.byref(cache), _stream(stream)), "emm_rope_kv_scatter_fp8")
 

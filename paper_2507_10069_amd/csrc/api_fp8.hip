@@ -16,7 +16,9 @@ using emm::api::view_of;
 
 namespace {
 
-// what the row kernels take: pages as everywhere, both dtypes, heads of 64 or 128
+constexpr int64_t MOST_TOKENS = int64_t(1) << 25, MOST_HEADS = 4096, MOST_ROWS = int64_t(1) << 30, MOST_SLOTS = int64_t(1) << 30, MOST_PAIRS = int64_t(1) << 20;
+
+// what the row kernels take: pages as everywhere, both dtypes, heads of 64 or 128, and numbers that their grids and indexes hold
 emm_status check_rows(const emm_batch* b)
 {
     const emm_status st = check_scalars(b);
@@ -24,6 +26,9 @@ emm_status check_rows(const emm_batch* b)
     if (b->page_size != 16 && b->page_size != 32 && b->page_size != 64 && b->page_size != 128 && b->page_size != 256)
         return EMM_ERR_UNSUPPORTED;
     if (b->head_dim != 64 && b->head_dim != 128) return EMM_ERR_UNSUPPORTED;
+    if (b->total_new_tokens > MOST_TOKENS || b->num_q_heads > MOST_HEADS || int64_t(b->total_new_tokens) * b->num_q_heads > MOST_ROWS ||
+        int64_t(b->max_pages_per_req) * b->page_size > MOST_SLOTS)
+        return EMM_ERR_UNSUPPORTED;
     return EMM_OK;
 }
 
@@ -240,7 +245,7 @@ emm_status emm_attn_fp8_workspace_size(const emm_batch* b, size_t* bytes)
     *bytes = 0;
     const emm_status st = check_rows(b);
     if (st != EMM_OK) return st;
-    if (b->dtype != EMM_BF16 || b->head_dim != 128) return EMM_ERR_UNSUPPORTED;
+    if (b->dtype != EMM_BF16 || b->head_dim != 128 || int64_t(b->num_reqs) * b->num_kv_heads > MOST_PAIRS) return EMM_ERR_UNSUPPORTED;
     *bytes = emm::attn_fp8_workspace_bytes(view_of(b));
     return EMM_OK;
 }

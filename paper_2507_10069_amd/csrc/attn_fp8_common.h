@@ -27,7 +27,8 @@ __device__ inline uint32_t most_of(const uint32_t (&pairs)[N])
     return (uint32_t)max(most[0], most[1]) << 16;
 }
 // Four values of a row of q as two parts: the nearest codes in the row's scale, and those of 16 times what they leave.  A
-// bf16 has eight significant bits and a code four, so the two hold it whole, down to 2^-22 of the row's largest value.
+// bf16 has eight significant bits and a code four, so the two hold it whole from 2^-6 in the row's scale on, where the low part's
+// steps are 2^-13: from 2^-13 of the row's largest value, which is above 224 there.  Smaller ones are off by half a step, 2^-21 of it.
 constexpr int LOW_PART_SCALE = -4;                       // of the scale byte: the low part's 1 / 16
 struct QCodes { uint32_t high, low; };
 __device__ inline QCodes split4(uint32_t pair0, uint32_t pair1, int byte)

@@ -144,6 +144,29 @@ def test_caches_and_workspaces():
         assert lib.emm_prefill_attn_fp8(big, OK, c, OK, None, OK, need - 1, None) == B.EMM_ERR_WORKSPACE
 
 
+LARGE = [dict(total_new_tokens=2 ** 25 + 1), dict(num_q_heads=4098), dict(total_new_tokens=2 ** 24, num_q_heads=66), dict(max_pages_per_req=2 ** 27)]
+
+
+@pytest.mark.parametrize("over", LARGE)
+def test_batches_beyond_the_limits_are_refused(over):
+    lib, b = B.load(), _batch(**over)
+    r, c, n = ctypes.byref(_rope()), ctypes.byref(_cache()), ctypes.c_size_t()
+    assert lib.emm_rope(b, r, OK, None, 0, 1 << 45, None, None) == B.EMM_ERR_UNSUPPORTED
+    assert lib.emm_kv_scatter_fp8(b, OK, OK, 0, c, None) == B.EMM_ERR_UNSUPPORTED
+    assert lib.emm_rope_kv_scatter_fp8(b, r, OK, OK, OK, 0, 1 << 45, c, None) == B.EMM_ERR_UNSUPPORTED
+    assert lib.emm_kv_gather_fp8(b, c, OK, OK, None) == B.EMM_ERR_UNSUPPORTED
+    assert lib.emm_attn_fp8_workspace_size(b, ctypes.byref(n)) == B.EMM_ERR_UNSUPPORTED
+
+
+def test_attention_limits():
+    lib, n = B.load(), ctypes.c_size_t()
+    at = dict(num_reqs=2 ** 19, total_new_tokens=2 ** 19, max_new_len=1)
+    assert lib.emm_attn_fp8_workspace_size(_batch(**at), ctypes.byref(n)) == B.EMM_OK            # 2^20 pairs
+    at["num_reqs"] += 1
+    assert lib.emm_attn_fp8_workspace_size(_batch(**at), ctypes.byref(n)) == B.EMM_ERR_UNSUPPORTED
+    assert lib.emm_cross_attn_fp8(_batch(**at), OK, ctypes.byref(_cache()), OK, None, OK, 1 << 40, None) == B.EMM_ERR_UNSUPPORTED
+
+
 def test_empty_batches_are_no_ops():
     lib, c, r = B.load(), ctypes.byref(_cache()), ctypes.byref(_rope())
     for b in (_batch(arrays=False, num_reqs=0, total_new_tokens=0, max_new_len=0), _batch(arrays=False, total_new_tokens=0, max_new_len=0)):
@@ -197,6 +220,10 @@ def test_binding_checks_tensors():
                 dict(positions=torch.zeros(3, 5, dtype=torch.int32)), dict(positions=torch.zeros(5, 3, dtype=torch.int32).t(), sections=[16, 24, 24])):
         with pytest.raises(ValueError):
             B.make_rope(**dict(dict(inv_freq=inv, rotary_dim=128), **bad))
+    rope = B.make_rope(inv_freq=inv, rotary_dim=128, positions=torch.zeros(3, 19, dtype=torch.int32), sections=[16, 24, 24])
+    for call in (lambda: B.emm_rope(_batch(), rope, None, None, None, None), lambda: B.emm_rope_kv_scatter_fp8(_batch(), rope, None, None, None, None, None)):
+        with pytest.raises(ValueError):                      # 19 positions, 20 tokens
+            call()
     codes = torch.zeros(4, 2, 16, 128, dtype=torch.uint8)
     with pytest.raises(ValueError):
         B.make_fp8_cache(codes.float(), codes, codes, codes)

@@ -385,6 +385,8 @@ ATTENTION_CASES = {
     "question": dict(prefix=[16384], new=[36]),
     "questions": dict(prefix=[3000, 4100, 2047], new=[9, 40, 2]),
     "many_short": dict(prefix=[(37 * i) % 90 for i in range(70)], new=[1 + (i * 7) % 12 for i in range(70)], heads=8, kv_heads=2),
+    "units_cut_in_two": dict(prefix=[700] * 5, new=[180] * 5),
+    "decode_600_requests": dict(prefix=[640 + i % 64 for i in range(600)], new=[1] * 600, heads=8, kv_heads=1),
     "cross": dict(prefix=[0, 5, 1000, 64], new=[3, 300, 17, 1], causal=False),
     "cross_one_token_each": dict(prefix=[700, 0, 33], new=[1, 1, 1], causal=False),
     "cross_nothing": dict(prefix=[0, 0], new=[5, 1], causal=False),
@@ -422,6 +424,56 @@ def test_attention_of_large_batches_on_sampled_tokens(prefix, new, reqs):
     out, lse = b.attend(q)
     tokens = sorted({0, 1, new - 1, new, b.T - 1} & set(range(b.T)) | set(b.rng.integers(0, b.T, 12).tolist()))
     print("   of the bound, lse:", b.compare(q, out, lse, tokens), flush=True)
+
+
+def test_units_cut_behind_whole_ones():
+    """320 units of 256 rows: a full round of them, and 64 that are cut along their keys."""
+    b = Batch([600 + 40 * i for i in range(16)], [180] * 16, seed=23).fill_contexts()
+    b.to_device()
+    q = b.queries()
+    b.compare(q, *b.attend(q), sorted(b.rng.choice(b.T, 60, replace=False).tolist() + [0, b.T - 1]))
+
+
+@pytest.mark.parametrize("prefix,new", [([3300] * 32, [1] * 32), ([3000, 2000, 3001], [1, 1, 1]), ([2048] * 3, [50] * 3)])
+def test_pages_in_several_places(prefix, new):
+    """Requests whose contexts begin with the same pages, and a context that holds a page twice."""
+    b = Batch(prefix, new, seed=24).fill_contexts()
+    for r in range(1, len(prefix)):
+        b.table[r, :100] = b.table[r // 2, :100]
+    b.table[0, 20:25] = b.table[0, 7]
+    b.table[-1, 101] = b.table[-1, 100]
+    b.dev["table"].copy_(torch.from_numpy(b.table))
+    b.to_device()
+    q = b.queries()
+    b.compare(q, *b.attend(q), sorted(set(b.rng.integers(0, b.T, 20).tolist()) | {0, b.T - 1}))
+
+
+@pytest.mark.parametrize("prefix,new", [([900, 3, 40], [1, 1, 1]), ([700, 0, 33], [60, 300, 2])])
+def test_pools_of_more_than_4_gib(prefix, new):
+    """Pages whose codes lie below and beyond 2^31 and 2^32 bytes: writing, reading back and attention have the bits of a small pool's."""
+    b = Batch(prefix, new, seed=25, spare=4).fill_contexts()
+    cache, q = b.to_device(), b.queries()
+    rows = [_dev(b.rng.standard_normal((b.T, 4, 128)).astype(np.float32), torch.bfloat16) for _ in range(2)]
+
+    def run(batch, cache):
+        B.emm_kv_scatter_fp8(batch, *rows, cache)
+        read = [torch.empty_like(x) for x in rows]
+        B.emm_kv_gather_fp8(batch, cache, *read)
+        b.batch, b.cache = batch, cache
+        return (*read, *b.attend(q))
+    far_pages = 530000                                       # of 8 KiB: 4.04 GiB of codes for K, and for V
+    at = torch.linspace(0, far_pages - 1, b.num_pages).round().long().to(DEV)
+    far = {n: torch.empty((far_pages,) + x.shape[1:], dtype=torch.uint8, device=DEV) for n, x in b.pools.items()}
+    for n, x in far.items():
+        x[at] = b.pools[n]
+    want = run(b.batch, cache)
+    table = b.dev["table"].long()
+    b.dev["table"].copy_(torch.where(table >= 0, at[table.clamp(min=0)], table))
+    b.batch.num_pages = far_pages
+    got = run(b.batch, B.make_fp8_cache(far["k"], far["v"], far["ks"], far["vs"]))
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    for n, x in far.items():
+        assert torch.equal(x[at], b.pools[n]), n
 
 
 @pytest.mark.parametrize("new", [[1, 1], [40, 300]])
@@ -496,6 +548,20 @@ def test_rows_behind_the_batch_and_bytes_behind_the_workspace_stay():
         guarded = torch.full((n + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
         out, lse = b.attend(q, workspace=guarded[:n] if n else None)
         assert (guarded[n:] == 0xA5).all() and (out[b.T:] == 7).all() and (lse[b.T:] == 7).all()
+        b.compare(q, out, lse)
+
+
+def test_a_batch_padded_for_capture():
+    """max_new_len and the token count say what there could be; the lengths say what there is."""
+    for new, most in (([3, 1, 0, 0], 64), ([1, 1, 0, 0], 16), ([40, 2, 0, 0], 64)):
+        b = Batch([900, 30, 0, 0], new, seed=22, extra_rows=64, wider=70).fill_contexts()
+        b.batch.max_new_len = most
+        b.to_device()
+        q = b.queries()
+        out, lse = torch.full((b.rows, 28, 128), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((b.rows, 28), 7.0, device=DEV)
+        ws = torch.empty(max(16, B.emm_attn_fp8_workspace_size(b.batch)), dtype=torch.uint8, device=DEV)
+        B.emm_prefill_attn_fp8(b.batch, q, b.cache, out, lse, ws)
+        assert (out[b.T:] == 7).all() and (lse[b.T:] == 7).all()
         b.compare(q, out, lse)
 
 
