@@ -10,8 +10,8 @@
  *   magnitudes above 448 * 2^119 = 2.98e38 are held as that;
  *   infinities and NaN become the format's NaN and change no other value of the row.
  *   value = code * 2^(byte - 127)
- * A power of two costs a floating format no precision, the division by it is exact, every value is exact in bf16 as
- * well as fp32, and the scale is what the chip's matrix instructions take beside the codes.
+ * A power of two costs a floating format no precision, the division by it is exact, and every value is exact in bf16
+ * as well as fp32, so that the chip's conversions and matrix instructions add no error of their own.
  *
  * Conventions are those of emm.h.  dtype of the batch is that of q, k_new, v_new, out and of what is read back; the
  * pools' are fixed.  Slots that hold no token may hold any bits.  emm_kv_pages_pack / emm_kv_pages_unpack move pages
@@ -63,10 +63,9 @@ emm_status emm_kv_gather_fp8(const emm_batch *batch, const emm_fp8_cache *cache,
 /*
  * emm_prefill_attn, emm_cross_attn and emm_decode_attn over such a cache: the attention of the values that it stands
  * for, for any number of new tokens per request (emm_decode_attn_fp8: at most one, else EMM_ERR_INVALID_ARG).
- * EMM_BF16 with head_dim 128.  Arguments and results as there.  Codes meet q on the matrix pipe as they are; q goes in
- * as the sum of two 8-bit parts, which holds a bf16 whole down to 2^-13 of its row's largest value and smaller ones to
- * within 2^-21 of that; scores, softmax statistics and sums are in 32 bits; softmax weights are rounded to bf16 for the
- * value product.  A NaN in V reaches only rows that see its slot.  Results are run-to-run bitwise deterministic.
+ * EMM_BF16 with head_dim 128.  Arguments and results as there.  Values are exact in bf16 and meet q as such; scores,
+ * softmax statistics and sums are in 32 bits; softmax weights are rounded to bf16 for the value product.  A NaN in V
+ * reaches only rows that see its slot.  Results are run-to-run bitwise deterministic.
  *   workspace  device scratch of at least emm_attn_fp8_workspace_size bytes, 16-byte aligned (may be NULL if that is
  *              0), the same size for all three calls; contents need no initialisation and mean nothing afterwards.
  *              Calls that may overlap must not share one.

@@ -10,9 +10,8 @@
 // records of a pair up.  Inside a workgroup the four waves take a pair's tiles in turn, straight from global memory to
 // registers, and meet in LDS at the end of the pair.
 //
-// Scores, S^T = K Q^T: v_mfma_scale_f32_16x16x128_f8f6f4 takes 16 keys with all 128 channels as they lie in the cache, a
-// key's scale byte beside them.  q is the sum of two 8-bit parts (split4); the second product carries the 1/16 in its
-// block scale.
+// Scores, S^T = K Q^T: a lane has 32 channels of a key, which v_cvt_scalef32_pk_bf16_fp8 makes bf16 in the key's scale (exact)
+// for four v_mfma_f32_16x16x32_bf16, and the same 32 channels of its row of q.
 // Values, O^T += V^T P^T: v_mfma_f32_16x16x32_bf16 wants for each channel 8 keys of a lane side by side.  A lane reads 8
 // neighbouring channels of the 8 keys whose scores it holds (the accumulators of two score products, which are then
 // its part of the operand P^T as they are), pairs keys by byte permutes, and v_cvt_scalef32_pk_bf16_fp8 makes two bf16 of
@@ -44,25 +43,6 @@ constexpr int MOST_COMPARED = 512;                       // requests among which
 // of the four lanes (l, l ^ 16, l ^ 32, l ^ 48) that hold a row
 __device__ inline float row_max(float x) { return max32(max16(x)); }
 __device__ inline float row_sum(float x) { return sum32(sum16(x)); }
-
-// q's operands of the score product: 32 channels of the lane's row
-struct QParts {
-    i32x8 high, low;
-    int scale_high, scale_low;                           // scale bytes
-};
-__device__ inline QParts split_q(const uint32_t (&pairs)[16])
-{
-    QParts p;
-    p.scale_high = q_scale_byte(__float_as_uint(row_max(__uint_as_float(most_of(pairs)))));
-    p.scale_low = p.scale_high == 0xff ? 0xff : p.scale_high + LOW_PART_SCALE;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-        const QCodes c = split4(pairs[2 * w], pairs[2 * w + 1], p.scale_high);
-        p.high[w] = (int)c.high;
-        p.low[w] = (int)c.low;
-    }
-    return p;
-}
 
 // how the batch's tiles are dealt
 struct RowsLayout {
@@ -279,13 +259,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Arg
     for (bool first_segment = true;; first_segment = false) {
         const int all_see = CAUSAL ? now.rq.P + 1 : now.rq.P;            // keys that every row sees
         int limit[RT];                                                   // last key that the lane's row sees
-        QParts q[RT];
+        bf16x8 q[RT][4];                                                 // of the lane's row: the channels that it has of a key
         float m[RT], l[RT];
         f32x4 o[RT][8];                                                  // channels 32 g + 8 v + i of the row, in o[i][v]
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             limit[rt] = CAUSAL ? now.rq.P + L.by_G.quotient(min(rt * ROWS + n16, now.n_rows - 1)) : now.rq.P - 1;
-            q[rt] = split_q(pairs[rt]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[rt][j] = __builtin_bit_cast(bf16x8, u32x4{pairs[rt][4 * j], pairs[rt][4 * j + 1], pairs[rt][4 * j + 2], pairs[rt][4 * j + 3]});
             m[rt] = -INFINITY;
             l[rt] = 0.f;
 #pragma unroll
@@ -306,13 +287,22 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Arg
             f32x4 s[RT][2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const uint4 k0 = tile.k[2 * k], k1 = tile.k[2 * k + 1];
-                const i32x8 kf = {(int)k0.x, (int)k0.y, (int)k0.z, (int)k0.w, (int)k1.x, (int)k1.y, (int)k1.z, (int)k1.w};
+                const uint32_t codes[8] = {tile.k[2 * k].x, tile.k[2 * k].y, tile.k[2 * k].z, tile.k[2 * k].w, tile.k[2 * k + 1].x, tile.k[2 * k + 1].y,
+                                           tile.k[2 * k + 1].z, tile.k[2 * k + 1].w};
+                const float scale = up_scale(tile.k_scale[k]);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    s[rt][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    s[rt][k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, q[rt].high, s[rt][k], 0, 0, 0, tile.k_scale[k], 0, q[rt].scale_high);
-                    s[rt][k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, q[rt].low, s[rt][k], 0, 0, 0, tile.k_scale[k], 0, q[rt].scale_low);
+                for (int rt = 0; rt < RT; ++rt) s[rt][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    u32x4 w;                                             // 8 channels of the lane's key
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * j + i], scale, false));
+                        w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * j + i], scale, true));
+                    }
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+                        s[rt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), q[rt][j], s[rt][k], 0, 0, 0);
                 }
             }
             const int key0 = t * TILE + 4 * g;                           // key of score (k, i): key0 + 16 k + i

@@ -1,4 +1,8 @@
-// What the two attention kernels over the 8-bit cache share: q's operands, the plan's scan, the format's NaN.
+// What the two attention kernels over the 8-bit cache share: sums over lanes, the format's NaN.
+//
+// Both make K's codes bf16, in their row's scale (v_cvt_scalef32_pk_bf16_fp8, exact), for products in bf16.  The matrix instructions
+// that take the codes as they are would save that, but keep a sum of 8-bit products only to about 2^-16 of the largest of them (128
+// random products of up to 5e4: off by 1.8, in bf16 by 0.001), which makes the scores 25 times less exact than 32 bits are.
 #pragma once
 
 #include "fp8_device.h"
@@ -6,47 +10,11 @@
 namespace emm {
 namespace fp8 {
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int HEAD_DIM = 128;
 constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
-
-// The scale byte of a row of q from the bits of its largest |x|; NaN's where a value is not finite, and then every score of the
-// row is NaN.
-__device__ inline int q_scale_byte(uint32_t most_bits) { return most_bits < 0x7f800000u ? scale_byte(most_bits) : 0xff; }
-// The largest |x| of the pairs of a row, as bits of 32
-template <int N>
-__device__ inline uint32_t most_of(const uint32_t (&pairs)[N])
-{
-    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-    u16x2 most = {0, 0};
-#pragma unroll
-    for (int i = 0; i < N; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, pairs[i] & 0x7fff7fffu));
-    return (uint32_t)max(most[0], most[1]) << 16;
-}
-// Four values of a row of q as two parts: the nearest codes in the row's scale, and those of 16 times what they leave.  A
-// bf16 has eight significant bits and a code four, so the two hold it whole from 2^-6 in the row's scale on, where the low part's
-// steps are 2^-13: from 2^-13 of the row's largest value, which is above 224 there.  Smaller ones are off by half a step, 2^-21 of it.
-constexpr int LOW_PART_SCALE = -4;                       // of the scale byte: the low part's 1 / 16
-struct QCodes { uint32_t high, low; };
-__device__ inline QCodes split4(uint32_t pair0, uint32_t pair1, int byte)
-{
-    typedef short s16x2 __attribute__((ext_vector_type(2)));
-    const float scale = up_scale(byte), low_scale = up_scale(byte + LOW_PART_SCALE);
-    s16x2 w = {0, 0};
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, pair0), scale, false);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, pair1), scale, true);
-    QCodes c;
-    c.high = __builtin_bit_cast(uint32_t, w);
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c.high, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c.high, scale, true);
-    s16x2 v = {0, 0};
-    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, __uint_as_float(pair0 << 16) - a[0], __uint_as_float(pair0 & 0xffff0000u) - a[1], low_scale, false);
-    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, __uint_as_float(pair1 << 16) - d[0], __uint_as_float(pair1 & 0xffff0000u) - d[1], low_scale, true);
-    c.low = __builtin_bit_cast(uint32_t, v);
-    return c;
-}
 
 // x with the lane 16 further (within 32), and with the lane 32 further, in both lanes
 __device__ inline float max16(float x)

@@ -3,15 +3,14 @@
 // Bound by the matrix pipe and the instructions around it.  Rows are (new token, query head of a KV group) pairs of one
 // (request, KV head), token-major; a workgroup of 8 waves takes 256 of them (a unit), a wave 32, and streams the keys
 // in tiles of 64, each fetched once for the workgroup:
-//   K     stays in 8 bits: global memory -> LDS (a ring of four tiles, fetched three ahead), 16-byte chunks placed so that the
-//         operand reads meet no bank twice (the hardware fixes where a lane's bytes land, so the lane picks what it fetches);
-//   V     goes to LDS as it is, and from there through the wave that fetched it, which makes it bf16 in its keys' scales
-//         (exact) and puts it into a ring of two tiles that the transposing reads take channels from;
-//   scale bytes travel with them.
-// S^T = K Q^T is v_mfma_scale_f32_32x32x64_f8f6f4: a key's scale byte is its row's block scale, and q comes as two 8-bit
-// parts (split4), so the scores are those of the bf16 q with half of K's LDS reads and none of its conversions.  A lane
-// has one row and 32 of a tile's keys; K's rows lie in LDS such that its weights, rounded to bf16, are the operand of
-// O^T += V^T P^T (v_mfma_f32_32x32x16_bf16) as they are.
+// K and V go to LDS as they are (K three tiles ahead, V two), and from there through the wave that fetched them, which makes them
+// bf16 in their keys' scales (exact) and puts them into rings of two tiles, in 16-byte chunks placed so that no read or write of
+// them meets a bank twice.  Scale bytes travel with them, K's a tile earlier: a wave brings those of other waves' rows, and K is
+// converted before the barrier that V waits for.  (Each wave converting what it needs of K in its registers takes 64 conversions
+// a tile in place of 8: two chunks of 2048 behind 16 k 923 us, so 900.)
+// S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_32x32x16_bf16.  A lane has one row and 32 of a tile's keys; K's rows lie in
+// LDS such that its weights, rounded to bf16, are the second product's operand as they are, and which channels a step of the first
+// takes is the same for K and q.
 // Weights are exp2(S c - m) with a reference m that is the row's maximum over its first tile, and follows only where a
 // tile's weights sum to more than 2^20: any reference gives the same result, and the sum, which is taken before
 // the weights are used, tells in time.  So the loop takes no maxima.  Row sums are of the weights before they are
@@ -41,8 +40,8 @@ constexpr float LAG_LIMIT = 1048576.f;                   // 2^20
 constexpr int QK_OPS = 80;                               // of a tile's 119 softmax instructions beside the score products
 
 // LDS
-constexpr int K_TILE = BC * HEAD_DIM, V_TILE = BC * HEAD_DIM * 2, RAW_TILE = BC * HEAD_DIM;
-constexpr int K_AT = 0, V_AT = K_AT + 4 * K_TILE, RAW_AT = V_AT + 2 * V_TILE, S_AT = RAW_AT + 2 * RAW_TILE, FLAG_AT = S_AT + 4 * 128, SMEM = FLAG_AT + 64;
+constexpr int TILE = BC * HEAD_DIM * 2, RAW_TILE = BC * HEAD_DIM;
+constexpr int K_AT = 0, V_AT = K_AT + 2 * TILE, K_RAW_AT = V_AT + 2 * TILE, RAW_AT = K_RAW_AT + 4 * RAW_TILE, S_AT = RAW_AT + 2 * RAW_TILE, FLAG_AT = S_AT + 4 * 128, SMEM = FLAG_AT + 64;
 constexpr int OUT_STRIDE = 272;                          // bytes between output rows on their way out
 static_assert(NW * 32 * OUT_STRIDE <= FLAG_AT, "output rows are staged over the rings");
 constexpr int FETCHES = 3;                               // of a wave for a tile: K, V, scales
@@ -197,8 +196,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     const int n_blocks = (e.ctx + 15) >> 4;
     const uint32_t smem_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
     const int r16 = 8 * (wave & 1) + (lane >> 3);            // row in the block
-    // K: LDS row = block row with the key's bits 2 and 3 changed places; chunk c of row r lies at place c ^ (r / 2 mod 8)
-    const uint32_t k_src = swap23(r16) * HEAD_DIM + (((lane & 7) ^ ((r16 >> 1) & 7)) << 4);
+    const uint32_t k_src = swap23(r16) * HEAD_DIM + ((lane & 7) << 4);    // K: LDS row = block row with the key's bits 2 and 3 changed places
     const uint32_t v_src = (wave & 1) * 1024 + lane * 16;    // V: as it is
     const unsigned char* scales = (wave & 1) ? a.pools.v_scale : a.pools.k_scale;
     int block_ids = 0, ids_from = 0;                         // lane k: the wave's block of tile ids_from + k, in blocks of the pool
@@ -219,25 +217,26 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
             pairs[4 * i] = x.x; pairs[4 * i + 1] = x.y; pairs[4 * i + 2] = x.z; pairs[4 * i + 3] = x.w;
         }
     }
-    i32x8 q_high[2], q_low[2];
-    int q_scale_high = 0, q_scale_low = 0;
-    auto split_q = [&]() {
-        const uint32_t most = __float_as_uint(max32(__uint_as_float(most_of(pairs))));
-        q_scale_high = q_scale_byte(most);
-        q_scale_low = q_scale_high == 0xff ? 0xff : q_scale_high + LOW_PART_SCALE;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) {
-            const QCodes c = split4(pairs[2 * w], pairs[2 * w + 1], q_scale_high);
-            q_high[w >> 3][w & 7] = (int)c.high;
-            q_low[w >> 3][w & 7] = (int)c.low;
-        }
-    };
     auto block_of = [&](int t) { return (long long)__builtin_amdgcn_readlane(block_ids, t - ids_from); };
-    auto fetch_k = [&](int t, int slot) { lds_dma16(a.pools.k + block_of(t) * 2048, k_src, smem_base + K_AT + slot * K_TILE + wave * 1024); };
+    auto fetch_k = [&](int t, int slot) { lds_dma16(a.pools.k + block_of(t) * 2048, k_src, smem_base + K_RAW_AT + slot * RAW_TILE + wave * 1024); };
     auto fetch_v = [&](int t, int slot) { lds_dma16(a.pools.v + block_of(t) * 2048, v_src, smem_base + RAW_AT + slot * RAW_TILE + wave * 1024); };
+    const int k_scales = 1 - (wave & 1);                     // the wave brings scales of K, and those a tile earlier
     auto fetch_scales = [&](int t, int slot) {
         const unsigned char* src = scales + block_of(t) * 16;
         if (lane < 4) lds_dma4(src, lane * 4, smem_base + S_AT + slot * 128 + (wave & 1) * 64 + (wave >> 1) * 16);
+    };
+
+    // ---- K to bf16: 16 channels of a key per lane.  K tile: chunk c of 16 bytes of row r lies at place c ^ (r mod 16)
+    const int k_row = 8 * wave + (lane >> 3), k_wr = K_AT + k_row * 256 + (((2 * (lane & 7)) ^ (k_row & 15)) << 4), ks_rd = S_AT + 16 * (wave >> 1) + swap23(r16);
+    auto read_raw_k = [&](int slot) -> uint4 { return *(const uint4*)(smem + K_RAW_AT + slot * RAW_TILE + wave * 1024 + lane * 16); };
+    auto store_k = [&](const uint4& codes, int scale, int slot) {
+        const float s = up_scale(scale);
+        auto half = [&](uint32_t w0, uint32_t w1) -> uint4 {
+            return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, true)),
+                              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true)));
+        };
+        *(uint4*)(smem + slot * TILE + k_wr) = half(codes.x, codes.y);
+        *(uint4*)(smem + slot * TILE + (k_wr ^ 16)) = half(codes.z, codes.w);
     };
 
     // ---- V to bf16: 16 channels of a key per lane.  Keys behind the context hold anything: zeros in their place.  In tiles that not every
@@ -271,8 +270,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
         return make_uint4(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1), __builtin_bit_cast(uint32_t, p2), __builtin_bit_cast(uint32_t, p3));
     };
     auto store_v = [&](int v_slot) {
-        *(uint4*)(smem + v_slot * V_TILE + v_wr) = widen(0);
-        *(uint4*)(smem + v_slot * V_TILE + (v_wr ^ 16)) = widen(1);
+        *(uint4*)(smem + v_slot * TILE + v_wr) = widen(0);
+        *(uint4*)(smem + v_slot * TILE + (v_wr ^ 16)) = widen(1);
     };
 
     // which of the lane's 64 outputs meet a NaN of V: bit 4 (4 nb + v / 4) + v % 4.  Rare: from global memory, key by key.
@@ -293,22 +292,20 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     };
 
     // ---- operands
-    const int k_rd = K_AT + l32 * HEAD_DIM + (((2 * h32) ^ ((l32 >> 1) & 7)) << 4);      // the other three chunks: ^ 16, ^ 64
-    const int ks_rd = S_AT + swap23(l32);
-    auto read_k = [&](int slot, int kb, int s) -> i32x8 {
-        const uint4 x = *(const uint4*)(smem + slot * K_TILE + kb * 32 * HEAD_DIM + (k_rd ^ (s << 6)));
-        const uint4 y = *(const uint4*)(smem + slot * K_TILE + kb * 32 * HEAD_DIM + (k_rd ^ (s << 6) ^ 16));
-        return i32x8{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
+    const int k_rd = K_AT + l32 * 256 + (((4 * h32) ^ (l32 & 15)) << 4);
+    auto read_k = [&](int slot, int kb, int j) -> bf16x8 {       // 8 of the lane's 64 channels of a key, as q_operand(j)
+        return *(const bf16x8*)(smem + slot * TILE + kb * 32 * 256 + (k_rd ^ (((j >> 2) * 8 + (j & 3)) << 4)));
     };
     // within each 16 lanes, lane j gives the address of 4 channels of key k0 + j / 4 and gets keys k0 .. k0 + 3 of channel d0 + j
     const int v_rd = V_AT + (8 * h32 + ((lane & 15) >> 2)) * 256 + ((4 * ((lane & 15) >> 2) + 2 * ((lane >> 4) & 1) + (((lane & 3) >> 1) ^ ((lane >> 2) & 1))) << 4) + (lane & 1) * 8;
     auto read_v = [&](int slot, int k16, int nb) -> bf16x8 {     // keys 16 k16 .. + 15, channels 32 nb .. + 31
         typedef short s16x4 __attribute__((ext_vector_type(4)));
-        const unsigned char* src = smem + slot * V_TILE + 16 * k16 * 256 + (v_rd ^ (nb << 6));
+        const unsigned char* src = smem + slot * TILE + 16 * k16 * 256 + (v_rd ^ (nb << 6));
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src + 4 * 256));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
+    auto q_operand = [&](int j) -> bf16x8 { return __builtin_bit_cast(bf16x8, u32x4{pairs[4 * j], pairs[4 * j + 1], pairs[4 * j + 2], pairs[4 * j + 3]}); };
     const float c_log2 = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, b.softmax_scale * LOG2E)));
 
     f32x16 o[4];
@@ -338,15 +335,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     auto scores = [&](int slot, f32x16 (&s)[2]) {            // not interleaved: first and only tiles
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const int scale = smem[ks_rd + slot * 128 + 32 * kb];
 #pragma unroll
             for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                const i32x8 kf = read_k(slot, kb, st);
-                s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, q_high[st], s[kb], 0, 0, 0, scale, 0, q_scale_high);
-                s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, q_low[st], s[kb], 0, 0, 0, scale, 0, q_scale_low);
-            }
+            for (int j = 0; j < 8; ++j) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_k(slot, kb, j), q_operand(j), s[kb], 0, 0, 0);
         }
     };
     // weights of half a tile (32 keys), packed, and their sum over the lane's keys
@@ -408,22 +400,28 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
             fetch_scales(t_begin + 1, 1);
             fetch_k(t_begin + 2, 2);
             fetch_scales(t_begin + 2, 2);
+            if (k_scales) fetch_scales(t_begin + 3, 3);
         }
-        if (active) split_q();
         __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0)
         __syncthreads();
         read_raw(0, 0);
         if (t_begin >= unit_clear) check_raw(t_begin, 0);
         store_v(0);
+        store_k(read_raw_k(0), smem[ks_rd], 0);
+        if (n_tiles > 1) store_k(read_raw_k(1), smem[ks_rd + 128], 1);
+        __syncthreads();
         const int t_end = t_begin + n_tiles;
         if (!active) {
+            if (n_tiles > 1) __syncthreads();
             for (int i = t_begin; i + 1 < t_end; ++i) {
                 const int R = (i - t_begin) & 3;
-                if (i + 3 - ids_from >= 64) ask_blocks(i + 2);
+                if (i + 4 - ids_from >= 64) ask_blocks(i + 2);
                 fetch_k(i + 3, (R + 3) & 3);
                 fetch_v(i + 2, R & 1);
-                fetch_scales(i + 3, (R + 3) & 3);
+                fetch_scales(i + 3 + k_scales, (R + 3 + k_scales) & 3);
                 __builtin_amdgcn_s_waitcnt(0x0f70 | FETCHES);
+                __builtin_amdgcn_sched_barrier(0);
+                store_k(read_raw_k((R + 2) & 3), smem[ks_rd + ((R + 2) & 3) * 128], R & 1);
                 __syncthreads();
                 read_raw((R + 1) & 1, (R + 1) & 3);
                 if (i + 1 >= unit_clear) check_raw(i + 1, (R + 1) & 1);
@@ -433,6 +431,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
         } else {
             f32x16 sc[2][2];                                 // scores of tile i in sc[i & 1]
             scores(0, sc[0]);
+            if (n_tiles > 1) __syncthreads();                // (tile 2 goes where tile 0 was)
             if (t_begin >= wave_clear) mask_tile(t_begin, sc[0]);
             const float top = row_max(sc[0]) * c_log2;
             m = top > -INFINITY ? top : 0.f;                 // (a row that sees none of a piece's keys: its weights are zeros)
@@ -479,31 +478,37 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
                 constexpr int OPS = 17 * 7, OPS_HERE = QK_OPS;   // (pairs 0 .. 7, the first half, are done after 63)
                 fa[0] = fmaf(s_cur[0][0], c_log2, -ref);
                 fb[0] = fmaf(s_cur[0][1], c_log2, -ref);
-                const int scale0 = smem[ks_rd + KS * 128], scale1 = smem[ks_rd + KS * 128 + 32];
-                i32x8 kf[4];                                 // channels 0 .. 63 and 64 .. 127 of block 0, then of block 1
-                kf[0] = read_k(KS, 0, 0);
+                bf16x8 ka[16 + 2];
+                ka[0] = read_k(VN, 0, 0);
+                ka[1] = read_k(VN, 0, 1);
+                uint4 raw_k;
+                int raw_k_scale;
                 __builtin_amdgcn_sched_barrier(0);
-                static_for<0, 8>([&](auto kc) {
-                    constexpr int k = decltype(kc)::value, st = (k >> 1) & 1, kb = k >> 2;
-                    constexpr bool low = (k & 1) != 0;
-                    if constexpr (!low && k < 6) kf[(k >> 1) + 1] = read_k(KS, (k + 2) >> 2, ((k >> 1) + 1) & 1);
-                    if constexpr ((k & 3) == 0) {
+                static_for<0, 16>([&](auto kc) {
+                    constexpr int k = decltype(kc)::value, kb = k >> 3;
+                    if constexpr (k + 2 < 16) ka[k + 2] = read_k(VN, (k + 2) >> 3, (k + 2) & 7);
+                    if constexpr ((k & 7) == 0) {
                         f32x16 zero;
 #pragma unroll
                         for (int v = 0; v < 16; ++v) zero[v] = 0.f;
-                        s_nxt[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[k >> 1], q_high[0], zero, 0, 0, 0, kb ? scale1 : scale0, 0, q_scale_high);
+                        s_nxt[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[k], q_operand(0), zero, 0, 0, 0);
                     } else {
-                        s_nxt[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[k >> 1], low ? q_low[st] : q_high[st], s_nxt[kb], 0, 0, 0, kb ? scale1 : scale0, 0,
-                                                                                    low ? q_scale_low : q_scale_high);
+                        s_nxt[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[k], q_operand(k & 7), s_nxt[kb], 0, 0, 0);
                     }
-                    static_for<(k * OPS_HERE) / 8, ((k + 1) * OPS_HERE) / 8>(softmax_op);
-                    if constexpr (k == 1) fetch_k(i + 3, (R + 3) & 3);
-                    if constexpr (k == 2) fetch_v(i + 2, R & 1);
-                    if constexpr (k == 3) fetch_scales(i + 3, (R + 3) & 3);
+                    static_for<(k * OPS_HERE) / 16, ((k + 1) * OPS_HERE) / 16>(softmax_op);
+                    if constexpr (k == 2) fetch_k(i + 3, (R + 3) & 3);
+                    if constexpr (k == 4) fetch_v(i + 2, R & 1);
+                    if constexpr (k == 6) fetch_scales(i + 3 + k_scales, (R + 3 + k_scales) & 3);
+                    if constexpr (k == 10) {
+                        __builtin_amdgcn_s_waitcnt(0x0f70 | FETCHES);        // all fetches but this iteration's have landed
+                        __builtin_amdgcn_sched_barrier(0);
+                        raw_k = read_raw_k((R + 2) & 3);
+                        raw_k_scale = smem[ks_rd + ((R + 2) & 3) * 128];
+                    }
+                    if constexpr (k == 14) store_k(raw_k, raw_k_scale, R & 1);
                     __builtin_amdgcn_sched_barrier(0);
                 });
                 settle(s_cur[0], p, sums[0] + sums[1], ref);
-                __builtin_amdgcn_s_waitcnt(0x0f70 | FETCHES);        // all fetches but this iteration's have landed
                 __syncthreads();
                 __builtin_amdgcn_sched_barrier(0);
                 read_raw(VN, KS);
@@ -537,7 +542,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
             };
             int i = t_begin;
             for (;;) {
-                if (i + 6 - ids_from >= 64) ask_blocks(i + 2);       // tiles i + 2 .. i + 6 may be fetched in this trip
+                if (i + 7 - ids_from >= 64) ask_blocks(i + 2);       // tiles i + 2 .. i + 7 may be fetched in this trip
                 if (i + 1 >= t_end) break;
                 iteration(i, std::integral_constant<int, 0>{});
                 if (i + 2 >= t_end) break;

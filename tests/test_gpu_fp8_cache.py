@@ -5,8 +5,8 @@ Tolerances.  Quantising, scales, reading back and moves are exact: bytes are com
 dtype (2^-8 of the value in bf16, 2^-24 in fp32) and the 32-bit arithmetic before it: cosine and sine are at most 5e-7 off
 (angle in turns rounded to 2^-25 turns = 1.9e-7 rad, sincospi 2 ulp), the products and their sum 3 * 2^-24: 1e-6 (|a| + |b|).
 Attention: softmax weights and the result are rounded to bf16, at most 2^-8 relative each: 2^-8 (sum of p |v| + |out|); a
-score is off by at most e = (130 * 2^-24 + 2^-21) * scale * |q| |k| (128 sums in 32 bits; q's two parts leave 2^-22 of its
-row's largest value), which changes the weights by 2 e relative, and lse by e, 2^-24 per key summed and 2^-22 of itself."""
+score is off by at most e = 130 * 2^-24 * scale * |q| |k| (128 sums in 32 bits of exact products), which changes the
+weights by 2 e relative, and lse by e, 2^-24 per key summed and 2^-22 of itself."""
 import numpy as np
 import pytest
 import torch
@@ -135,7 +135,7 @@ class Batch:
             got, got_lse = got[tokens], got_lse[tokens]
         q_len = np.linalg.norm(_f64(q)[: self.T], axis=-1).max(initial=0)
         k_len = np.linalg.norm(W.bf16_bits_to_f32(self.bits("k")).astype(np.float64), axis=-1).max()
-        e = (130 * 2.0 ** -24 + 2.0 ** -21) * self.batch.softmax_scale * q_len * k_len
+        e = 130 * 2.0 ** -24 * self.batch.softmax_scale * q_len * k_len
         keys = int((self.prefix + self.new).max())
         bound = (2.0 ** -8 + 2 * e + keys * 2.0 ** -24) * size + 2.0 ** -8 * np.abs(want) + 1e-30
         off = np.abs(got - want)
