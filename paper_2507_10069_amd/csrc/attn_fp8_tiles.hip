@@ -475,25 +475,26 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
                         pin(sums[2 * ((g - 1) >> 3) + 1]);
                     }
                 };
+                __builtin_amdgcn_s_setprio(0);
                 constexpr int OPS = 17 * 7, OPS_HERE = QK_OPS;   // (pairs 0 .. 7, the first half, are done after 63)
                 fa[0] = fmaf(s_cur[0][0], c_log2, -ref);
                 fb[0] = fmaf(s_cur[0][1], c_log2, -ref);
                 bf16x8 ka[16 + 2];
                 ka[0] = read_k(VN, 0, 0);
-                ka[1] = read_k(VN, 0, 1);
+                ka[1] = read_k(VN, 1, 0);
                 uint4 raw_k;
                 int raw_k_scale;
                 __builtin_amdgcn_sched_barrier(0);
                 static_for<0, 16>([&](auto kc) {
-                    constexpr int k = decltype(kc)::value, kb = k >> 3;
-                    if constexpr (k + 2 < 16) ka[k + 2] = read_k(VN, (k + 2) >> 3, (k + 2) & 7);
-                    if constexpr ((k & 7) == 0) {
+                    constexpr int k = decltype(kc)::value, kb = k & 1;
+                    if constexpr (k + 2 < 16) ka[k + 2] = read_k(VN, k & 1, (k + 2) >> 1);
+                    if constexpr (k < 2) {
                         f32x16 zero;
 #pragma unroll
                         for (int v = 0; v < 16; ++v) zero[v] = 0.f;
                         s_nxt[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[k], q_operand(0), zero, 0, 0, 0);
                     } else {
-                        s_nxt[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[k], q_operand(k & 7), s_nxt[kb], 0, 0, 0);
+                        s_nxt[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[k], q_operand(k >> 1), s_nxt[kb], 0, 0, 0);
                     }
                     static_for<(k * OPS_HERE) / 16, ((k + 1) * OPS_HERE) / 16>(softmax_op);
                     if constexpr (k == 2) fetch_k(i + 3, (R + 3) & 3);
@@ -511,6 +512,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
                 settle(s_cur[0], p, sums[0] + sums[1], ref);
                 __syncthreads();
                 __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(1);                       // a wave at its value products, which have less beside them, goes first
                 read_raw(VN, KS);
                 bf16x8 vf[16 + 2];
                 vf[0] = read_v(VS, 0, 0);
