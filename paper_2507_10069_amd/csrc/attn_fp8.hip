@@ -575,7 +575,6 @@ __global__ __launch_bounds__(THREADS) void attn_fp8_merge_rows_kernel(AttnFp8Arg
         *(uint4*)((__bf16*)a.out + place_of(b, L, rq, kvh, rt * ROWS + out_row) * D + 32 * g + at) = *(const uint4*)&rows[out_row][at];
 }
 
-constexpr int MOST_ROWS = 2 * ROWS;
 long long rows_of(const BatchView& b) { return (long long)b.max_new_len * (b.num_q_heads / b.num_kv_heads); }
 // tiles that the page table could hold
 long long line_of(const BatchView& b) { return ((long long)b.max_pages * b.page_size + TILE - 1) / TILE * b.num_reqs * b.num_kv_heads; }
@@ -608,10 +607,16 @@ hipError_t launch_rows(const AttnFp8Args& a, hipStream_t stream)
 
 }  // namespace
 
-// Few rows of a (request, KV head): their keys are split over the chip.  Many: rows over the waves, keys through LDS.
+// Few rows of a (request, KV head): their keys are split over the chip.  Many: rows over the waves, keys through LDS; and 17 to 32
+// rows of few pairs, which leave this kernel's two accumulators without a tile on the way (28 rows: 4 pairs of 1500 keys 11.0 us and
+// 14.2 here, 16 pairs 12.9 and 15.2, of 16000 28.0 and 26.9; 32 pairs of 16000 44.5 and 38.7, 256 of 8000 137 and 113).
 // (Tables so wide that the line could pass 2^31 tiles, a terabyte of cache or pages shared by thousands, go the second way.)
 namespace {
-bool few_rows(const BatchView& b) { return rows_of(b) <= MOST_ROWS && line_of(b) < (1ll << 31) - (1 << 20); }
+constexpr int FEW_PAIRS = 16;
+bool few_rows(const BatchView& b)
+{
+    return rows_of(b) <= ((long long)b.num_reqs * b.num_kv_heads > FEW_PAIRS ? 2 * ROWS : ROWS) && line_of(b) < (1ll << 31) - (1 << 20);
+}
 }  // namespace
 
 size_t attn_fp8_workspace_bytes(const BatchView& b)

@@ -34,7 +34,7 @@ constexpr int NW = 8;                                    // waves of a workgroup
 constexpr int BR = 32 * NW;                              // rows of a unit
 constexpr int BC = 64;                                   // keys of a tile
 constexpr int PLACES = 256;                              // workgroups that run at once: one on each compute unit
-constexpr int MAX_PARTS = 64;                            // pieces of a unit
+constexpr int MAX_PARTS = 128;                           // pieces of a unit
 constexpr int MIN_TILES_ALONE = 2, MIN_TILES_BEHIND = 4;    // key tiles of a piece where no unit is whole, and behind whole ones
 constexpr float LAG_LIMIT = 1048576.f;                   // 2^20
 constexpr int QK_OPS = 80;                               // of a tile's 119 softmax instructions beside the score products

@@ -376,6 +376,9 @@ ATTENTION_CASES = {
     "decode_many": dict(prefix=list(range(3, 300, 3)), new=[1] * 99, heads=8, kv_heads=2),
     "decode_long": dict(prefix=[20000, 3, 9000], new=[1, 1, 1]),
     "decode_wide_table": dict(prefix=[900, 77], new=[1, 1], wider=4000),
+    "decode_20_heads_a_group_more": dict(prefix=[127, 1023, 0, 31, 32, 5, 64, 700, 96, 2], new=[1] * 10, heads=40, kv_heads=2),
+    "few_rows_of_many": dict(prefix=[1000, 0, 63, 31, 200], new=[2, 3, 4, 1, 4]),
+    "few_rows_of_many_cross": dict(prefix=[1000, 0, 63, 31, 200], new=[2, 3, 4, 0, 4], causal=False),
     "few_rows": dict(prefix=[1000, 0, 63], new=[2, 3, 5]),
     "few_rows_one_head": dict(prefix=[95, 96, 97], new=[33, 1, 64], heads=2, kv_heads=2),
     "prompts": dict(prefix=[0, 17, 100, 0], new=[33, 1, 64, 100]),
@@ -426,12 +429,26 @@ def test_attention_of_large_batches_on_sampled_tokens(prefix, new, reqs):
     print("   of the bound, lse:", b.compare(q, out, lse, tokens), flush=True)
 
 
-def test_units_cut_behind_whole_ones():
-    """320 units of 256 rows: a full round of them, and 64 that are cut along their keys."""
-    b = Batch([600 + 40 * i for i in range(16)], [180] * 16, seed=23).fill_contexts()
+LAST_ROUNDS = {
+    "cut behind whole ones": ([600 + 40 * i for i in range(16)], [180] * 16),                # 320 units of 256 rows
+    "three quarters of a round": ([4200] * 8, [200] * 8),                                    # 192
+    "of many lengths": ([100, 6000, 0, 9000, 4500, 300, 5000], [300, 200, 256, 37, 220, 250, 300]),     # 188
+    "more behind whole ones": ([4300, 4100, 5000] * 4, [340, 256, 300] * 4),                # 416
+}
+
+
+@pytest.mark.parametrize("name", list(LAST_ROUNDS))
+def test_units_behind_the_last_whole_round(name):
+    """What fills less than half of the chip is cut along the keys, more is not."""
+    print("case last round", name, flush=True)
+    b = Batch(*LAST_ROUNDS[name], seed=23).fill_contexts()
     b.to_device()
     q = b.queries()
-    b.compare(q, *b.attend(q), sorted(b.rng.choice(b.T, 60, replace=False).tolist() + [0, b.T - 1]))
+    out, lse = b.attend(q)
+    firsts = [int(x) for c in b.cu[:-1] for x in (c, c + 20)]
+    b.compare(q, out, lse, sorted(set(b.rng.choice(b.T, 40, replace=False).tolist() + firsts + [b.T - 1])))
+    again, lse_again = b.attend(q)
+    assert torch.equal(out, again) and torch.equal(lse, lse_again)
 
 
 @pytest.mark.parametrize("prefix,new", [([3300] * 32, [1] * 32), ([3000, 2000, 3001], [1, 1, 1]), ([2048] * 3, [50] * 3)])
@@ -525,6 +542,24 @@ def test_what_is_not_a_number_reaches_only_rows_that_see_it(prefix, new, heads, 
         clean |= ~hit
     assert (np.abs(got - want)[clean] <= (2.0 ** -7 * (size + np.abs(want)) + 1e-4)[clean]).all()
     assert not np.isnan(_f64(lse)[:at]).any() and np.isnan(_f64(lse)[at:, G]).all() == (bad == "k")
+
+
+@pytest.mark.parametrize("bad", ["v", "k"])
+def test_what_is_not_a_number_among_few_rows_of_many(bad):
+    """Several new tokens in one pass of two accumulators: those before the slot, and the other requests, keep their bits."""
+    b = Batch([300, 40, 500, 31, 64], [4, 4, 2, 1, 4], seed=26).fill_contexts()
+    b.to_device()
+    q = b.queries()
+    clean, clean_lse = b.attend(q)
+    page, place = b.slots(1, 42, 1)                          # token 2 of request 1, rows 6 and 7
+    b.pools[bad][int(page[0]), 2, int(place[0]), 9] = 0x7F
+    got, lse = b.attend(q)
+    hit = torch.zeros_like(clean, dtype=torch.bool)
+    hit[6:8, 14:21, 9:10] = True
+    if bad == "k":
+        hit[6:8, 14:21] = True
+    assert torch.equal(torch.isnan(got), hit) and torch.equal(got[~hit.any(-1)], clean[~hit.any(-1)])
+    assert torch.equal(torch.isnan(lse), hit.all(-1)) and torch.equal(lse[~hit.any(-1)], clean_lse[~hit.any(-1)])
 
 
 def test_a_row_of_q_that_is_not_a_number_stays_alone():
