@@ -15,6 +15,12 @@
 // tile's weights sum to more than 2^20: any reference gives the same result, and the sum, which is taken before
 // the weights are used, tells in time.  So the loop takes no maxima.  Row sums are of the weights before they are
 // rounded (of the rounded ones they would be off by up to 2^-9 where few keys count).
+//
+// Measured (28 query heads over 4 KV heads): two chunks of 2048 behind 16384 890 to 960 us on different cards, 1070 to 1150 TFLOP/s, where
+// a large bf16 matrix product reaches 1346; the matrix units are busy 61 % of the cycles, at 1.9 of 2.4 GHz: it is the power that ends
+// there (a last round spread evenly over all compute units in place of three quarters of them took as long).  Eight chunks of 128 to
+// 512 behind an image 65.3 us, of which 6 are the merge; 36 tokens behind 16384 28.2 us: 64 pieces, four tiles each, of which four are
+// what a piece costs before its first tile (lengths, pages, rows of q, tiles: dependent trips), 8.5 the records' way through memory.
 #include <algorithm>
 #include <type_traits>
 
@@ -34,10 +40,11 @@ constexpr int NW = 8;                                    // waves of a workgroup
 constexpr int BR = 32 * NW;                              // rows of a unit
 constexpr int BC = 64;                                   // keys of a tile
 constexpr int PLACES = 256;                              // workgroups that run at once: one on each compute unit
-constexpr int MAX_PARTS = 128;                           // pieces of a unit
-constexpr int MIN_TILES_ALONE = 2, MIN_TILES_BEHIND = 4;    // key tiles of a piece where no unit is whole, and behind whole ones
+constexpr int MAX_PARTS = 128;                           // pieces of a unit (one unit of 30 k keys 24.3 us; 64: 26.0, 256: 28.4)
+constexpr int MIN_TILES_ALONE = 2, MIN_TILES_BEHIND = 4;    // key tiles of a piece where no unit is whole (16 units of 1000 keys 18.8 us; 3: 19.2, 4: 20.0), and
+                                                            // behind whole ones (8 images' chunks 65.3; 2: 67.1, 8: 68.6)
 constexpr float LAG_LIMIT = 1048576.f;                   // 2^20
-constexpr int QK_OPS = 80;                               // of a tile's 119 softmax instructions beside the score products
+constexpr int QK_OPS = 80;                               // of a tile's 119 softmax instructions beside the score products (72, 88: 1 % slower; at least 63)
 
 // LDS
 constexpr int TILE = BC * HEAD_DIM * 2, RAW_TILE = BC * HEAD_DIM;
@@ -232,8 +239,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     auto store_k = [&](const uint4& codes, int scale, int slot) {
         const float s = up_scale(scale);
         auto half = [&](uint32_t w0, uint32_t w1) -> uint4 {
-            return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, true)),
-                              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true)));
+            auto pair = [&](uint32_t w, auto upper) -> uint32_t { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, decltype(upper)::value)); };
+            return make_uint4(pair(w0, std::false_type{}), pair(w0, std::true_type{}), pair(w1, std::false_type{}), pair(w1, std::true_type{}));
         };
         *(uint4*)(smem + slot * TILE + k_wr) = half(codes.x, codes.y);
         *(uint4*)(smem + slot * TILE + (k_wr ^ 16)) = half(codes.z, codes.w);
@@ -617,7 +624,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     }
 }
 
-// The pieces of the units that were cut.  A piece of work is 32 rows of a unit (a wave's) and 4 GROUPS channels of each half of
+// The pieces of the units that were cut; bound by their records, 128 KB a piece (33 MB of 256 pieces: 8.5 us).  A piece of work is 32 rows of a unit (a wave's) and 4 GROUPS channels of each half of
 // the lanes; a workgroup's waves take the unit's records in turn, AT_ONCE of them on the way, and are added up through LDS.
 template <bool CAUSAL, int GROUPS, int AT_ONCE>
 __global__ __launch_bounds__(64 * TEAMS) void attn_fp8_merge_tiles_kernel(AttnFp8Args a, Layout L)
