@@ -9,6 +9,9 @@
 // (sums, reference, unnormalised rows) of its first and of its last pair at most, and a second kernel adds the
 // records of a pair up.  Inside a workgroup the four waves take a pair's tiles in turn, straight from global memory to
 // registers, and meet in LDS at the end of the pair.
+// Small calls are bound by the trips through memory that follow each other, and finding the part is one of them.  Where the page table says
+// that they are small, every pair has the same number of parts, of the same number of tiles: page ids, and the merge's records, then
+// travel with the lengths, and pairs of one part need no merge.
 //
 // Scores, S^T = K Q^T: a lane has 32 channels of a key, which v_cvt_scalef32_pk_bf16_fp8 makes bf16 in the key's scale (exact)
 // for four v_mfma_f32_16x16x32_bf16, and the same 32 channels of its row of q.
@@ -19,8 +22,8 @@
 //
 // Measured (28 query heads over 4 KV heads unless said): 64 contexts of 8192 96 us with the records' merge, 5.6 TB/s of the cache's
 // bytes, 91 without it; 32 contexts of 300 to 4600 with 32 over 8 heads 41.5 us, 4.1 TB/s (a request with little to do at its end
-// has its record, its merge and its start like any other: 36 us of the main kernel, of which 26 are bytes); one of 1500 10.8 us, of
-// which 7 are three dependent trips (lengths, pages, rows), a tile and a record, and 4 the second launch.
+// has its record, its merge and its start like any other: 36 us of the main kernel, of which 26 are bytes).  In fixed parts one of 1500
+// 7.5 us, of which an empty launch after the other would be 3.4, one of 60 4.5, 32 of 200 5.9, 8 of 2000 10.1, one of 16000 12.0.
 #include <algorithm>
 #include <type_traits>
 
@@ -39,6 +42,10 @@ constexpr int TILE = 32;                                 // keys per step of a w
 constexpr int ROWS = 16;
 constexpr int OUT_STRIDE = D + 8;                        // bf16 values between output rows in LDS
 constexpr int LEAST_TILES = WAVES;                       // of a part: one for each wave
+// Fixed parts, where the page table holds at most so many tiles for each of the workgroups (16 contexts of 300 to 8000 22.6 us, and 24.4 as
+// a line; 32 of 2000 19.0 and 21.4; one of 1500 7.6 and 10.8; of the next size, 48 of 400 to 4000, 35.5 and 25.5)
+constexpr int FIXED_TILES = 32;
+constexpr int WHOLE_TILES = 16;                          // of a pair that one workgroup does (32 of 500 10.6 us, in two parts 14.5; one of 1000 10.5 where two parts take 8.4)
 constexpr int WORKGROUPS = 512;                          // two on each compute unit (256 of twice the waves: ragged 49 us in place of 42)
 constexpr int ALONE = 256;                               // so many parts have a compute unit to themselves
 constexpr int MANY_RECORDS = 16;                         // of a pair: then 1024 threads merge (one of 16000 14.4 us, and 16.5 with 256; ragged 41.9, 48.2 with 1024)
@@ -53,7 +60,8 @@ __device__ inline float row_sum(float x) { return sum32(sum16(x)); }
 // how the batch's tiles are dealt
 struct RowsLayout {
     int G, workgroups;
-    Divisor by_G, by_kv_heads, by_workgroups;
+    int parts, part_tiles;                               // fixed: workgroups of a pair, and their tiles; else 0
+    Divisor by_G, by_kv_heads, by_workgroups, by_parts;
 };
 
 // a request's rows and keys, and where its tiles lie in the line (of one KV head; heads follow each other)
@@ -121,8 +129,8 @@ struct Line {
     }
 };
 
-// Tiles of a part: equal shares for all workgroups, but not too short ones.  (Parts of four tiles where each has a compute unit to itself, of eight
-// at least else: one context of 1500 tokens 11.4 us with 4 and 12.4 with 8, 8 of 2000 15.0 and 13.6, one of 16000 17.6 and 15.0.)
+// Tiles of a part of the line: equal shares for all workgroups, but not too short ones.  (Parts of four tiles where each has a compute unit to itself,
+// of eight at least else: as a line, one context of 1500 tokens 11.4 us with 4 and 12.4 with 8, 8 of 2000 15.0 and 13.6, one of 16000 17.6 and 15.0.)
 __device__ inline int part_tiles(const RowsLayout& L, int all)
 {
     return max(all <= LEAST_TILES * ALONE ? LEAST_TILES : 2 * LEAST_TILES, L.by_workgroups.quotient(all - 1) + 1);
@@ -133,6 +141,21 @@ __device__ inline int small_quotient(int x, int d)
     const int q = __builtin_amdgcn_readfirstlane((int)((float)x * __builtin_amdgcn_rcpf((float)d)));
     const int rest = x - q * d;
     return rest < 0 ? q - 1 : rest >= d ? q + 1 : q;
+}
+
+// a fixed deal's request: its lengths travel with the page ids
+template <bool CAUSAL>
+__device__ inline Request request_of(const BatchView& b, int r)
+{
+    const int n = b.new_lens[r], p = b.prefix_lens[r], cu = b.cu_new_lens[r];
+    Request q;
+    q.r = r;
+    q.N = clamp_new_len(b, n, CAUSAL);
+    q.P = clamp_prefix_len(b, p, CAUSAL ? q.N : 0);
+    q.first_row = clamp_first_row(b, cu, q.N);
+    q.tiles = q.N > 0 ? max(((CAUSAL ? q.P + q.N : q.P) + TILE - 1) / TILE, 1) : 0;
+    q.before = 0;
+    return q;
 }
 
 // a row's place among the packed (token, head) rows
@@ -162,18 +185,20 @@ struct Segment {
     int kvh, t0, t1, n_rows, ctx;
 };
 
-template <bool CAUSAL, int RT>
+struct NoLine { int total; };                            // in its place where parts are fixed
+
+template <bool CAUSAL, int RT, bool FIXED>
 __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Args a, RowsLayout L)
 {
     const BatchView& b = a.b;
     __shared__ f32x4 part_o[WAVES][ROWS * D / 4];
     __shared__ f32x2 part_ml[WAVES][ROWS];
-    Line<CAUSAL> line(b);
+    auto line = [&] { if constexpr (FIXED) return NoLine{1}; else return Line<CAUSAL>(b); }();
     const int all = line.total * b.num_kv_heads;
     if (all == 0) return;
-    const int share = part_tiles(L, all);
-    int x = (int)min((long long)blockIdx.x * share, (long long)all);
-    const int x_end = x + min(share, all - x);
+    const int share = FIXED ? L.part_tiles : part_tiles(L, all);
+    int x = FIXED ? 0 : (int)min((long long)blockIdx.x * share, (long long)all);
+    const int x_end = FIXED ? 1 : x + min(share, all - x);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int n16 = lane & 15, g = lane >> 4;
     const float c = b.softmax_scale * LOG2E;
@@ -182,27 +207,37 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Arg
     auto next_segment = [&]() -> Segment {
         Segment s = {};
         if (x >= x_end) return s;
-        s.rq = line.holding(L.by_kv_heads.quotient(x));
-        const int off = x - s.rq.before * b.num_kv_heads;
-        if (off < 0 || s.rq.tiles <= 0) return s;                        // (lengths that change meanwhile)
-        s.kvh = min(small_quotient(off, s.rq.tiles), b.num_kv_heads - 1);
-        s.t0 = off - s.kvh * s.rq.tiles;
-        s.t1 = max(min(s.rq.tiles, s.t0 + (x_end - x)), s.t0);
+        if constexpr (FIXED) {
+            const int pair = L.by_parts.quotient(blockIdx.x), r = L.by_kv_heads.quotient(pair);
+            s.rq = request_of<CAUSAL>(b, r);
+            s.kvh = pair - r * b.num_kv_heads;
+            s.t0 = min((int)(blockIdx.x - pair * L.parts) * share, s.rq.tiles);
+            s.t1 = min(s.t0 + share, s.rq.tiles);
+            x = x_end;
+        } else {
+            s.rq = line.holding(L.by_kv_heads.quotient(x));
+            const int off = x - s.rq.before * b.num_kv_heads;
+            if (off < 0 || s.rq.tiles <= 0) return s;                    // (lengths that change meanwhile)
+            s.kvh = min(small_quotient(off, s.rq.tiles), b.num_kv_heads - 1);
+            s.t0 = off - s.kvh * s.rq.tiles;
+            s.t1 = max(min(s.rq.tiles, s.t0 + (x_end - x)), s.t0);
+            x += s.t1 - s.t0;
+        }
         s.n_rows = min(s.rq.N * L.G, RT * ROWS);
         s.ctx = CAUSAL ? s.rq.P + s.rq.N : s.rq.P;                       // slots that hold tokens
-        x += s.t1 - s.t0;
         return s;
     };
     // lane 2 j + k: block k of the wave's j-th tile from `from` on, in 16-key blocks of the pool
-    auto ask_ids = [&](const Segment& s, int from) -> int {
-        const int blk = min(2 * (from + WAVES * (lane >> 1)) + (lane & 1), max(((s.ctx + 15) >> 4) - 1, 0));
-        const int page = min(max(b.page_table[(long long)s.rq.r * b.max_pages + (blk >> b.page_shift)], 0), b.num_pages - 1);
-        return ((page * b.num_kv_heads + s.kvh) << b.page_shift) + (blk & ((1 << b.page_shift) - 1));
+    auto ids_of = [&](int r, int kvh, int from, int last) -> int {
+        const int blk = min(2 * (from + WAVES * (lane >> 1)) + (lane & 1), last);
+        const int page = min(max(b.page_table[(long long)r * b.max_pages + (blk >> b.page_shift)], 0), b.num_pages - 1);
+        return ((page * b.num_kv_heads + kvh) << b.page_shift) + (blk & ((1 << b.page_shift) - 1));
     };
+    auto ask_ids = [&](const Segment& s, int from) -> int { return ids_of(s.rq.r, s.kvh, from, max(((s.ctx + 15) >> 4) - 1, 0)); };
     // Are K and V of the segment to go past the caches?  Not where all of a call fits them, nor where another request holds the same
     // pages: what the first brings in serves the others.
     auto streamed = [&](const Segment& s) -> bool {
-        if (all < STREAM_TILES || s.t0 >= s.t1) return false;
+        if (FIXED || all < STREAM_TILES || s.t0 >= s.t1) return false;
         const int entry = min((2 * s.t0) >> b.page_shift, b.max_pages - 1);
         const int mine = b.page_table[(long long)s.rq.r * b.max_pages + entry];
         bool shared = false;
@@ -254,9 +289,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Arg
 
     constexpr bool AHEAD = RT == 1;                                      // one tile is computed, one travels (32 rows leave no registers for that)
     Tile even, odd;
+    int ids = 0;
+    if constexpr (FIXED) {                                               // (they need no lengths: what is behind the context is masked)
+        const int pair = L.by_parts.quotient(blockIdx.x), r = L.by_kv_heads.quotient(pair);
+        ids = ids_of(r, pair - r * b.num_kv_heads, (int)(blockIdx.x - pair * L.parts) * share + wave, (b.max_pages << b.page_shift) - 1);
+    }
     Segment now = next_segment();
     if (now.t0 >= now.t1) return;
-    int ids = ask_ids(now, now.t0 + wave);
+    if constexpr (!FIXED) ids = ask_ids(now, now.t0 + wave);
     uint32_t pairs[RT][16];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) ask_q(now, rt, pairs[rt]);
@@ -437,7 +477,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Arg
         // The waves' parts, 16 rows at a time, in the order of the accumulators: four of them, channels 32 g + 8 k + i for k = 0 .. 3, are
         // the 16 bytes at place i * 64 + lane.  A thread adds up SUMS places, its own and those that far behind.
         const bool whole = now.t0 == 0 && now.t1 == now.rq.tiles;
-        float* rec = (float*)a.workspace + (2ll * blockIdx.x + (first_segment ? 0 : 1)) * RECORD_FLOATS<RT>;
+        float* rec = (float*)a.workspace + (FIXED ? (long long)blockIdx.x : 2ll * blockIdx.x + (first_segment ? 0 : 1)) * RECORD_FLOATS<RT>;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             if (rt * ROWS >= now.n_rows) break;                          // (the same for all waves)
@@ -501,30 +541,51 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Arg
 // 128 threads of it a record at a time.  4 to 5 us, of which 1.7 are any launch's and 1.5 the lengths.  (The last workgroup of a pair
 // merging in the first kernel saves that where parts are long and costs two trips through memory where they are not: 64 of 8192 94 us,
 // but one of 1500 16, ragged 45.)
-template <bool CAUSAL, int RT, int THREADS>
+template <bool CAUSAL, int RT, int THREADS, bool FIXED>
 __global__ __launch_bounds__(THREADS) void attn_fp8_merge_rows_kernel(AttnFp8Args a, RowsLayout L)
 {
     constexpr int TEAMS = THREADS / 128, AT_ONCE = 8;
     const BatchView& b = a.b;
     const int g = blockIdx.x & 3, rt = RT == 1 ? 0 : (blockIdx.x >> 2) & 1, pair = blockIdx.x >> (RT == 1 ? 2 : 3);
     const int r = L.by_kv_heads.quotient(pair), kvh = pair - r * b.num_kv_heads;
-    Line<CAUSAL> line(b);
-    const int all = line.total * b.num_kv_heads;
-    if (all == 0) return;
-    const int share = part_tiles(L, all);
-    const Request rq = line.request(r);
+    const int team = threadIdx.x >> 7, in_team = threadIdx.x & 127, i = in_team >> 4, n16 = threadIdx.x & 15;
+    const int ml_at = RT * ROWS * D + 2 * (rt * ROWS + n16), v_at = (rt * 512 + i * 64 + 16 * g + n16) * 4;
+    f32x4 v[AT_ONCE];
+    f32x2 ml[AT_ONCE];
+    auto fetch_record = [&](int u, long long at) {
+        const float* rec = (const float*)a.workspace + at * RECORD_FLOATS<RT>;
+        v[u] = *(const f32x4*)(rec + v_at);
+        ml[u] = *(const f32x2*)(rec + ml_at);
+    };
+    if constexpr (FIXED) {                                               // the first of the records that there could be travel with the lengths
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) fetch_record(u, (long long)pair * L.parts + min(team + TEAMS * u, L.parts - 1));
+        asm volatile("" ::: "memory");
+    }
+    Request rq;
+    int w0, w1, odd = 0;                                                 // odd: the pair begins inside w0's part
+    if constexpr (FIXED) {
+        rq = request_of<CAUSAL>(b, r);
+        w0 = pair * L.parts;
+        w1 = w0 + small_quotient(max(rq.tiles - 1, 0), L.part_tiles);
+    } else {
+        Line<CAUSAL> line(b);
+        const int all = line.total * b.num_kv_heads;
+        if (all == 0) return;
+        const int share = part_tiles(L, all);
+        rq = line.request(r);
+        const int x = rq.before * b.num_kv_heads + kvh * rq.tiles;
+        w0 = small_quotient(x, share);
+        w1 = small_quotient(x + rq.tiles - 1, share);
+        odd = x != w0 * share ? 1 : 0;
+    }
     const int n_rows = min(rq.N * L.G, RT * ROWS);
-    if (rt * ROWS >= n_rows || rq.tiles == 0) return;
-    const int x = rq.before * b.num_kv_heads + kvh * rq.tiles;
-    const int w0 = small_quotient(x, share), w1 = small_quotient(x + rq.tiles - 1, share);
-    if (w0 == w1) return;                                                // done where it was
+    if (rt * ROWS >= n_rows || rq.tiles == 0 || w0 == w1) return;        // (one: done where it was)
     __shared__ f32x4 part[TEAMS][128];
     __shared__ f32x2 part_ml[TEAMS][ROWS];
     __shared__ __bf16 rows[ROWS][40];
-    const int team = threadIdx.x >> 7, in_team = threadIdx.x & 127, i = in_team >> 4, n16 = threadIdx.x & 15;
     // the first workgroup's record is its last pair's, unless the pair is where its part begins; of the others it is the first
-    auto record = [&](int w) { return (const float*)a.workspace + (2ll * w + (w == w0 && x != w0 * share ? 1 : 0)) * RECORD_FLOATS<RT>; };
-    const int ml_at = RT * ROWS * D + 2 * (rt * ROWS + n16), v_at = (rt * 512 + i * 64 + 16 * g + n16) * 4;
+    auto record = [&](int w) { return FIXED ? (long long)w : 2ll * w + (w == w0 ? odd : 0); };
     float top = -INFINITY, sum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     // what there is in terms of a larger reference, and more of it
@@ -542,14 +603,9 @@ __global__ __launch_bounds__(THREADS) void attn_fp8_merge_rows_kernel(AttnFp8Arg
         for (int k = 0; k < 4; ++k) acc[k] = fmaf(v[k], f, acc[k]);
     };
     for (int from = w0 + team; from <= w1; from += TEAMS * AT_ONCE) {
-        f32x4 v[AT_ONCE];
-        f32x2 ml[AT_ONCE];
+        if (!FIXED || from != w0 + team)
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            const float* rec = record(min(from + TEAMS * u, w1));
-            v[u] = *(const f32x4*)(rec + v_at);
-            ml[u] = *(const f32x2*)(rec + ml_at);
-        }
+            for (int u = 0; u < AT_ONCE; ++u) fetch_record(u, record(min(from + TEAMS * u, w1)));
         float most = top;
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u)
@@ -595,22 +651,43 @@ RowsLayout layout_of(const BatchView& b)
     L.by_kv_heads = divisor_of(b.num_kv_heads);
     // no more workgroups than the page table can hold work for
     L.workgroups = (int)std::max<long long>(std::min<long long>(WORKGROUPS, (line_of(b) + LEAST_TILES - 1) / LEAST_TILES), 1);
+    L.parts = L.part_tiles = 0;
+    const long long pairs = (long long)b.num_reqs * b.num_kv_heads, most = line_of(b) / pairs;    // tiles of a pair
+    if (rows_of(b) <= ROWS && pairs <= WORKGROUPS && line_of(b) <= (long long)WORKGROUPS * FIXED_TILES) {
+        const long long per_pair = WORKGROUPS / pairs;                   // workgroups that a pair may have
+        // (short parts only where a merge has few of them: one of 16000 12.0 us in parts of 8 tiles, and 13.8 of 4; of 1500 8.7 and 7.5)
+        const int least = most <= WHOLE_TILES ? WHOLE_TILES : most <= MANY_RECORDS * LEAST_TILES ? LEAST_TILES : 2 * LEAST_TILES;
+        L.part_tiles = (int)std::max<long long>(least, (most + per_pair - 1) / per_pair);
+        L.parts = (int)std::max<long long>((most + L.part_tiles - 1) / L.part_tiles, 1);
+        L.workgroups = (int)pairs * L.parts;
+    }
+    L.by_parts = divisor_of(std::max(L.parts, 1));
     L.by_workgroups = divisor_of(L.workgroups);
     return L;
 }
-size_t rows_workspace_bytes(const BatchView& b) { return 2 * (size_t)layout_of(b).workgroups * (rows_of(b) <= ROWS ? RECORD_FLOATS<1> : RECORD_FLOATS<2>) * sizeof(float); }
-
-template <bool CAUSAL, int RT>
-hipError_t launch_rows(const AttnFp8Args& a, hipStream_t stream)
+size_t rows_workspace_bytes(const BatchView& b)
 {
-    const RowsLayout L = layout_of(a.b);
-    hipLaunchKernelGGL((attn_fp8_rows_kernel<CAUSAL, RT>), dim3(L.workgroups), dim3(64 * WAVES), 0, stream, a, L);
+    const RowsLayout L = layout_of(b);
+    return (L.parts == 1 ? 0 : L.parts > 0 ? 1 : 2) * (size_t)L.workgroups * (rows_of(b) <= ROWS ? RECORD_FLOATS<1> : RECORD_FLOATS<2>) * sizeof(float);
+}
+
+template <bool CAUSAL, int RT, bool FIXED>
+hipError_t launch_rows(const AttnFp8Args& a, const RowsLayout& L, hipStream_t stream)
+{
+    hipLaunchKernelGGL((attn_fp8_rows_kernel<CAUSAL, RT, FIXED>), dim3(L.workgroups), dim3(64 * WAVES), 0, stream, a, L);
     // few pairs have many records each: more of them at a time
     const long long pairs = (long long)a.b.num_reqs * a.b.num_kv_heads;
     const dim3 grid((unsigned)(pairs * 4 * RT));
-    if (L.workgroups > MANY_RECORDS * pairs) hipLaunchKernelGGL((attn_fp8_merge_rows_kernel<CAUSAL, RT, 1024>), grid, dim3(1024), 0, stream, a, L);
-    else if (L.workgroups > 1) hipLaunchKernelGGL((attn_fp8_merge_rows_kernel<CAUSAL, RT, 256>), grid, dim3(256), 0, stream, a, L);
+    if (L.workgroups > MANY_RECORDS * pairs) hipLaunchKernelGGL((attn_fp8_merge_rows_kernel<CAUSAL, RT, 1024, FIXED>), grid, dim3(1024), 0, stream, a, L);
+    else if (FIXED ? L.parts > 1 : L.workgroups > 1) hipLaunchKernelGGL((attn_fp8_merge_rows_kernel<CAUSAL, RT, 256, FIXED>), grid, dim3(256), 0, stream, a, L);
     return hipGetLastError();
+}
+template <bool CAUSAL>
+hipError_t launch_few(const AttnFp8Args& a, hipStream_t stream)
+{
+    const RowsLayout L = layout_of(a.b);
+    if (rows_of(a.b) > ROWS) return launch_rows<CAUSAL, 2, false>(a, L, stream);
+    return L.parts > 0 ? launch_rows<CAUSAL, 1, true>(a, L, stream) : launch_rows<CAUSAL, 1, false>(a, L, stream);
 }
 
 }  // namespace
@@ -636,8 +713,7 @@ size_t attn_fp8_workspace_bytes(const BatchView& b)
 hipError_t launch_attn_fp8(const AttnFp8Args& a, bool causal, hipStream_t stream)
 {
     if (!few_rows(a.b)) return launch_attn_fp8_tiles(a, causal, stream);
-    if (rows_of(a.b) <= ROWS) return causal ? launch_rows<true, 1>(a, stream) : launch_rows<false, 1>(a, stream);
-    return causal ? launch_rows<true, 2>(a, stream) : launch_rows<false, 2>(a, stream);
+    return causal ? launch_few<true>(a, stream) : launch_few<false>(a, stream);
 }
 
 }  // namespace emm

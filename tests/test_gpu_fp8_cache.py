@@ -376,6 +376,9 @@ ATTENTION_CASES = {
     "decode_many": dict(prefix=list(range(3, 300, 3)), new=[1] * 99, heads=8, kv_heads=2),
     "decode_long": dict(prefix=[20000, 3, 9000], new=[1, 1, 1]),
     "decode_wide_table": dict(prefix=[900, 77], new=[1, 1], wider=4000),
+    "decode_wider_table": dict(prefix=[900, 77, 0, 2500, 31], new=[1, 1, 1, 1, 0], wider=12000),
+    "decode_wider_table_cross": dict(prefix=[900, 77, 0, 2500, 31], new=[1, 1, 1, 1, 0], wider=12000, causal=False),
+    "decode_whole_pairs": dict(prefix=[511, 0, 31, 32, 255, 500], new=[1, 1, 1, 1, 0, 1]),
     "decode_20_heads_a_group_more": dict(prefix=[127, 1023, 0, 31, 32, 5, 64, 700, 96, 2], new=[1] * 10, heads=40, kv_heads=2),
     "few_rows_of_many": dict(prefix=[1000, 0, 63, 31, 200], new=[2, 3, 4, 1, 4]),
     "few_rows_of_many_cross": dict(prefix=[1000, 0, 63, 31, 200], new=[2, 3, 4, 0, 4], causal=False),
