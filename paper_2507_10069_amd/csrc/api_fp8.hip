@@ -2,7 +2,7 @@
 // All checks that can fail run before the first HIP call.
 #include "../../include/emm_fp8.h"
 #include "api_checks.h"
-#include "emm_internal.h"
+#include "fp8_internal.h"
 
 #include <algorithm>
 #include <cmath>

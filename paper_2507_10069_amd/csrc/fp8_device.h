@@ -1,7 +1,7 @@
 // The 8-bit cache's format on the device (see include/emm_fp8.h), and where a packed token's slot is.
 #pragma once
 
-#include "emm_internal.h"
+#include "fp8_internal.h"
 
 namespace emm {
 namespace fp8 {
