@@ -3,10 +3,11 @@
 // Bound by the matrix pipe and the instructions around it.  Rows are (new token, query head of a KV group) pairs of one
 // (request, KV head), token-major; a workgroup of 8 waves takes 256 of them (a unit), a wave 32, and streams the keys
 // in tiles of 64, each fetched once for the workgroup:
-// K and V go to LDS as they are (K three tiles ahead, V two), and from there through the wave that fetched them, which makes them
-// bf16 in their keys' scales (exact) and puts them into rings of two tiles, in 16-byte chunks placed so that no read or write of
-// them meets a bank twice.  Scale bytes travel with them, K's a tile earlier: a wave brings those of other waves' rows, and K is
-// converted before the barrier that V waits for.  (Each wave converting what it needs of K in its registers takes 64 conversions
+// K and V go to LDS as they are (K three tiles ahead, V two), and from there through the wave that fetched them, which makes
+// them bf16 in their keys' scales (exact) and puts them into rings of two tiles, in 16-byte chunks placed so that no read of
+// them meets a bank twice.  (The stores do, 8 % of the cycles; storing the halves the other way round in every second four lanes
+// ends that and changes no time.)  Scale bytes travel with them, K's a tile earlier: a wave brings those of other waves' rows, and K
+// is converted before the barrier that V waits for.  (Each wave converting what it needs of K in its registers takes 64 conversions
 // a tile in place of 8: two chunks of 2048 behind 16 k 923 us, so 900.)
 // S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_32x32x16_bf16.  A lane has one row and 32 of a tile's keys; K's rows lie in
 // LDS such that its weights, rounded to bf16, are the second product's operand as they are, and which channels a step of the first
@@ -14,7 +15,7 @@
 // Weights are exp2(S c - m) with a reference m that is the row's maximum over its first tile, and follows only where a
 // tile's weights sum to more than 2^20: any reference gives the same result, and the sum, which is taken before
 // the weights are used, tells in time.  So the loop takes no maxima.  Row sums are of the weights before they are
-// rounded (of the rounded ones they would be off by up to 2^-9 where few keys count).
+// rounded (of the rounded ones, and lse with them, they would be off by up to 2^-8 where few keys count).
 //
 // Measured (28 query heads over 4 KV heads): two chunks of 2048 behind 16384 890 to 960 us on different cards, 1070 to 1150 TFLOP/s, where
 // a large bf16 matrix product reaches 1346; the matrix units are busy 61 % of the cycles, at 1.9 of 2.4 GHz: it is the power that ends
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     // ---- V to bf16: 16 channels of a key per lane.  Keys behind the context hold anything: zeros in their place.  In tiles that not every
     //      row sees whole, a NaN would reach rows that do not see it (0 * NaN): it becomes a zero too, and flags say that there was one.
     const int v_key = 8 * wave + (lane >> 3);
-    // V tile: chunk c of 16 bytes of key k lies at place c ^ 4 (k mod 4) ^ (k mod 2): neither the transposing reads nor these stores meet a bank twice
+    // V tile: chunk c of 16 bytes of key k lies at place c ^ 4 (k mod 4) ^ (k mod 2): the transposing reads meet no bank twice
     const int v_wr = V_AT + v_key * 256 + (((2 * (lane & 7)) ^ ((v_key & 3) << 2) ^ (v_key & 1)) << 4);
     uint4 raw;
     int raw_scale;
