@@ -661,6 +661,43 @@ def test_a_step_captured_and_replayed():
             assert torch.equal(replayed, out) and torch.equal(replayed_lse, lse), i
 
 
+@pytest.mark.parametrize("wider", [0, 12000])
+def test_a_captured_step_follows_the_lengths(wider):
+    """A decode step and a chunk are captured once; lengths, pages and padding change between the replays."""
+    for most, heads, new_of in ((1, 28, lambda rng: [1, 1, 0, 1]), (40, 28, lambda rng: rng.integers(0, 41, 4).tolist())):
+        rng = np.random.default_rng(27)
+        b = Batch([3000] * 4, [most] * 4, heads=heads, seed=27, wider=wider).fill_contexts()
+        b.to_device()
+        q, out, lse = b.queries(), torch.empty((b.rows, heads, 128), dtype=torch.bfloat16, device=DEV), torch.empty((b.rows, heads), device=DEV)
+        ws = torch.empty(max(16, B.emm_attn_fp8_workspace_size(b.batch)), dtype=torch.uint8, device=DEV)
+
+        def step():
+            b.attend(q, out=out, lse=lse, workspace=ws)
+        step()
+        torch.cuda.synchronize()
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        for i in range(4):
+            b.prefix[:] = [[0, 17, 2999, 512], [1, 511, 64, 3000], [700, 31, 32, 33], [1500, 1500, 0, 0]][i]
+            b.new[:] = new_of(rng)
+            b.cu[:] = np.concatenate([[0], np.cumsum(b.new)])
+            b.table[:] = b.table[rng.permutation(4)]
+            for n, x in (("prefix", b.prefix), ("new", b.new), ("cu", b.cu), ("table", b.table)):
+                b.dev[n].copy_(torch.from_numpy(x))
+            b.T = int(b.cu[-1])
+            out.fill_(7), lse.fill_(7), ws.fill_(0xA5)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert (out[b.T:] == 7).all() and (lse[b.T:] == 7).all()
+            b.compare(q, out, lse, sorted(set(rng.integers(0, b.T, 12).tolist())))
+            replayed = out.clone()
+            out.fill_(7)
+            step()
+            torch.cuda.synchronize()
+            assert torch.equal(out, replayed), i
+
+
 # ---- together, as they would be used --------------------------------------------------------------------------------
 
 def test_serving_loop_over_the_prefix_cache():
