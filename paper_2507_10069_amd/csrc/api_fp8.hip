@@ -9,6 +9,7 @@
 #include <cstdint>
 #include <initializer_list>
 
+using emm::MOST_SLOTS;
 using emm::api::aligned16;
 using emm::api::check_arrays;
 using emm::api::check_scalars;
@@ -16,7 +17,7 @@ using emm::api::view_of;
 
 namespace {
 
-constexpr int64_t MOST_TOKENS = int64_t(1) << 25, MOST_HEADS = 4096, MOST_ROWS = int64_t(1) << 30, MOST_SLOTS = int64_t(1) << 30, MOST_PAIRS = int64_t(1) << 20;
+constexpr int64_t MOST_TOKENS = int64_t(1) << 25, MOST_HEADS = 4096, MOST_ROWS = int64_t(1) << 30, MOST_PAIRS = int64_t(1) << 20;
 
 // what the row kernels take: pages as everywhere, both dtypes, heads of 64 or 128, and numbers that their grids and indexes hold
 emm_status check_rows(const emm_batch* b)

@@ -138,6 +138,11 @@ struct Plan {
     }
 };
 
+// the first of a unit's key tiles that is piece `part`'s (part == pieces: behind the last); without a sign, since
+// MAX_PARTS times the tiles of the longest context is 2^31
+constexpr int piece_begin(int part, int n_tiles, int pieces) { return (int)((uint32_t)part * (uint32_t)n_tiles / (uint32_t)pieces); }
+static_assert(MAX_PARTS * (MOST_SLOTS / BC) < 1ll << 32 && piece_begin(MAX_PARTS, MOST_SLOTS / BC, MAX_PARTS) == MOST_SLOTS / BC, "a piece's end holds in 32 bits");
+
 // a unit's rows and keys
 struct Extent {
     int N, P, first_row, ctx, n_rows, row0, kv_len, n_tiles, pieces;
@@ -187,7 +192,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
     if (u.req < 0) return;
     const Extent e = extent_of<CAUSAL>(b, L, u, L.units_max <= PLACES);
     if (e.row0 >= e.n_rows || u.part >= e.pieces) return;
-    const int t_begin = u.part * e.n_tiles / e.pieces, n_tiles = (u.part + 1) * e.n_tiles / e.pieces - t_begin;
+    const int t_begin = piece_begin(u.part, e.n_tiles, e.pieces), n_tiles = piece_begin(u.part + 1, e.n_tiles, e.pieces) - t_begin;
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int l32 = lane & 31, h32 = lane >> 5;

@@ -5,6 +5,8 @@
 
 namespace emm {
 
+constexpr long long MOST_SLOTS = 1ll << 30;  // in a row of the page table, for the calls of emm_fp8.h and emm_rope
+
 // Rotary positions (see emm_rope_params): arrays of the device, ends[a] = frequencies of the axes up to a
 struct RopeView {
     const double* inv_freq;
