@@ -198,7 +198,8 @@ emm_status emm_rope(const emm_batch* b, const emm_rope_params* rope, const void*
     // (a pair that is not given has no row that the stride must hold)
     const int64_t sq = q != nullptr ? stride_of(b, b->num_q_heads, token_stride) : 0, sk = k != nullptr ? stride_of(b, b->num_kv_heads, token_stride) : 0;
     if (sq < 0 || sk < 0) return EMM_ERR_INVALID_ARG;
-    if (b->num_reqs == 0 || b->total_new_tokens == 0) return EMM_OK;
+    // (given positions belong to rows, whether or not a request has them)
+    if (b->total_new_tokens == 0 || (b->num_reqs == 0 && rope->num_axes == 0)) return EMM_OK;
     if (rope->num_axes == 0 && (st = check_arrays(b)) != EMM_OK) return st;
     if ((st = check_rope_arrays(rope)) != EMM_OK) return st;
     if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || (q == nullptr && k == nullptr)) return EMM_ERR_NULL;

@@ -1,0 +1,20 @@
+"""Rotary positions and the 8-bit cache without a GPU: what the entry points answer at the edges of their arguments."""
+import ctypes
+
+from paper_2507_10069_amd import binding as B
+from test_fp8_host import OK, _batch, _rope
+
+FAR = 0x1000000
+
+
+def test_given_positions_turn_rows_of_no_request():
+    """A batch without requests is no empty one where positions are given: its rows are looked at like any others."""
+    lib, b = B.load(), _batch(arrays=False, num_reqs=0, max_new_len=0)
+    given = ctypes.byref(_rope(num_axes=1, sections=(64, 0, 0, 0), positions=OK))
+    assert lib.emm_rope(b, given, None, None, 0, None, None, None) == B.EMM_ERR_NULL
+    assert lib.emm_rope(b, given, OK, None, 0, None, None, None) == B.EMM_ERR_NULL
+    assert lib.emm_rope(b, given, OK + 8, None, 0, FAR, None, None) == B.EMM_ERR_INVALID_ARG
+    missing = ctypes.byref(_rope(num_axes=1, sections=(64, 0, 0, 0)))
+    assert lib.emm_rope(b, missing, OK, None, 0, FAR, None, None) == B.EMM_ERR_NULL
+    # places in requests: without requests there are none
+    assert lib.emm_rope(b, ctypes.byref(_rope()), OK, None, 0, FAR, None, None) == B.EMM_OK
