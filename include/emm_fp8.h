@@ -47,7 +47,8 @@ emm_status emm_kv_scatter_fp8(const emm_batch *batch, const void *k_new, const v
 /*
  * emm_rope and emm_kv_scatter_fp8 in one launch, with the bits of the two: q is rotated into q_out (packed; may be q
  * where that is packed), k_new is rotated, rounded to the batch's dtype and quantised, v_new is quantised.
- * token_stride holds for q, k_new and v_new.
+ * token_stride holds for q, k_new and v_new.  As by emm_rope, q's rows of no request are turned where positions are
+ * given, and else left as they were.
  */
 emm_status emm_rope_kv_scatter_fp8(const emm_batch *batch, const emm_rope_params *rope, const void *q, const void *k_new,
                                    const void *v_new, int64_t token_stride, void *q_out, const emm_fp8_cache *cache,

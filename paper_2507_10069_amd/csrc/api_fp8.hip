@@ -125,7 +125,9 @@ emm_status scatter(const emm_batch* b, const emm_rope_params* rope, const void* 
     if (rope != nullptr && (st = check_rope(b, rope)) != EMM_OK) return st;
     const int64_t sq = rope != nullptr ? stride_of(b, b->num_q_heads, token_stride) : 0, skv = stride_of(b, b->num_kv_heads, token_stride);
     if (sq < 0 || skv < 0) return EMM_ERR_INVALID_ARG;
-    if (b->num_reqs == 0 || b->total_new_tokens == 0) return EMM_OK;
+    if (b->total_new_tokens == 0) return EMM_OK;
+    // (without requests nothing is written, but given positions turn q's rows all the same)
+    if (b->num_reqs == 0) return rope != nullptr && rope->num_axes > 0 ? emm_rope(b, rope, q, nullptr, token_stride, q_out, nullptr, hip_stream) : EMM_OK;
     if ((st = check_arrays(b)) != EMM_OK) return st;
     if (rope != nullptr && (st = check_rope_arrays(rope)) != EMM_OK) return st;
     if (k_new == nullptr || v_new == nullptr || (rope != nullptr && (q == nullptr || q_out == nullptr))) return EMM_ERR_NULL;

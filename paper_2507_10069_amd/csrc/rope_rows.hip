@@ -128,7 +128,7 @@ __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, Rope
     const bool from_batch = ROPE && rope.num_axes == 0;
     if (QUANT || from_batch) {
         place = place_of_token(b, t);
-        if (place.slot < 0) return;                      // a row of no request stays as it was
+        if (place.slot < 0 && (!ROPE || from_batch)) return;     // a row of no request stays as it was; with a given position its q is turned
     }
     if (QUANT) row0 = pool_row(b, place);
     if (ROPE && lane < rope.rotary_dim / 2) {

@@ -2,7 +2,7 @@
 import ctypes
 
 from paper_2507_10069_amd import binding as B
-from test_fp8_host import OK, _batch, _rope
+from test_fp8_host import OK, _batch, _cache, _rope
 
 FAR = 0x1000000
 
@@ -18,3 +18,13 @@ def test_given_positions_turn_rows_of_no_request():
     assert lib.emm_rope(b, missing, OK, None, 0, FAR, None, None) == B.EMM_ERR_NULL
     # places in requests: without requests there are none
     assert lib.emm_rope(b, ctypes.byref(_rope()), OK, None, 0, FAR, None, None) == B.EMM_OK
+
+
+def test_rotation_and_write_without_requests_is_the_rotation():
+    lib, b, c = B.load(), _batch(arrays=False, num_reqs=0, max_new_len=0), ctypes.byref(_cache())
+    given = ctypes.byref(_rope(num_axes=1, sections=(64, 0, 0, 0), positions=OK))
+    assert lib.emm_rope_kv_scatter_fp8(b, given, OK, OK, OK, 0, None, c, None) == B.EMM_ERR_NULL
+    assert lib.emm_rope_kv_scatter_fp8(b, given, OK, OK, OK, 0, FAR + 4, c, None) == B.EMM_ERR_INVALID_ARG
+    assert lib.emm_rope_kv_scatter_fp8(b, given, OK, OK, OK, 0, OK + 256, c, None) == B.EMM_ERR_INVALID_ARG
+    assert lib.emm_rope_kv_scatter_fp8(b, ctypes.byref(_rope()), OK, OK, OK, 0, FAR, c, None) == B.EMM_OK
+    assert lib.emm_kv_scatter_fp8(b, OK, OK, 0, c, None) == B.EMM_OK

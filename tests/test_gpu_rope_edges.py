@@ -6,7 +6,7 @@ import torch
 
 from oracle import fp8_model as F
 from paper_2507_10069_amd import binding as B
-from test_gpu_fp8_cache import DEV, _check_rotated, _dev, _f64
+from test_gpu_fp8_cache import DEV, Batch, _check_rotated, _dev, _f64
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +23,28 @@ def test_given_positions_turn_all_rows_without_requests():
     B.emm_rope(batch, rope, q, None, out, None)
     want = F.rotate(_f64(q), np.repeat(at[:, None], 32, 1), inv, 64, "half")
     _check_rotated(_f64(out), _f64(q), want, None, 64, "half", 1.0, "f32")
+
+
+@pytest.mark.parametrize("axes", [0, 1, 3])
+@pytest.mark.parametrize("requests", [True, False])
+def test_rotation_and_write_has_the_bits_of_the_two_calls_in_rows_of_no_request(axes, requests):
+    """A padded batch, and one that is nothing but padding: given positions turn those rows of q, places in requests leave them."""
+    print("case padded rotation and write", axes, requests, flush=True)
+    b = Batch([3, 100, 9], [4, 0, 30], heads=12, kv_heads=2, seed=axes, extra_rows=21)
+    if not requests:
+        b.batch.num_reqs = b.batch.max_new_len = 0
+    inv, _ = B.emm_rope_inv_freq_host(128, 1e6)
+    pos = _dev(b.rng.integers(0, 9000, (axes, b.rows)).astype(np.int32)) if axes else None
+    rope = B.make_rope(_dev(inv), rotary_dim=128, positions=pos, sections=[16, 24, 24] if axes == 3 else None)
+    q, k, v = (_dev(b.rng.standard_normal((b.rows, h, 128)).astype(np.float32), torch.bfloat16) for h in (12, 2, 2))
+    got, want, k_two = torch.full_like(q, 5.0), torch.full_like(q, 5.0), torch.full_like(k, 5.0)
+    B.emm_rope_kv_scatter_fp8(b.batch, rope, q, k, v, got, b.to_device())
+    fused = {n: t.clone() for n, t in b.pools.items()}
+    cache = b.to_device()
+    B.emm_rope(b.batch, rope, q, k, want, k_two)
+    B.emm_kv_scatter_fp8(b.batch, k_two, v, cache)
+    assert torch.equal(got, want)
+    for n, t in b.pools.items():
+        assert torch.equal(fused[n], t), n
+    turned = b.rows if axes else b.T if requests else 0
+    assert (got[turned:] == 5).all() and not (got[:turned] == 5).all(dim=-1).any()
