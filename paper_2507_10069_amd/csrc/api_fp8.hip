@@ -83,7 +83,9 @@ int64_t stride_of(const emm_batch* b, int64_t heads, int64_t token_stride)
 {
     const int64_t row = heads * b->head_dim;
     if (token_stride == 0) return row;
-    if (token_stride < row || token_stride > (int64_t(1) << 40) || token_stride * elt_bytes(b) % 16 != 0) return -1;
+    // (rows that span 2^60 bytes are in no memory, and what follows counts them in 64 bits)
+    if (token_stride < row || token_stride > (int64_t(1) << 60) / elt_bytes(b) / std::max(b->total_new_tokens, 1)) return -1;
+    if (token_stride * elt_bytes(b) % 16 != 0) return -1;
     return token_stride;
 }
 

@@ -28,3 +28,13 @@ def test_rotation_and_write_without_requests_is_the_rotation():
     assert lib.emm_rope_kv_scatter_fp8(b, given, OK, OK, OK, 0, OK + 256, c, None) == B.EMM_ERR_INVALID_ARG
     assert lib.emm_rope_kv_scatter_fp8(b, ctypes.byref(_rope()), OK, OK, OK, 0, FAR, c, None) == B.EMM_OK
     assert lib.emm_kv_scatter_fp8(b, OK, OK, 0, c, None) == B.EMM_OK
+
+
+def test_strides_beyond_any_memory_are_refused():
+    """Rows so far apart that the bytes they span pass 2^63: refused by the check itself, which counts them."""
+    lib, c = B.load(), ctypes.byref(_cache())
+    b, r = _batch(total_new_tokens=1 << 25), ctypes.byref(_rope())
+    for stride in (1 << 40, (1 << 40) + 8, 1 << 38, 1 << 62):
+        assert lib.emm_rope(b, r, OK, None, stride, FAR, None, None) == B.EMM_ERR_INVALID_ARG, stride
+        assert lib.emm_rope_kv_scatter_fp8(b, r, OK, OK, OK, stride, FAR, c, None) == B.EMM_ERR_INVALID_ARG, stride
+        assert lib.emm_kv_scatter_fp8(b, OK, OK, stride, c, None) == B.EMM_ERR_INVALID_ARG, stride
