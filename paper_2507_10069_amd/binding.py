@@ -390,6 +390,8 @@ def make_rope(inv_freq, *, rotary_dim: int, layout="half", factor: float = 1.0, 
     None for the tokens' places in their requests; sections: frequencies of each axis (default: one axis has them all).
     The returned object keeps both tensors alive."""
     axes = 0 if positions is None else int(positions.shape[0]) if positions.dim() == 2 else 1
+    if positions is not None and axes == 0:
+        raise ValueError("positions have no axis")
     parts = list(sections) if sections is not None and axes else [rotary_dim // 2] if axes == 1 else []
     if len(parts) != axes:
         raise ValueError("%d sections for %d axes of positions" % (len(parts), axes))

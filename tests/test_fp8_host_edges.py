@@ -1,6 +1,9 @@
 """Rotary positions and the 8-bit cache without a GPU: what the entry points answer at the edges of their arguments."""
 import ctypes
 
+import pytest
+import torch
+
 from paper_2507_10069_amd import binding as B
 from test_fp8_host import OK, _batch, _cache, _rope
 
@@ -38,3 +41,13 @@ def test_strides_beyond_any_memory_are_refused():
         assert lib.emm_rope(b, r, OK, None, stride, FAR, None, None) == B.EMM_ERR_INVALID_ARG, stride
         assert lib.emm_rope_kv_scatter_fp8(b, r, OK, OK, OK, stride, FAR, c, None) == B.EMM_ERR_INVALID_ARG, stride
         assert lib.emm_kv_scatter_fp8(b, OK, OK, stride, c, None) == B.EMM_ERR_INVALID_ARG, stride
+
+
+def test_positions_without_axes_are_refused():
+    """(as positions of the wrong type are: by the binding, before there is a descriptor)"""
+    inv = torch.zeros(64, dtype=torch.float64)
+    for shape in ((0, 5), (0, 0)):
+        with pytest.raises(ValueError):
+            B.make_rope(inv, rotary_dim=128, positions=torch.zeros(shape, dtype=torch.int32))
+    five = B.make_rope(inv, rotary_dim=128, positions=torch.zeros(5, 20, dtype=torch.int32), sections=[16, 16, 16, 8, 8])
+    assert B.load().emm_rope(_batch(), ctypes.byref(five), OK, None, 0, FAR, None, None) == B.EMM_ERR_INVALID_ARG
