@@ -181,12 +181,13 @@ emm_status emm_rope_inv_freq_host(const emm_rope_scaling* s, double* inv_freq, f
     auto index_of = [&](double turns) { return n * std::log(s->original_len / (turns * two_pi)) / (2.0 * std::log(s->base)); };
     const double lo = ramp ? std::max(std::floor(index_of(s->fast)), 0.0) : 0.0;
     const double hi = ramp ? std::max(std::min(std::ceil(index_of(s->slow)), n - 1.0), lo + 0.001) : 1.0;
+    // (the ramp's ends are held at frequency 0 or above; where even that one turns less than `slow` times there is no ramp)
+    const bool none_kept = s->kind == EMM_ROPE_LINEAR || (ramp && index_of(s->slow) < 0.0);
     for (int i = 0; i < s->rotary_dim / 2; ++i) {
         const double f = std::pow(base, -2.0 * i / n);
-        double kept = 1.0;                                   // share of the frequency that is not divided by scale
-        if (s->kind == EMM_ROPE_LINEAR) kept = 0.0;
-        if (s->kind == EMM_ROPE_YARN) kept = 1.0 - std::min(std::max((i - lo) / (hi - lo), 0.0), 1.0);
-        if (s->kind == EMM_ROPE_BANDS) kept = std::min(std::max((s->original_len * f / two_pi - s->slow) / (s->fast - s->slow), 0.0), 1.0);
+        double kept = none_kept ? 0.0 : 1.0;                 // share of the frequency that is not divided by scale
+        if (s->kind == EMM_ROPE_YARN && !none_kept) kept = 1.0 - std::min(std::max((i - lo) / (hi - lo), 0.0), 1.0);
+        if (s->kind == EMM_ROPE_BANDS && !none_kept) kept = std::min(std::max((s->original_len * f / two_pi - s->slow) / (s->fast - s->slow), 0.0), 1.0);
         inv_freq[i] = f * kept + f / s->scale * (1.0 - kept);
     }
     if (factor != nullptr) *factor = s->kind == EMM_ROPE_YARN ? static_cast<float>(0.1 * std::log(s->scale) + 1.0) : 1.0f;

@@ -1,6 +1,7 @@
 """Rotary positions and the 8-bit cache without a GPU: what the entry points answer at the edges of their arguments."""
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
@@ -51,3 +52,22 @@ def test_positions_without_axes_are_refused():
             B.make_rope(inv, rotary_dim=128, positions=torch.zeros(shape, dtype=torch.int32))
     five = B.make_rope(inv, rotary_dim=128, positions=torch.zeros(5, 20, dtype=torch.int32), sections=[16, 16, 16, 8, 8])
     assert B.load().emm_rope(_batch(), ctypes.byref(five), OK, None, 0, FAR, None, None) == B.EMM_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kind", ["yarn", "bands"])
+@pytest.mark.parametrize("original_len,slow,fast", [(6, 1.0, 32.0), (1, 0.5, 1.0), (100, 20.0, 32.0), (150, 24.0, 25.0)])
+def test_frequencies_that_all_turn_too_seldom_are_all_divided(kind, original_len, slow, fast):
+    """Even the highest frequency has fewer than `slow` turns in the trained length."""
+    n, base, scale = 64, 1e4, 8.0
+    plain = base ** (-2.0 * np.arange(n // 2) / n)
+    assert original_len / (2 * np.pi) < slow
+    inv, _ = B.emm_rope_inv_freq_host(n, base, kind, scale, original_len, slow=slow, fast=fast)
+    assert np.allclose(inv, plain / scale, rtol=1e-13, atol=0)
+
+
+@pytest.mark.parametrize("kind", ["yarn", "bands"])
+def test_frequencies_that_all_turn_often_enough_stay(kind):
+    n, base = 64, 1e4
+    plain = base ** (-2.0 * np.arange(n // 2) / n)
+    inv, _ = B.emm_rope_inv_freq_host(n, base, kind, 8.0, 2 ** 31 - 1, slow=1.0, fast=32.0)
+    assert (2 ** 31 - 1) * plain[-1] / (2 * np.pi) > 32 and np.allclose(inv, plain, rtol=1e-13, atol=0)
