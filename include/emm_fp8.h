@@ -67,6 +67,9 @@ emm_status emm_kv_gather_fp8(const emm_batch *batch, const emm_fp8_cache *cache,
  * EMM_BF16 with head_dim 128.  Arguments and results as there.  Values are exact in bf16 and meet q as such; scores,
  * softmax statistics and sums are in 32 bits; softmax weights are rounded to bf16 for the value product.  A NaN in V
  * reaches only rows that see its slot.  Results are run-to-run bitwise deterministic.
+ * The sums are divided by the sum of the weights at the end, and weights are at most 2^16 on average until then: results
+ * are finite where 2^16 * (slots of the context) * (largest |v|) is at most 2^127, so in a context of 2^17 slots for |v|
+ * up to 2^94.  Larger values, which the format holds, may come out as infinities or NaN.
  *   workspace  device scratch of at least emm_attn_fp8_workspace_size bytes, 16-byte aligned (may be NULL if that is
  *              0), the same size for all three calls; contents need no initialisation and mean nothing afterwards.
  *              Calls that may overlap must not share one.

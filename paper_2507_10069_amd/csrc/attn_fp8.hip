@@ -18,7 +18,10 @@
 // Values, O^T += V^T P^T: v_mfma_f32_16x16x32_bf16 wants for each channel 8 keys of a lane side by side.  A lane reads 8
 // neighbouring channels of the 8 keys whose scores it holds (the accumulators of two score products, which are then
 // its part of the operand P^T as they are), pairs keys by byte permutes, and v_cvt_scalef32_pk_bf16_fp8 makes two bf16 of
-// a pair.  V's scales go into P (a power of two; a weight is rounded to bf16 after it, half a step off either way).
+// a pair.  V's scales go into P (a power of two; a weight is rounded to bf16 after it, half a step off either way.  With V's least
+// scale, 2^-117, weights below 2^-9 of the row's largest are subnormal there, and off by up to 2^-17 of it.)
+// Weights are rounded to bf16 because the product takes both operands so; in 32 bits it would need 16 times the matrix instructions.
+// out is then 0.0018 of itself off (root mean square) where its own rounding makes 0.0017.
 //
 // Measured (28 query heads over 4 KV heads unless said): 64 contexts of 8192 96 us with the records' merge, 5.6 TB/s of the cache's
 // bytes, 91 without it; 32 contexts of 300 to 4600 with 32 over 8 heads 41.5 us, 4.1 TB/s (a request with little to do at its end

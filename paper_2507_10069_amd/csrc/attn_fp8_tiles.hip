@@ -12,10 +12,12 @@
 // S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_32x32x16_bf16.  A lane has one row and 32 of a tile's keys; K's rows lie in
 // LDS such that its weights, rounded to bf16, are the second product's operand as they are, and which channels a step of the first
 // takes is the same for K and q.
-// Weights are exp2(S c - m) with a reference m that is the row's maximum over its first tile, and follows only where a
-// tile's weights sum to more than 2^20: any reference gives the same result, and the sum, which is taken before
-// the weights are used, tells in time.  So the loop takes no maxima.  Row sums are of the weights before they are
-// rounded (of the rounded ones, and lse with them, they would be off by up to 2^-8 where few keys count).
+// Weights are exp2(S c - m) with a reference m that is the row's maximum over its first tile, and follows only where the
+// weights that a lane has of half a tile (16 keys; its partner lane has the row's other 16) sum to more than 2^20: any reference gives the
+// same result as long as the sums stay finite, which emm_fp8.h says of what values they do, and the sum, which is taken before the weights are
+// used, tells in time.  So the loop takes no maxima.  Row sums are of the weights before they are rounded (of the rounded ones, and lse
+// with them, they would be off by up to 2^-8 where few keys count).  The product's are rounded to bf16 because it takes both operands so; in
+// 32 bits it would need 16 times the matrix instructions.  out is then 0.0022 of itself off (root mean square) where its own rounding makes 0.0017.
 //
 // Measured (28 query heads over 4 KV heads): two chunks of 2048 behind 16384 890 to 960 us on different cards, 1070 to 1150 TFLOP/s, where
 // a large bf16 matrix product reaches 1346; the matrix units are busy 61 % of the cycles, at 1.9 of 2.4 GHz: it is the power that ends
@@ -44,7 +46,7 @@ constexpr int PLACES = 256;                              // workgroups that run 
 constexpr int MAX_PARTS = 128;                           // pieces of a unit (one unit of 30 k keys 24.3 us; 64: 26.0, 256: 28.4)
 constexpr int MIN_TILES_ALONE = 2, MIN_TILES_BEHIND = 4;    // key tiles of a piece where no unit is whole (16 units of 1000 keys 18.8 us; 3: 19.2, 4: 20.0), and
                                                             // behind whole ones (8 images' chunks 65.3; 2: 67.1, 8: 68.6)
-constexpr float LAG_LIMIT = 1048576.f;                   // 2^20
+constexpr float LAG_LIMIT = 1048576.f;                   // 2^20 for 16 keys: 2^16 a key, the factor in the header's bound on V
 constexpr int QK_OPS = 80;                               // of a tile's 119 softmax instructions beside the score products (72, 88: 1 % slower; at least 63)
 
 // LDS
