@@ -48,3 +48,38 @@ def test_rotation_and_write_has_the_bits_of_the_two_calls_in_rows_of_no_request(
         assert torch.equal(fused[n], t), n
     turned = b.rows if axes else b.T if requests else 0
     assert (got[turned:] == 5).all() and not (got[:turned] == 5).all(dim=-1).any()
+
+
+def test_rows_of_no_request_stay_and_all_others_are_turned():
+    print("case rows of no request", flush=True)
+    b = Batch([3, 9, 0], [4, 2, 11], heads=4, kv_heads=2, seed=5, extra_rows=5)
+    inv, _ = B.emm_rope_inv_freq_host(128, 1e4)
+    x = {n: _dev(b.rng.standard_normal((b.rows, h, 128)).astype(np.float32), torch.bfloat16) for n, h in (("q", 4), ("k", 2))}
+    out = {n: torch.full_like(t, 5.0) for n, t in x.items()}
+    B.emm_rope(b.batch, B.make_rope(_dev(inv), rotary_dim=128), x["q"], x["k"], out["q"], out["k"])
+    at = np.concatenate([np.arange(p, p + n) for p, n in zip(b.prefix, b.new)])
+    for n, t in out.items():
+        have = _f64(x[n])[: b.T]
+        _check_rotated(_f64(t)[: b.T], have, F.rotate(have, np.repeat(at[:, None], 64, 1), inv, 128, "half"), None, 128, "half", 1.0, "bf16")
+        assert (t[b.T:] == 5).all()
+
+
+def test_reading_back_skips_what_has_no_slot_in_both_outputs():
+    """Entries of the table outside the pool, slots behind the table, rows of no request: of K and of V every row is what its slot holds or what it was."""
+    print("case no slot", flush=True)
+    b = Batch([10, 0, 60, 4], [8, 3, 8, 6], kv_heads=2, heads=2, seed=8, extra_rows=4)
+    b.table[1, 0], b.table[3, 0] = b.num_pages + 7, -9
+    b.prefix[2] = b.table.shape[1] * 16 - 3                  # its last five tokens lie behind the table
+    b.table[2, -1] = b.table[2, 3]
+    b.dev["table"].copy_(_dev(b.table)), b.dev["prefix"].copy_(_dev(b.prefix))
+    for n in "kv":
+        b.codes[n] = np.where((b.codes[n] & 0x7F) == 0x7F, 0x30 + (n == "v"), b.codes[n]).astype(np.uint8)
+        b.scales[n] = b.rng.integers(100, 150, b.scales[n].shape).astype(np.uint8)
+    out = {n: torch.full((b.rows, 2, 128), 3.0, dtype=torch.bfloat16, device=DEV) for n in "kv"}
+    B.emm_kv_gather_fp8(b.batch, b.to_device(), out["k"], out["v"])
+    for n, t in out.items():
+        want = np.full((b.rows, 2, 128), 3.0)
+        for r, held in ((0, 8), (2, 3)):
+            pages, places = b.slots(r, int(b.prefix[r]), held)
+            want[b.cu[r]:b.cu[r] + held] = F.values_of(b.codes[n][pages, :, places], b.scales[n][pages, :, places])
+        assert np.array_equal(_f64(t), want), n
