@@ -10,8 +10,8 @@
 // records of a pair up.  Inside a workgroup the four waves take a pair's tiles in turn, straight from global memory to
 // registers, and meet in LDS at the end of the pair.
 // Small calls are bound by the trips through memory that follow each other, and finding the part is one of them.  Where the page table says
-// that they are small, every pair has the same number of parts, of the same number of tiles: page ids, and the merge's records, then
-// travel with the lengths, and pairs of one part need no merge.
+// that they are small, every pair has the same number of workgroups, which share its own tiles: nobody sums the lengths of others, the
+// merge's records travel with the lengths, and where the table holds no more than 512 tokens there is one part and no merge.
 //
 // Scores, S^T = K Q^T: a lane has 32 channels of a key, which v_cvt_scalef32_pk_bf16_fp8 makes bf16 in the key's scale (exact)
 // for four v_mfma_f32_16x16x32_bf16, and the same 32 channels of its row of q.
@@ -45,10 +45,12 @@ constexpr int TILE = 32;                                 // keys per step of a w
 constexpr int ROWS = 16;
 constexpr int OUT_STRIDE = D + 8;                        // bf16 values between output rows in LDS
 constexpr int LEAST_TILES = WAVES;                       // of a part: one for each wave
-// Fixed parts, where the page table holds at most so many tiles for each of the workgroups (16 contexts of 300 to 8000 22.6 us, and 24.4 as
-// a line; 32 of 2000 19.0 and 21.4; one of 1500 7.6 and 10.8; of the next size, 48 of 400 to 4000, 35.5 and 25.5)
+// Fixed parts, where the page table holds at most so many tiles for each of the workgroups.  Tables as wide as the longest context: 16 contexts of
+// 300 to 8000 23.5 us, and 25.3 as a line; 32 of 2000 19.0 and 21.4; one of 1500 7.4 and 11.0; of the next size, 48 of 400 to 4000, 35.5 and
+// 25.5.  Wider ones: one of 1500 with room for 8 k, 32 k, 128 k tokens 9.1, 10.0, 9.9 and 12.0; one of 500 8.9, 9.8, 9.9 and 9.0; 16 of 1500 with room
+// for 8 k 12.6 and 15.6.  (Parts by the table's width, whatever the contexts are: one of 1500 9.9, 11.6, 20.8; 16 of 1500 22.1.)
 constexpr int FIXED_TILES = 32;
-constexpr int WHOLE_TILES = 16;                          // of a pair that one workgroup does (32 of 500 10.6 us, in two parts 14.5; one of 1000 10.5 where two parts take 8.4)
+constexpr int WHOLE_TILES = 16;                          // in the table, for a pair that one workgroup does (32 of 500 10.6 us, in two parts 14.5; one of 1000 10.5 where two parts take 8.4)
 constexpr int WORKGROUPS = 512;                          // two on each compute unit (256 of twice the waves: ragged 49 us in place of 42)
 constexpr int ALONE = 256;                               // so many parts have a compute unit to themselves
 constexpr int MANY_RECORDS = 16;                         // of a pair: then 1024 threads merge (one of 16000 14.4 us, and 16.5 with 256; ragged 41.9, 48.2 with 1024)
@@ -63,7 +65,7 @@ __device__ inline float row_sum(float x) { return sum32(sum16(x)); }
 // how the batch's tiles are dealt
 struct RowsLayout {
     int G, workgroups;
-    int parts, part_tiles;                               // fixed: workgroups of a pair, and their tiles; else 0
+    int parts;                                           // fixed: workgroups of a pair; else 0
     Divisor by_G, by_kv_heads, by_workgroups, by_parts;
 };
 
@@ -138,6 +140,13 @@ __device__ inline int part_tiles(const RowsLayout& L, int all)
 {
     return max(all <= LEAST_TILES * ALONE ? LEAST_TILES : 2 * LEAST_TILES, L.by_workgroups.quotient(all - 1) + 1);
 }
+// Tiles of a fixed part of a pair that has so many in all, where it may have several.  (Short parts only where a merge has few of them: one of
+// 16000 12.0 us in parts of 8 tiles, and 13.8 of 4; of 1500 8.7 and 7.5.)
+__host__ __device__ inline int least_fixed_part(long long tiles) { return tiles <= MANY_RECORDS * LEAST_TILES ? LEAST_TILES : 2 * LEAST_TILES; }
+__device__ inline int fixed_part(const RowsLayout& L, int tiles)
+{
+    return L.parts == 1 ? tiles : max(least_fixed_part(tiles), L.by_parts.quotient(tiles + L.parts - 1));
+}
 // x / d, the same in all lanes, for d > 0, 0 <= x < 2^31 and a quotient below 2^20: by the reciprocal, which is off by less than one whole
 __device__ inline int small_quotient(int x, int d)
 {
@@ -146,11 +155,13 @@ __device__ inline int small_quotient(int x, int d)
     return rest < 0 ? q - 1 : rest >= d ? q + 1 : q;
 }
 
-// a fixed deal's request: its lengths travel with the page ids
+// a fixed deal's request
 template <bool CAUSAL>
 __device__ inline Request request_of(const BatchView& b, int r)
 {
-    const int n = b.new_lens[r], p = b.prefix_lens[r], cu = b.cu_new_lens[r];
+    int n = b.new_lens[r], p = b.prefix_lens[r], cu = b.cu_new_lens[r];
+    n = __builtin_amdgcn_readfirstlane(n), p = __builtin_amdgcn_readfirstlane(p), cu = __builtin_amdgcn_readfirstlane(cu);
+    asm volatile("" : "+s"(n), "+s"(p), "+s"(cu));                       // one trip for the three
     Request q;
     q.r = r;
     q.N = clamp_new_len(b, n, CAUSAL);
@@ -199,7 +210,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Arg
     auto line = [&] { if constexpr (FIXED) return NoLine{1}; else return Line<CAUSAL>(b); }();
     const int all = line.total * b.num_kv_heads;
     if (all == 0) return;
-    const int share = FIXED ? L.part_tiles : part_tiles(L, all);
+    const int share = FIXED ? 0 : part_tiles(L, all);
     int x = FIXED ? 0 : (int)min((long long)blockIdx.x * share, (long long)all);
     const int x_end = FIXED ? 1 : x + min(share, all - x);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -214,8 +225,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Arg
             const int pair = L.by_parts.quotient(blockIdx.x), r = L.by_kv_heads.quotient(pair);
             s.rq = request_of<CAUSAL>(b, r);
             s.kvh = pair - r * b.num_kv_heads;
-            s.t0 = min((int)(blockIdx.x - pair * L.parts) * share, s.rq.tiles);
-            s.t1 = min(s.t0 + share, s.rq.tiles);
+            const int size = fixed_part(L, s.rq.tiles);
+            s.t0 = min((int)(blockIdx.x - pair * L.parts) * size, s.rq.tiles);
+            s.t1 = min(s.t0 + size, s.rq.tiles);
             x = x_end;
         } else {
             s.rq = line.holding(L.by_kv_heads.quotient(x));
@@ -231,12 +243,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Arg
         return s;
     };
     // lane 2 j + k: block k of the wave's j-th tile from `from` on, in 16-key blocks of the pool
-    auto ids_of = [&](int r, int kvh, int from, int last) -> int {
-        const int blk = min(2 * (from + WAVES * (lane >> 1)) + (lane & 1), last);
-        const int page = min(max(b.page_table[(long long)r * b.max_pages + (blk >> b.page_shift)], 0), b.num_pages - 1);
-        return ((page * b.num_kv_heads + kvh) << b.page_shift) + (blk & ((1 << b.page_shift) - 1));
+    auto ask_ids = [&](const Segment& s, int from) -> int {
+        const int blk = min(2 * (from + WAVES * (lane >> 1)) + (lane & 1), max(((s.ctx + 15) >> 4) - 1, 0));
+        const int page = min(max(b.page_table[(long long)s.rq.r * b.max_pages + (blk >> b.page_shift)], 0), b.num_pages - 1);
+        return ((page * b.num_kv_heads + s.kvh) << b.page_shift) + (blk & ((1 << b.page_shift) - 1));
     };
-    auto ask_ids = [&](const Segment& s, int from) -> int { return ids_of(s.rq.r, s.kvh, from, max(((s.ctx + 15) >> 4) - 1, 0)); };
     // Are K and V of the segment to go past the caches?  Not where all of a call fits them, nor where another request holds the same
     // pages: what the first brings in serves the others.
     auto streamed = [&](const Segment& s) -> bool {
@@ -292,14 +303,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_fp8_rows_kernel(AttnFp8Arg
 
     constexpr bool AHEAD = RT == 1;                                      // one tile is computed, one travels (32 rows leave no registers for that)
     Tile even, odd;
-    int ids = 0;
-    if constexpr (FIXED) {                                               // (they need no lengths: what is behind the context is masked)
-        const int pair = L.by_parts.quotient(blockIdx.x), r = L.by_kv_heads.quotient(pair);
-        ids = ids_of(r, pair - r * b.num_kv_heads, (int)(blockIdx.x - pair * L.parts) * share + wave, (b.max_pages << b.page_shift) - 1);
-    }
     Segment now = next_segment();
     if (now.t0 >= now.t1) return;
-    if constexpr (!FIXED) ids = ask_ids(now, now.t0 + wave);
+    int ids = ask_ids(now, now.t0 + wave);
     uint32_t pairs[RT][16];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) ask_q(now, rt, pairs[rt]);
@@ -570,7 +576,7 @@ __global__ __launch_bounds__(THREADS) void attn_fp8_merge_rows_kernel(AttnFp8Arg
     if constexpr (FIXED) {
         rq = request_of<CAUSAL>(b, r);
         w0 = pair * L.parts;
-        w1 = w0 + small_quotient(max(rq.tiles - 1, 0), L.part_tiles);
+        w1 = w0 + small_quotient(max(rq.tiles - 1, 0), fixed_part(L, rq.tiles));
     } else {
         Line<CAUSAL> line(b);
         const int all = line.total * b.num_kv_heads;
@@ -654,14 +660,13 @@ RowsLayout layout_of(const BatchView& b)
     L.by_kv_heads = divisor_of(b.num_kv_heads);
     // no more workgroups than the page table can hold work for
     L.workgroups = (int)std::max<long long>(std::min<long long>(WORKGROUPS, (line_of(b) + LEAST_TILES - 1) / LEAST_TILES), 1);
-    L.parts = L.part_tiles = 0;
+    L.parts = 0;
     const long long pairs = (long long)b.num_reqs * b.num_kv_heads, most = line_of(b) / pairs;    // tiles of a pair
     if (rows_of(b) <= ROWS && pairs <= WORKGROUPS && line_of(b) <= (long long)WORKGROUPS * FIXED_TILES) {
         const long long per_pair = WORKGROUPS / pairs;                   // workgroups that a pair may have
-        // (short parts only where a merge has few of them: one of 16000 12.0 us in parts of 8 tiles, and 13.8 of 4; of 1500 8.7 and 7.5)
-        const int least = most <= WHOLE_TILES ? WHOLE_TILES : most <= MANY_RECORDS * LEAST_TILES ? LEAST_TILES : 2 * LEAST_TILES;
-        L.part_tiles = (int)std::max<long long>(least, (most + per_pair - 1) / per_pair);
-        L.parts = (int)std::max<long long>((most + L.part_tiles - 1) / L.part_tiles, 1);
+        const long long least = most <= WHOLE_TILES ? WHOLE_TILES : least_fixed_part(most);
+        const long long part = std::max(least, (most + per_pair - 1) / per_pair);    // of a context that fills the table
+        L.parts = (int)((most + part - 1) / part);
         L.workgroups = (int)pairs * L.parts;
     }
     L.by_parts = divisor_of(std::max(L.parts, 1));

@@ -229,3 +229,23 @@ def test_line_of_tiles(name):
     b.compare(q, out, lse, tokens)
     again, lse_again = b.attend(q)
     assert torch.equal(out, again) and torch.equal(lse, lse_again)
+
+
+@pytest.mark.parametrize("wider", [0, 40, 300, 1200])
+@pytest.mark.parametrize("causal", [True, False])
+def test_few_rows_under_tables_of_any_width(wider, causal):
+    """A pair's workgroups share its own tiles, not the table's: contexts on both sides of every least part, next to nothing, under tables up to
+    the widest that is dealt so."""
+    print("case table width", wider, causal, flush=True)
+    b = Batch([511, 512, 2047, 2048, 0, 33, 1500], [1, 1, 1, 1, 1, 0, 1], heads=21, kv_heads=3, seed=wider, wider=wider, causal=causal).fill_contexts()
+    b.to_device()
+    n = B.emm_attn_fp8_workspace_size(b.batch)
+    parts, rest = divmod(n, 7 * 3 * 16 * 130 * 4)
+    assert rest == 0 and 2 <= parts <= 512 // 21              # a record for each of a pair's workgroups: not the line's
+    q, guarded = b.queries(), torch.full((n + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    out, lse = b.attend(q, workspace=guarded[:n])
+    b.compare(q, out, lse)
+    assert (guarded[n:] == 0xA5).all()
+    guarded[:n] = 0xFF                                       # (records of NaN, as far as nobody writes them)
+    again, lse_again = b.attend(q, workspace=guarded[:n])
+    assert torch.equal(out, again) and torch.equal(lse, lse_again)
