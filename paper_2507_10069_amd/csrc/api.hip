@@ -14,6 +14,7 @@
 using emm::api::aligned16;
 using emm::api::check_arrays;
 using emm::api::check_scalars;
+using emm::api::page_size_ok;
 using emm::api::view_of;
 
 namespace {
@@ -22,8 +23,7 @@ constexpr int kVersion = 100;   // 0.1.0
 
 emm_status check_supported(const emm_batch* b)
 {
-    if (b->page_size != 16 && b->page_size != 32 && b->page_size != 64 && b->page_size != 128 && b->page_size != 256)
-        return EMM_ERR_UNSUPPORTED;
+    if (!page_size_ok(b)) return EMM_ERR_UNSUPPORTED;
     if (b->dtype == EMM_BF16 && b->head_dim != 128) return EMM_ERR_UNSUPPORTED;
     if (b->dtype == EMM_F32 && b->head_dim != 64 && b->head_dim != 128) return EMM_ERR_UNSUPPORTED;
     return EMM_OK;

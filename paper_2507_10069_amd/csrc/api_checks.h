@@ -26,6 +26,11 @@ inline emm_status check_scalars(const emm_batch* b)
     return EMM_OK;
 }
 
+inline bool page_size_ok(const emm_batch* b)
+{
+    return b->page_size == 16 || b->page_size == 32 || b->page_size == 64 || b->page_size == 128 || b->page_size == 256;
+}
+
 inline emm_status check_arrays(const emm_batch* b)
 {
     if (b->num_reqs == 0) return EMM_OK;

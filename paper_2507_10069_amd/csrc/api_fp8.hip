@@ -13,6 +13,7 @@ using emm::MOST_SLOTS;
 using emm::api::aligned16;
 using emm::api::check_arrays;
 using emm::api::check_scalars;
+using emm::api::page_size_ok;
 using emm::api::view_of;
 
 namespace {
@@ -24,8 +25,7 @@ emm_status check_rows(const emm_batch* b)
 {
     const emm_status st = check_scalars(b);
     if (st != EMM_OK) return st;
-    if (b->page_size != 16 && b->page_size != 32 && b->page_size != 64 && b->page_size != 128 && b->page_size != 256)
-        return EMM_ERR_UNSUPPORTED;
+    if (!page_size_ok(b)) return EMM_ERR_UNSUPPORTED;
     if (b->head_dim != 64 && b->head_dim != 128) return EMM_ERR_UNSUPPORTED;
     if (b->total_new_tokens > MOST_TOKENS || b->num_q_heads > MOST_HEADS || int64_t(b->total_new_tokens) * b->num_q_heads > MOST_ROWS ||
         int64_t(b->max_pages_per_req) * b->page_size > MOST_SLOTS)

@@ -59,8 +59,8 @@ constexpr int STREAM_TILES = 12000;                      // 96 MiB of codes: fro
 constexpr int MOST_COMPARED = 512;                       // requests among which shared pages are looked for
 
 // of the four lanes (l, l ^ 16, l ^ 32, l ^ 48) that hold a row
-__device__ inline float row_max(float x) { return max32(max16(x)); }
-__device__ inline float row_sum(float x) { return sum32(sum16(x)); }
+__device__ inline float row_max(float x) { return pair_max(max16(x)); }
+__device__ inline float row_sum(float x) { return pair_sum(sum16(x)); }
 
 // how the batch's tiles are dealt
 struct RowsLayout {

@@ -5,10 +5,14 @@
 // random products of up to 5e4: off by 1.8, in bf16 by 0.001), which makes the scores 25 times less exact than 32 bits are.
 #pragma once
 
+#include "attn_bf16_common.h"
 #include "fp8_device.h"
 
 namespace emm {
 namespace fp8 {
+
+using bf16attn::pair_max;
+using bf16attn::pair_sum;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -16,25 +20,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int HEAD_DIM = 128;
 constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
 
-// x with the lane 16 further (within 32), and with the lane 32 further, in both lanes
+// x with the lane 16 further (within 32), in both lanes; with the lane 32 further: pair_max, pair_sum
 __device__ inline float max16(float x)
 {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ inline float max32(float x)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
 __device__ inline float sum16(float x)
 {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ inline float sum32(float x)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 

@@ -27,7 +27,6 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "attn_bf16_common.h"
 #include "attn_fp8_common.h"
 
 namespace emm {
@@ -345,7 +344,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int v = 0; v < 16; ++v) x = fmaxf(x, s[kb][v]);
-        return max32(x);
+        return pair_max(x);
     };
     auto scores = [&](int slot, f32x16 (&s)[2]) {            // not interleaved: first and only tiles
 #pragma unroll
@@ -376,11 +375,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
         const bool grown = sum > LAG_LIMIT;
         if (__builtin_amdgcn_ballot_w64(grown || m != ref) != 0) {
             // (both lanes of a row decide alike)
-            if (max32(sum) > LAG_LIMIT) {
+            if (pair_max(sum) > LAG_LIMIT) {
                 float top = s[0];
 #pragma unroll
                 for (int v = 1; v < 16; ++v) top = fmaxf(top, s[v]);
-                const float to = fmaxf(m, max32(top) * c_log2), scale = __builtin_amdgcn_exp2f(m - to);
+                const float to = fmaxf(m, pair_max(top) * c_log2), scale = __builtin_amdgcn_exp2f(m - to);
                 m = to;
                 l *= scale;
 #pragma unroll
@@ -598,7 +597,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fp8_tiles_kernel(AttnFp8Args 
             for (int v = 0; v < 16; ++v)
                 if ((poison >> (16 * nb + v)) & 1) o[nb][v] = __builtin_nanf("");
     }
-    const float l_row = sum32(l);
+    const float l_row = pair_sum(l);
     if (e.pieces > 1) {
         float* rec = (float*)a.workspace + (long long)(u.slot * u.parts + u.part) * RECORD_FLOATS;
 #pragma unroll
