@@ -25,8 +25,9 @@
 //
 // Measured (28 query heads over 4 KV heads unless said): 64 contexts of 8192 96 us with the records' merge, 5.6 TB/s of the cache's
 // bytes, 91 without it; 32 contexts of 300 to 4600 with 32 over 8 heads 41.5 us, 4.1 TB/s (a request with little to do at its end
-// has its record, its merge and its start like any other: 36 us of the main kernel, of which 26 are bytes).  In fixed parts one of 1500
-// 7.5 us, of which an empty launch after the other would be 3.4, one of 60 4.5, 32 of 200 5.9, 8 of 2000 10.1, one of 16000 12.0.
+// has its record, its merge and its start like any other: 36 us of the main kernel, of which 26 are bytes).  In fixed parts, under tables as wide
+// as the contexts, calls in a graph: one of 1500 7.4 us, of which an empty launch after the other would be 3.4 (called one by one 7.5 in some runs
+// and 8.5 in others), one of 60 4.4, 32 of 200 6.0, 8 of 2000 10.5, one of 16000 12.4; what wider tables cost stands at FIXED_TILES.
 #include <algorithm>
 #include <type_traits>
 
@@ -45,12 +46,14 @@ constexpr int TILE = 32;                                 // keys per step of a w
 constexpr int ROWS = 16;
 constexpr int OUT_STRIDE = D + 8;                        // bf16 values between output rows in LDS
 constexpr int LEAST_TILES = WAVES;                       // of a part: one for each wave
-// Fixed parts, where the page table holds at most so many tiles for each of the workgroups.  Tables as wide as the longest context: 16 contexts of
-// 300 to 8000 23.5 us, and 25.3 as a line; 32 of 2000 19.0 and 21.4; one of 1500 7.4 and 11.0; of the next size, 48 of 400 to 4000, 35.5 and
-// 25.5.  Wider ones: one of 1500 with room for 8 k, 32 k, 128 k tokens 9.1, 10.0, 9.9 and 12.0; one of 500 8.9, 9.8, 9.9 and 9.0; 16 of 1500 with room
-// for 8 k 12.6 and 15.6.  (Parts by the table's width, whatever the contexts are: one of 1500 9.9, 11.6, 20.8; 16 of 1500 22.1.)
+// Fixed parts, where the page table holds at most so many tiles for each of the workgroups; as a line in brackets, us.  Tables as wide as the
+// longest context: 16 of 300 to 8000 23.8 (25.6), 32 of 2000 19.3 (22.2), one of 1500 7.4 (11.0), of the next size, 48 of 400 to 4000, 39.7
+// (33.2).  Wider ones: one of 1500 with room for 8 k, 32 k, 128 k tokens 9.1, 10.0, 9.9 (12.0); one of 500 8.9, 9.8, 9.9 (9.0); 16 of 1500 with room
+// for 8 k 12.6 (15.6), of the next size, for 32 k, 12.6 (15.5).  (Parts by the table's width, whatever the contexts are: one of 1500 9.9, 11.6,
+// 20.8; 16 of 1500 22.1.)
 constexpr int FIXED_TILES = 32;
-constexpr int WHOLE_TILES = 16;                          // in the table, for a pair that one workgroup does (32 of 500 10.6 us, in two parts 14.5; one of 1000 10.5 where two parts take 8.4)
+constexpr int WHOLE_TILES = 16;                          // in the table, for a pair that one workgroup does (32 of 500 9.3 us, in parts of four 11.4; of twice the pairs
+                                                         // 11.1 and 15.2; one of 1000, which would be 10.6, has parts: 7.5)
 constexpr int WORKGROUPS = 512;                          // two on each compute unit (256 of twice the waves: ragged 49 us in place of 42)
 constexpr int ALONE = 256;                               // so many parts have a compute unit to themselves
 constexpr int MANY_RECORDS = 16;                         // of a pair: then 1024 threads merge (one of 16000 14.4 us, and 16.5 with 256; ragged 41.9, 48.2 with 1024)
