@@ -184,14 +184,14 @@ STREAMED_TILES = 12000                                       # 32-key tiles of a
 
 
 def _over_few_pages(prefix, new, seed, shared=(), pool=400, **kw):
-    """Long contexts over a pool of few pages, each held many times; requests in `shared` begin with the same pages."""
+    """Long contexts over a pool of few pages, each held many times; requests in `shared` begin with the same pages, nine tenths of the longest."""
     b = Batch([16 * (pool // len(prefix) - 1)] * len(prefix), new, seed=seed, **kw)
     b.prefix[:] = prefix
     width = -(-int((b.prefix + b.new).max()) // b.page)
     # no two requests have the same page in the same place, but for those that share
     b.table = np.argsort(b.rng.random((b.num_pages, width)), axis=0)[: len(prefix)].astype(np.int32)
     for group in shared:
-        b.table[group, : width // 2] = b.table[group[0], : width // 2]
+        b.table[group, : width * 9 // 10] = b.table[group[0], : width * 9 // 10]
     codes = {n: torch.from_numpy(b.rng.standard_normal(b.codes[n].shape).astype(np.float32) * 120).clamp(-448, 448) for n in "kv"}
     b.codes = {n: x.to(torch.float8_e4m3fn).view(torch.uint8).numpy() for n, x in codes.items()}
     b.scales = {n: b.rng.integers(118, 122, b.codes[n].shape[:3]).astype(np.uint8) for n in "kv"}
@@ -204,7 +204,7 @@ def _over_few_pages(prefix, new, seed, shared=(), pool=400, **kw):
 
 
 LINES = {
-    # requests that share the first half of their pages, and others of other lengths beside them: from one part of a pair to the next a
+    # requests that share most of their pages, and others of other lengths beside them: from one part of a pair to the next a
     # workgroup goes from loads through the caches to loads past them and back
     "shared and private pages": (16, dict(prefix=[3000 + 37 * i for i in range(64)], new=[1] * 64, shared=[list(range(0, 20)), [25, 40, 41]])),
     "shared and private pages, 28 rows": (32, dict(prefix=[1800 + 23 * (i % 7) for i in range(70)], new=[4, 3, 4, 0, 1] * 14, shared=[list(range(9)), [30, 68]])),
@@ -215,6 +215,22 @@ LINES = {
 }
 
 
+def _ways_of_workgroups(b, tiles):
+    """For each of 512 workgroups, part by part: does another request hold the page that the part begins with?  The line is cut evenly; a part
+    ends with its workgroup's share or with its (request, KV head) pair."""
+    share, x, ways, own = -(-tiles // 512), 0, [[] for _ in range(512)], -(-(b.prefix + b.new) // 32)
+    for r in range(len(b.new)):
+        for _ in range(b.kv_heads if b.new[r] else 0):
+            t = 0
+            while t < own[r]:
+                column = b.table[:, 2 * t]
+                ways[x // share].append(int((column == b.table[r, 2 * t]).sum() > 1))
+                step = min(int(own[r]) - t, share - x % share)
+                x, t = x + step, t + step
+    assert x == tiles
+    return ways
+
+
 @pytest.mark.parametrize("name", list(LINES))
 def test_line_of_tiles(name):
     print("case line", name, flush=True)
@@ -223,6 +239,9 @@ def test_line_of_tiles(name):
     tiles = int((-(-(b.prefix + b.new) // 32) * (b.new > 0)).sum()) * b.kv_heads
     assert B.emm_attn_fp8_workspace_size(b.batch) == LINE_BYTES[rows] and tiles >= STREAMED_TILES      # it goes the way that it is here for
     assert ("long" in name) == (-(-tiles // 512) > 128)
+    if "shared" in name:                                     # some go from one way of loading to the other, and some back
+        changes = [(u, v) for w in _ways_of_workgroups(b, tiles) for u, v in zip(w, w[1:])]
+        assert (0, 1) in changes and (1, 0) in changes
     q = b.queries()
     out, lse = b.attend(q)
     tokens = sorted(set(b.rng.choice(b.T, min(b.T, 24), replace=False).tolist()) | {0, b.T - 1})
