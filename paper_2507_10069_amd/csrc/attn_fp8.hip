@@ -669,7 +669,7 @@ RowsLayout layout_of(const BatchView& b)
         const long long per_pair = WORKGROUPS / pairs;                   // workgroups that a pair may have
         const long long least = most <= WHOLE_TILES ? WHOLE_TILES : least_fixed_part(most);
         const long long part = std::max(least, (most + per_pair - 1) / per_pair);    // of a context that fills the table
-        L.parts = (int)((most + part - 1) / part);
+        L.parts = (int)std::max<long long>((most + part - 1) / part, 1);
         L.workgroups = (int)pairs * L.parts;
     }
     L.by_parts = divisor_of(std::max(L.parts, 1));

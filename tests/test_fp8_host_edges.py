@@ -71,3 +71,12 @@ def test_frequencies_that_all_turn_often_enough_stay(kind):
     plain = base ** (-2.0 * np.arange(n // 2) / n)
     inv, _ = B.emm_rope_inv_freq_host(n, base, kind, 8.0, 2 ** 31 - 1, slow=1.0, fast=32.0)
     assert (2 ** 31 - 1) * plain[-1] / (2 * np.pi) > 32 and np.allclose(inv, plain, rtol=1e-13, atol=0)
+
+
+@pytest.mark.parametrize("reqs", [1, 2, 600])
+def test_tables_without_pages(reqs):
+    """A size is told without dividing by what there is none of, and the call itself is refused."""
+    n = ctypes.c_size_t(7)
+    b = _batch(num_reqs=reqs, total_new_tokens=reqs, max_new_len=1, max_pages_per_req=0)
+    assert B.load().emm_attn_fp8_workspace_size(b, ctypes.byref(n)) == B.EMM_OK
+    assert B.load().emm_decode_attn_fp8(b, OK, ctypes.byref(_cache()), FAR, None, OK, 1 << 40, None) == B.EMM_ERR_INVALID_ARG
