@@ -227,11 +227,11 @@ def _prepare_pages(case, seed):
     table = torch.where(place < _ints(entries)[:, None], order[at], -1).to(torch.int32).contiguous()
     free_pages = torch.full((max(num_pages, 1),), -1, dtype=torch.int32, device=DEVICE)
     free_pages[:free] = order[sum(entries):]
-    s = {"case": case, "num_pages": max(num_pages, 1), "width": width, "tokens": sum(new), "page_table": table, "free_pages": free_pages,
+    s = {"case": case, "num_pages": max(num_pages, 1), "width": width, "tokens": max(sum(new), 1), "page_table": table, "free_pages": free_pages,
          "lens": _ints(cached), "add_lens": _ints(new), "held_from": _ints(held_from), "free_count": _ints([free])}
     for name, n, dt in (("prefix_lens", reqs, torch.int32), ("new_lens", reqs, torch.int32), ("cu_new_lens", reqs + 1, torch.int32),
                         ("lens_out", reqs, torch.int32), ("held_out", reqs, torch.int32), ("free_count_out", 1, torch.int32),
-                        ("slots", max(sum(new), 1), torch.int64), ("positions", max(sum(new), 1), torch.int32), ("refused", 1, torch.int32)):
+                        ("slots", s["tokens"], torch.int64), ("positions", s["tokens"], torch.int32), ("refused", 1, torch.int32)):
         s[name] = torch.zeros(n, dtype=dt, device=DEVICE)
     if own:
         from paper_2507_10069_amd import binding as B
