@@ -1,4 +1,4 @@
-"""ctypes binding of the C-ABI library declared in ``include/emm.h`` and ``include/emm_fp8.h``.
+"""ctypes binding of the C-ABI library declared in ``include/emm.h``, ``include/emm_fp8.h`` and ``include/emm_step.h``.
 
 Argument marshalling only: every function has the name and the meaning of the C entry point it
 calls, takes torch tensors that live on the GPU (PyTorch is used for device memory and streams,
@@ -29,6 +29,8 @@ EXPORTS = ["emm_kv_scatter", "emm_prefill_attn_workspace_size", "emm_prefill_att
            "emm_validate_batch_host", "emm_prefill_plan_host", "emm_rope", "emm_rope_inv_freq_host", "emm_status_string", "emm_version"]
 FP8_EXPORTS = ["emm_kv_scatter_fp8", "emm_rope_kv_scatter_fp8", "emm_kv_gather_fp8", "emm_attn_fp8_workspace_size", "emm_prefill_attn_fp8",
                "emm_cross_attn_fp8", "emm_decode_attn_fp8"]
+STEP_EXPORTS = ["emm_page_step", "emm_norm_rope", "emm_norm_rope_kv_scatter", "emm_norm_rope_kv_scatter_fp8", "emm_attn_window_workspace_size",
+                "emm_prefill_attn_window", "emm_decode_attn_window"]
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_KINDS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
 
@@ -84,6 +86,17 @@ class emm_rope_scaling(ctypes.Structure):
 
 class emm_fp8_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class emm_qk_norm(ctypes.Structure):
+    _fields_ = [("eps", ctypes.c_float), ("reserved", ctypes.c_int32), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
+    _head_dim = None                                     # of the weights, where make_qk_norm was given them
+
+
+class emm_page_step_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_reqs", "page_size", "num_pages", "max_pages_per_req", "max_tokens", "window", "sinks", "reserved")] + \
+               [(n, ctypes.c_void_p) for n in ("page_table", "free_pages", "lens", "add_lens", "held_from", "free_count", "prefix_lens", "new_lens",
+                                               "cu_new_lens", "lens_out", "held_out", "free_count_out", "slots", "positions", "refused")]
 
 
 _lib = None
@@ -147,6 +160,14 @@ def load() -> ctypes.CDLL:
                   "emm_attn_fp8_workspace_size": [bp, ctypes.POINTER(ctypes.c_size_t)]}
     for name in ("emm_prefill_attn_fp8", "emm_cross_attn_fp8", "emm_decode_attn_fp8"):
         signatures[name] = [bp, vp, cp, vp, vp, vp, ctypes.c_size_t, vp]
+    np_, i32 = ctypes.POINTER(emm_qk_norm), ctypes.c_int32
+    signatures["emm_page_step"] = [ctypes.POINTER(emm_page_step_params), vp]
+    signatures["emm_norm_rope"] = [bp, np_, rp, vp, vp, i64, vp, vp, vp]
+    signatures["emm_norm_rope_kv_scatter"] = [bp, np_, rp, vp, vp, vp, i64, vp, vp, vp, vp, vp]
+    signatures["emm_norm_rope_kv_scatter_fp8"] = [bp, np_, rp, vp, vp, vp, i64, vp, vp, cp, vp]
+    signatures["emm_attn_window_workspace_size"] = [bp, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+    for name in ("emm_prefill_attn_window", "emm_decode_attn_window"):
+        signatures[name] = [bp, i32, i32, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     for name, args in signatures.items():
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = args
@@ -476,6 +497,96 @@ def emm_cross_attn_fp8(batch: emm_batch, q, cache: emm_fp8_cache, out, lse=None,
 
 def emm_decode_attn_fp8(batch: emm_batch, q, cache: emm_fp8_cache, out, lse=None, workspace=None, stream=None) -> None:
     _attn_fp8("emm_decode_attn_fp8", batch, q, cache, out, lse, workspace, stream)
+
+
+def make_qk_norm(q_weight, k_weight, *, eps: float) -> emm_qk_norm:
+    """Fill the descriptor: float32 device tensors [head_dim], which the returned object keeps alive."""
+    for t in (q_weight, k_weight):
+        if str(t.dtype) != "torch.float32" or not t.is_contiguous() or t.dim() != 1:
+            raise ValueError("norm weights are contiguous float32 vectors")
+    if q_weight.numel() != k_weight.numel():
+        raise ValueError("weights of %d and %d channels" % (q_weight.numel(), k_weight.numel()))
+    norm = emm_qk_norm(eps, 0, _ptr(q_weight), _ptr(k_weight))
+    norm._keepalive = (q_weight, k_weight)
+    norm._head_dim = q_weight.numel()
+    return norm
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def _check_rows(batch: emm_batch, norm, rope, slots=None) -> None:
+    if rope is not None:
+        _check_positions(batch, rope)
+    if norm is not None and norm._head_dim is not None and norm._head_dim != batch.head_dim:
+        raise ValueError("norm weights of %d channels, heads of %d" % (norm._head_dim, batch.head_dim))
+    if slots is not None and (str(slots.dtype) != "torch.int64" or not slots.is_contiguous() or slots.numel() < batch.total_new_tokens):
+        raise ValueError("slots are a contiguous int64 tensor, one for each of %d tokens" % batch.total_new_tokens)
+
+
+def emm_norm_rope(batch: emm_batch, norm: Optional[emm_qk_norm], rope: Optional[emm_rope_params], q, k, q_out, k_out, token_stride: int = 0,
+                  stream=None) -> None:
+    _check_rows(batch, norm, rope)
+    _check(load().emm_norm_rope(ctypes.byref(batch), _ref(norm), _ref(rope), _ptr(q), _ptr(k), token_stride, _ptr(q_out), _ptr(k_out),
+                                _stream(stream)), "emm_norm_rope")
+
+
+def emm_norm_rope_kv_scatter(batch: emm_batch, norm: Optional[emm_qk_norm], rope: Optional[emm_rope_params], q, k_new, v_new, q_out, k_cache, v_cache,
+                             token_stride: int = 0, slots=None, stream=None) -> None:
+    _check_rows(batch, norm, rope, slots)
+    _check(load().emm_norm_rope_kv_scatter(ctypes.byref(batch), _ref(norm), _ref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), token_stride, _ptr(slots),
+                                           _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream(stream)), "emm_norm_rope_kv_scatter")
+
+
+def emm_norm_rope_kv_scatter_fp8(batch: emm_batch, norm: Optional[emm_qk_norm], rope: Optional[emm_rope_params], q, k_new, v_new, q_out,
+                                 cache: emm_fp8_cache, token_stride: int = 0, slots=None, stream=None) -> None:
+    _check_rows(batch, norm, rope, slots)
+    _check(load().emm_norm_rope_kv_scatter_fp8(ctypes.byref(batch), _ref(norm), _ref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), token_stride, _ptr(slots),
+                                               _ptr(q_out), ctypes.byref(cache), _stream(stream)), "emm_norm_rope_kv_scatter_fp8")
+
+
+def make_page_step(*, num_reqs, page_size, num_pages, max_pages_per_req, max_tokens, window=0, sinks=0, page_table, free_pages, lens, add_lens, held_from,
+                   free_count, prefix_lens, new_lens, cu_new_lens, lens_out, held_out, free_count_out, slots=None, positions=None,
+                   refused=None) -> emm_page_step_params:
+    """Fill the descriptor: int32 device tensors (slots: int64), large enough, which the returned object keeps alive."""
+    per_req = {"lens": lens, "add_lens": add_lens, "held_from": held_from, "prefix_lens": prefix_lens, "new_lens": new_lens, "lens_out": lens_out,
+               "held_out": held_out}
+    sizes = {**{k: (t, num_reqs) for k, t in per_req.items()}, "page_table": (page_table, num_reqs * max_pages_per_req), "free_pages": (free_pages, num_pages),
+             "free_count": (free_count, 1), "cu_new_lens": (cu_new_lens, num_reqs + 1), "free_count_out": (free_count_out, 1), "slots": (slots, max_tokens),
+             "positions": (positions, max_tokens), "refused": (refused, 1)}
+    for name, (t, n) in sizes.items():
+        kind = "torch.int64" if name == "slots" else "torch.int32"
+        if t is not None and (str(t.dtype) != kind or not t.is_contiguous() or t.numel() < n):
+            raise ValueError("%s is a contiguous %s tensor of %d or more" % (name, kind, n))
+    arrays = [sizes[n][0] for n in ("page_table", "free_pages", "lens", "add_lens", "held_from", "free_count", "prefix_lens", "new_lens", "cu_new_lens",
+                                    "lens_out", "held_out", "free_count_out", "slots", "positions", "refused")]
+    step = emm_page_step_params(num_reqs, page_size, num_pages, max_pages_per_req, max_tokens, window, sinks, 0, *[_ptr(t) for t in arrays])
+    step._keepalive = tuple(arrays)
+    return step
+
+
+def emm_page_step(step: emm_page_step_params, stream=None) -> None:
+    _check(load().emm_page_step(ctypes.byref(step), _stream(stream)), "emm_page_step")
+
+
+def emm_attn_window_workspace_size(batch: emm_batch, window: int, sinks: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().emm_attn_window_workspace_size(ctypes.byref(batch), window, sinks, ctypes.byref(n)), "emm_attn_window_workspace_size")
+    return int(n.value)
+
+
+def _attn_window(name: str, batch, window, sinks, q, k_cache, v_cache, out, lse, workspace, stream) -> None:
+    _check(getattr(load(), name)(ctypes.byref(batch), window, sinks, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(lse), _ptr(workspace),
+                                 _bytes(workspace), _stream(stream)), name)
+
+
+def emm_prefill_attn_window(batch: emm_batch, window: int, sinks: int, q, k_cache, v_cache, out, lse=None, workspace=None, stream=None) -> None:
+    _attn_window("emm_prefill_attn_window", batch, window, sinks, q, k_cache, v_cache, out, lse, workspace, stream)
+
+
+def emm_decode_attn_window(batch: emm_batch, window: int, sinks: int, q, k_cache, v_cache, out, lse=None, workspace=None, stream=None) -> None:
+    _attn_window("emm_decode_attn_window", batch, window, sinks, q, k_cache, v_cache, out, lse, workspace, stream)
 
 
 def emm_validate_batch_host(batch: emm_batch, page_table: np.ndarray, prefix_lens: np.ndarray,

@@ -26,7 +26,9 @@
 // heads, 4 x (1024 + 256) tokens 254 -> 26 us; 8 heads on 2 of 128, 4096 new tokens 5.59 -> 0.44 ms (78 TFLOP/s of the
 // 154 that a large fp32 matrix product reaches).  Relative error against 64 bits 4.2e-7 -> 3.0e-7 on the first.
 #include "emm_internal.h"
+#include "step_internal.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace emm {
@@ -62,8 +64,12 @@ __device__ inline bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800
 __device__ inline long long first_slot(int cu_new, int G, int r) { return (long long)max(cu_new, 0) * G / ROWS + r; }
 
 // NW: waves per workgroup; SPLIT: workgroups that share a row tile's channels; APART: fewer workgroups fit a compute unit (see PLACES)
-template <int D, int NW, int SPLIT, bool APART>
-__global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnArgs a, int G, Divisor by_G, Divisor by_kv_heads)
+// WINDOW: rows see the last keys up to their own and the first ones (emm_step.h).  The chunks that hold such keys are then a list without
+// a gap: the sinks', and those from the first row's window on.
+struct NoWindow {};
+template <int D, int NW, int SPLIT, bool APART, bool WINDOW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnArgs a, int G, Divisor by_G, Divisor by_kv_heads,
+                                                              std::conditional_t<WINDOW, WindowView, NoWindow> w)
 {
     constexpr int QK = D / 16;                        // 16-byte pieces of a Q or K row per lane
     constexpr int CH = D / SPLIT;                     // channels of the output that this workgroup makes
@@ -93,10 +99,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnArgs a, int G,
     // pages in a vector register every chunk waited for all loads on their way.)
     const __attribute__((address_space(4))) int32_t* pt =
         (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(b.page_table + (long long)r * b.max_pages);
-    auto page_of = [&](int i) -> int { return pt[min((int)(((uint32_t)(wave + NW * i) * KEYS) >> pg_log2), b.max_pages - 1)]; };
+    int sink_chunks = 0, gap = 0;                     // of the list of chunks; without a window it is all of them
+    auto chunk = [&](int i) -> int {                  // of this wave's i-th
+        const int c = wave + NW * i;
+        return WINDOW && c >= sink_chunks ? c + gap : c;
+    };
+    auto page_of = [&](int i) -> int { return pt[min((int)(((uint32_t)chunk(i) * KEYS) >> pg_log2), b.max_pages - 1)]; };
     // all lengths in one round trip, and with it every argument that is needed further down
     const int new_len = b.new_lens[r], prefix_len = b.prefix_lens[r], cu_new = b.cu_new_lens[r];
-    int page = page_of(0);                            // (an entry past the request's pages is read and not used)
+    int page = WINDOW ? 0 : page_of(0);               // (an entry past the request's pages is read and not used)
     asm volatile("" ::"s"(page), "s"(new_len), "s"(prefix_len), "s"(cu_new), "s"(a.q), "s"(a.k_cache), "s"(a.v_cache), "s"(a.out), "s"(a.lse), "s"(a.causal));
     __builtin_amdgcn_sched_barrier(0);
 
@@ -108,11 +119,23 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnArgs a, int G,
     const int row0 = (int)row0_wide;
     const int P = clamp_prefix_len(b, prefix_len, a.causal ? N : 0);
     const int kv_len = a.causal ? P + by_G.quotient(min(row0 + ROWS - 1, n_rows - 1)) + 1 : P;   // keys that some row here sees
-    const int n_chunks = (kv_len + KEYS - 1) / KEYS;
+    int n_chunks = (kv_len + KEYS - 1) / KEYS;
+    int low_first = 0, low_last = 0, sinks = 0;       // where the window of the first row and of the last begins
+    if constexpr (WINDOW) {
+        sinks = w.sinks;
+        low_first = window_low(w, P + by_G.quotient(row0));
+        low_last = window_low(w, kv_len - 1);
+        sink_chunks = min((int)(((uint32_t)sinks + KEYS - 1) / KEYS), low_first / KEYS);
+        gap = low_first / KEYS - sink_chunks;
+        n_chunks -= gap;
+        page = page_of(0);
+    }
     const int min_limit = a.causal ? P + by_G.quotient(row0) : P - 1;               // last key that every row here sees
     const int row = min(row0 + l16, n_rows - 1);
     const int tok = by_G.quotient(row);
     const int limit = a.causal ? P + tok : P - 1;                           // last key of this lane's row
+    int low = 0;                                                            // first key of its window
+    if constexpr (WINDOW) low = window_low(w, limit);
     const long long first_row = clamp_first_row(b, cu_new, N);
 
     const float* __restrict__ qp = (const float*)a.q + ((first_row + tok) * b.num_q_heads + kvh * G + (row - tok * G)) * D + 4 * g;
@@ -126,7 +149,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnArgs a, int G,
     for (int i = 0; i < VE * NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     auto chunk_base = [&](int i, int pg) -> long long {       // element offset of the KV head's 16 rows of chunk wave + NW i
-        const int off = ((wave + NW * i) * KEYS) & (ps - 1);
+        const int off = (chunk(i) * KEYS) & (ps - 1);
         return (((long long)min(max(pg, 0), b.num_pages - 1) * b.num_kv_heads + kvh) * ps + off) * D;
     };
     f32x4 k[2][QK];
@@ -149,12 +172,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnArgs a, int G,
         for (int j = 0; j < QK; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[j][e], q[j][e], s, 0, 0, 0);
-        const bool masked = c * KEYS + KEYS - 1 > min_limit;                // some row does not see some key
+        const bool masked = c * KEYS + KEYS - 1 > min_limit ||              // some row does not see some key
+                            (WINDOW && c * KEYS < low_last && c * KEYS + KEYS - 1 >= sinks);
+        auto before = [&](int key, int first) { return WINDOW && key < first && key >= sinks; };
         float x[4], p[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             x[u] = s[u] * b.softmax_scale;
-            if (masked && c * KEYS + 4 * g + u > limit) x[u] = -INFINITY;
+            if (masked && (c * KEYS + 4 * g + u > limit || before(c * KEYS + 4 * g + u, low))) x[u] = -INFINITY;
         }
         const float m_new = fmaxf(m, group_max(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))));
         const float ref = m_new == -INFINITY ? 0.f : m_new;                 // a row that sees none of the keys so far
@@ -174,7 +199,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnArgs a, int G,
             for (int u = 0; u < 4; ++u)
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
-                    if (c * KEYS + 4 * g + u >= kv_len) v[u][n] = vec(0.f);
+                    if (c * KEYS + 4 * g + u >= kv_len || before(c * KEYS + 4 * g + u, low_first)) v[u][n] = vec(0.f);
 #pragma unroll
                     for (int e = 0; e < VE; ++e) odd = odd || !is_finite(v[u][n][e]);
                 }
@@ -184,7 +209,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnArgs a, int G,
                     const float mine = u == 0 ? p[0] : u == 1 ? p[1] : u == 2 ? p[2] : p[3];
                     const float pk = __shfl(mine, l16 + 16 * (kk2 >> 2));
                     const float* vp = (const float*)a.v_cache + at + (long long)kk2 * D + ch0 + 4 * VE * g;
-                    if (c * KEYS + kk2 <= limit)
+                    if (c * KEYS + kk2 <= limit && !before(c * KEYS + kk2, low))
 #pragma unroll
                         for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -217,13 +242,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnArgs a, int G,
             const long long next = chunk_base(min(i + 1, end), page);
             load_k(next, k[1]);
             page = page_of(min(i + 2, end));
-            compute(wave + NW * i, at, k[0]);
+            compute(chunk(i), at, k[0]);
             if (i + 1 > end) break;
             load_v(next);
             at = chunk_base(min(i + 2, end), page);
             load_k(at, k[0]);
             page = page_of(min(i + 3, end));
-            compute(wave + NW * (i + 1), next, k[1]);
+            compute(chunk(i + 1), next, k[1]);
         }
     }
 
@@ -308,7 +333,8 @@ bool apart_of(int waves, long long workgroups, long long pairs, long long keys)
 
 }  // namespace
 
-hipError_t launch_attn_f32(const AttnArgs& a, hipStream_t stream)
+template <bool WINDOW>
+static hipError_t launch(const AttnArgs& a, std::conditional_t<WINDOW, WindowView, NoWindow> w, long long keys, hipStream_t stream)
 {
     const BatchView& b = a.b;
     if (b.total_new_tokens == 0 || b.num_reqs == 0) return hipSuccess;
@@ -317,10 +343,9 @@ hipError_t launch_attn_f32(const AttnArgs& a, hipStream_t stream)
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
     auto go = [&](auto d, auto nw, auto split, auto apart) {
         constexpr int D = decltype(d)::value, NW = decltype(nw)::value, SPLIT = decltype(split)::value;
-        hipLaunchKernelGGL((attn_f32_kernel<D, NW, SPLIT, decltype(apart)::value>), dim3((unsigned)(grid * SPLIT)), dim3(64 * NW), 0, stream, a, G, divisor_of(G), divisor_of(b.num_kv_heads));
+        hipLaunchKernelGGL((attn_f32_kernel<D, NW, SPLIT, decltype(apart)::value, WINDOW>), dim3((unsigned)(grid * SPLIT)), dim3(64 * NW), 0, stream, a, G, divisor_of(G), divisor_of(b.num_kv_heads), w);
     };
     const bool single = (long long)b.max_new_len * G <= ROWS;              // at most one row tile for a (request, KV head)
-    const long long keys = (long long)b.max_pages * b.page_size;
     const int waves = waves_of(grid, single, keys);
     const bool apart = single && apart_of(waves, grid, (long long)b.num_reqs * b.num_kv_heads, keys);
     auto of_dim = [&](auto d) {
@@ -338,6 +363,18 @@ hipError_t launch_attn_f32(const AttnArgs& a, hipStream_t stream)
     if (b.head_dim == 64) of_dim(std::integral_constant<int, 64>{});
     else of_dim(std::integral_constant<int, 128>{});
     return hipGetLastError();
+}
+
+hipError_t launch_attn_f32(const AttnArgs& a, hipStream_t stream)
+{
+    return launch<false>(a, NoWindow{}, (long long)a.b.max_pages * a.b.page_size, stream);
+}
+
+hipError_t launch_attn_f32_window(const AttnArgs& a, const WindowView& w, hipStream_t stream)
+{
+    // what a row tile looks at: the window, the sinks, the tile's own tokens
+    const long long keys = std::min((long long)a.b.max_pages * a.b.page_size, (long long)w.window + w.sinks + ROWS);
+    return launch<true>(a, w, keys, stream);
 }
 
 }  // namespace emm

@@ -1,0 +1,589 @@
+// Attention with a window and sinks over the paged bf16 cache, head_dim 128 (include/emm_step.h says which slots a row sees).
+//
+// A row is one (new token j, query head g of a KV group), index j * G + g, so that the G heads that share a KV head are neighbours.
+// The rows of a tile look at slots from the first that its first row's window holds to its last row's own, and at the sinks before
+// them.  In blocks of 16 slots, which lie in one page each, these are a list without a gap: the sinks' blocks, then the window's.
+// Tiles are taken from that list, so nothing is fetched or multiplied that no row sees, but for the ends of blocks and tiles.
+//
+// Two shapes of the same loop:
+//   rows   a workgroup has 128 rows, 32 to a wave, and its four waves share tiles of 64 keys: prompts, bound by the matrix pipes;
+//   keys   a workgroup has 32 rows, all of its four waves the same ones, and each wave takes every fourth tile of 32 keys by
+//          itself, without a barrier; they meet in LDS at the end.  Decode steps (bound by reading K and V) and small calls (bound by
+//          the trips through memory), whose contexts are cut into `parts` besides, so that they fill the chip: a second kernel adds
+//          the parts' records up.
+// K and V go from memory straight into LDS, whole rows of 256 bytes in XOR-swizzled chunks of 16; K is read with ds_read_b128, V with
+// the transposing read.  Scores are made transposed, S^T = K Q^T, and K's rows are stored with bits 2 and 3 of the place in the block
+// swapped: then a lane has one row's scores, and those are the value product's operand O^T += V^T P^T as they stand.
+//
+// The softmax's reference is a row's maximum of an earlier tile: it is raised, and the sums scaled, only when a tile brings a score that
+// is more than 2^LAG of it, which the lane's own maximum tells without asking the other half of the row.  (Any reference gives the same
+// quotient; weights are at most 2^LAG.)
+//
+// A slot that some row of a tile sees and another does not may hold an infinity or NaN, which a weight of 0 would not remove.  In the
+// tiles at the ends of windows such values are looked for, replaced by 0 and added to the rows that see them by hand.
+#include "attn_bf16_common.h"
+#include "step_internal.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace emm {
+
+namespace {
+
+using namespace bf16attn;
+
+constexpr int WAVES = 4;
+constexpr int WIDE_ROWS = 32 * WAVES;                    // rows of a workgroup of the rows shape
+constexpr int WAVE_ROWS = 32;
+constexpr int BLK = 16;                                  // slots of a block
+constexpr int SLAB = BLK * D * 2;                        // bytes of a block of one KV head
+constexpr int OUT_STRIDE = 272;                          // bytes between output rows in LDS
+constexpr int REC_STRIDE = D + 4;                        // floats between rows of records, in LDS and in the workspace: D values, m, l
+constexpr float LAG = 16.0f;                             // log2 of the largest weight
+constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
+
+struct WindowLayout {
+    int G, slots;                                        // row tiles per KV head that the grid has room for
+    int single;                                          // 1: a request has one row tile at most, and slot r is request r's
+    int parts;                                           // of a row tile's keys (keys shape)
+    int per_xcd;                                         // items of an XCD, in order; 0: item i is workgroup i
+    int items;
+    Divisor by_G, by_slots, by_parts, by_kv_heads;
+};
+
+// A row tile: which request's, and the list of blocks that its rows look at
+struct Tile {
+    int r, N, P, first_row;                              // request, new tokens, cached tokens, packed row of the first new token
+    int row0, n_rows;                                    // first row; rows of the (request, KV head)
+    int last;                                            // the last slot that any row sees
+    int low_first, low_last;                             // first slot of the first row's window, of the last row's
+    int sink_blocks, gap, blocks;                        // the list: blocks 0 .. sink_blocks - 1, then the others `gap` further on
+    __device__ int block(int v) const { return v + (v >= sink_blocks ? gap : 0); }
+};
+
+// First row tile of request r: its ceil(rows / ROWS) tiles fit between this and the next request's, whatever cu_new_lens[r] is.
+template <int ROWS> __device__ inline long long first_slot(int cu_new, int G, int r) { return (long long)max(cu_new, 0) * G / ROWS + r; }
+
+// The tile in `slot`; false: there is none.  Uniform over the workgroup.
+template <int ROWS> __device__ inline bool find_tile(const BatchView& b, const WindowLayout& L, const WindowView& w, int slot, Tile& t)
+{
+    int r = slot, row0 = 0;
+    if (!L.single) {
+        int lo = 0, hi = b.num_reqs;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first_slot<ROWS>(b.cu_new_lens[mid], L.G, mid) <= slot) lo = mid; else hi = mid;
+        }
+        r = lo;
+    }
+    const int new_len = b.new_lens[r], prefix_len = b.prefix_lens[r], cu = b.cu_new_lens[r];
+    t.r = r;
+    t.N = clamp_new_len(b, new_len, true);
+    t.n_rows = t.N * L.G;                                // (at most 2^30: see check_rows)
+    if (!L.single) {
+        const long long at = ((long long)slot - first_slot<ROWS>(cu, L.G, r)) * ROWS;
+        if (at < 0 || at >= t.n_rows) return false;
+        row0 = (int)at;
+    }
+    if (row0 >= t.n_rows) return false;
+    t.row0 = row0;
+    t.P = clamp_prefix_len(b, prefix_len, t.N);
+    t.first_row = clamp_first_row(b, cu, t.N);
+    t.last = t.P + L.by_G.quotient(min(row0 + ROWS, t.n_rows) - 1);
+    t.low_first = window_low(w, t.P + L.by_G.quotient(row0));
+    t.low_last = window_low(w, t.last);
+    const int first_block = t.low_first / BLK;
+    t.sink_blocks = min((int)(((uint32_t)w.sinks + BLK - 1) / BLK), first_block);
+    t.gap = first_block - t.sink_blocks;
+    t.blocks = t.last / BLK + 1 - t.gap;
+    return true;
+}
+
+__device__ inline bool is_finite_bf16(uint32_t half) { return (half & 0x7f80u) != 0x7f80u; }
+
+template <bool KEYS>
+__global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(AttnArgs a, WindowView w, WindowLayout L)
+{
+    constexpr int ROWS = KEYS ? WAVE_ROWS : WIDE_ROWS;
+    constexpr int BC_ = KEYS ? 32 : 64;                  // keys of a tile
+    constexpr int KB = BC_ / 32, TB = BC_ / BLK;         // 32-key parts and blocks of a tile
+    constexpr int TILE_BYTES = BC_ * D * 2;              // of K, or of V
+    constexpr int RING = 4 * TILE_BYTES;                 // two slots of K and V
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[KEYS ? WAVES * RING : RING];
+    __shared__ int bad_s[2][WAVES];                      // rows shape: keys of a tile's blocks whose V holds an infinity or NaN
+    const BatchView& b = a.b;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, h32 = lane >> 5;
+
+    int item = blockIdx.x;
+    if (L.per_xcd > 0) item = (blockIdx.x % NUM_XCD) * L.per_xcd + blockIdx.x / NUM_XCD;
+    if (item >= L.items) return;
+    int part = 0, slot, kvh;
+    if (L.per_xcd > 0) {                                 // neighbours share a KV head, and mostly a request
+        const int group = L.by_slots.quotient(item);
+        slot = item - group * L.slots;
+        kvh = KEYS ? L.by_parts.quotient(group) : group;
+        if (KEYS) part = group - kvh * L.parts;
+    } else {
+        const int pair = KEYS ? L.by_parts.quotient(item) : item;
+        if (KEYS) part = item - pair * L.parts;
+        slot = L.by_kv_heads.quotient(pair);
+        kvh = pair - slot * b.num_kv_heads;
+    }
+    Tile t;
+    if (!find_tile<ROWS>(b, L, w, slot, t)) return;
+    const int G = L.G;
+
+    // this workgroup's tiles (KEYS: of its part), and of those this wave's
+    const int all_tiles = (t.blocks + TB - 1) / TB;
+    int t_begin = 0, t_end = all_tiles;
+    if (KEYS) {
+        const int share = L.by_parts.quotient(all_tiles + L.parts - 1);
+        t_begin = min(part * share, all_tiles);
+        t_end = min(t_begin + share, all_tiles);
+    }
+    const int step = KEYS ? WAVES : 1, t_first = KEYS ? t_begin + wave : 0;
+    const int n_mine = t_end > t_first ? (t_end - t_first + step - 1) / step : 0;
+
+    const int wrow0 = t.row0 + (KEYS ? 0 : wave * WAVE_ROWS);
+    const bool active = wrow0 < t.n_rows;                // (a wave without rows only fetches)
+    const int row_c = min(wrow0 + l32, t.n_rows - 1);
+    const int tok = L.by_G.quotient(row_c);
+    const int limit = t.P + tok, low = window_low(w, limit);             // of this lane's row
+    const int limit_min = t.P + L.by_G.quotient(min(wrow0, t.n_rows - 1));
+    const int low_max = window_low(w, t.P + L.by_G.quotient(min(wrow0 + WAVE_ROWS, t.n_rows) - 1));
+
+    const __bf16* __restrict__ qp = (const __bf16*)a.q + (((long long)t.first_row + tok) * b.num_q_heads + kvh * G + (row_c - tok * G)) * D + 8 * h32;
+    bf16x8 qf[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) qf[s] = *(const bf16x8*)(qp + 16 * s);
+
+    // ---- fetching.  An instruction brings 4 rows of 256 bytes; lane i lands on row i / 16, chunk i % 16, and takes the chunk that belongs there.
+    //        K: row = 16 block + swap23(key in block), chunk c of it at c ^ (row & 15)    (read with ds_read_b128)
+    //        V: row = key,                             chunk c of it at c ^ ((row & 3) << 2)      (read with ds_read_tr16_b64)
+    const int ld_row = lane >> 4, ld_p = lane & 15;
+    int k_goff[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) k_goff[j] = swap23(4 * j + ld_row) * 256 + ((ld_p ^ (4 * j + ld_row)) << 4);
+    const int v_goff = ld_row * 256 + ((ld_p ^ (ld_row << 2)) << 4);
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem + (KEYS ? wave * RING : 0);
+    unsigned char* const my_ring = smem + (KEYS ? wave * RING : 0);
+    const int32_t* __restrict__ pt = b.page_table + (long long)t.r * b.max_pages;
+    const unsigned char* const kcb = (const unsigned char*)a.k_cache;
+    const unsigned char* const vcb = (const unsigned char*)a.v_cache;
+    // Where this wave's blocks lie, in slabs of the pool: lane k has that of the k-th block it fetches (KEYS: two of each of its tiles, else one of each
+    // tile) from its tile id_base on.  Behind the list's end the last block again: its keys are hidden from all rows.
+    constexpr int PER_TILE = KEYS ? TB : 1, IDS = 64 / PER_TILE;
+    int id_base = 0;
+    auto slab_of_block = [&](int blk) {
+        const int page = min(max(pt[min(blk >> b.page_shift, b.max_pages - 1)], 0), b.num_pages - 1);
+        return (long long)((((long long)page * b.num_kv_heads + kvh) << b.page_shift) + (blk & ((1 << b.page_shift) - 1)));
+    };
+    long long id_vec = 0;
+    auto refill = [&](int i) {
+        const int tile = t_first + (i + lane / PER_TILE) * step;
+        const int v = min(tile * TB + (KEYS ? lane % PER_TILE : wave), t.blocks - 1);
+        id_vec = slab_of_block(t.block(v));
+        id_base = i;
+    };
+    auto slab = [&](int i, int which) -> long long {         // byte offset of the block
+        const int at = (i - id_base) * PER_TILE + which;
+        const uint32_t lo = __builtin_amdgcn_readlane((int)id_vec, at), hi = __builtin_amdgcn_readlane((int)(id_vec >> 32), at);
+        return (long long)(((unsigned long long)hi << 32) | lo) * SLAB;
+    };
+    auto fetch = [&](int i) {                                // this wave's share of its tile i (KEYS: all of it)
+        const int buf = i & 1;
+#pragma unroll
+        for (int which = 0; which < PER_TILE; ++which) {
+            const long long at = slab(i, which);
+            const uint32_t to = ring + buf * TILE_BYTES + (KEYS ? which : wave) * SLAB;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) lds_dma16(kcb + at, k_goff[j], to + j * 1024);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) lds_dma16(vcb + at, v_goff + j * 1024, to + 2 * TILE_BYTES + j * 1024);
+        }
+    };
+    // is block v of the list seen whole by all rows of this wave?  (by all of a tile's blocks: no masks)
+    const int clear_lo = t.sink_blocks + (max(low_max, t.low_first) + BLK - 1) / BLK - t.low_first / BLK;
+    const int clear_hi = (limit_min + 1) / BLK - t.gap;
+    const int clear_sinks = min(min((int)((uint32_t)w.sinks / BLK), t.sink_blocks), (limit_min + 1) / BLK);
+    auto clear = [&](int tile) { return (tile * TB >= clear_lo && (tile + 1) * TB <= clear_hi) || (tile + 1) * TB <= clear_sinks; };
+    // the same for all rows of the workgroup: does V need looking at?
+    const int wg_lo = t.sink_blocks + (t.low_last + BLK - 1) / BLK - t.low_first / BLK;
+    const int wg_hi = (t.P + L.by_G.quotient(t.row0) + 1) / BLK - t.gap;
+    const int wg_sinks = min(clear_sinks, wg_hi + t.gap);
+    auto wg_clear = [&](int tile) { return (tile * TB >= wg_lo && (tile + 1) * TB <= wg_hi) || (tile + 1) * TB <= wg_sinks; };
+
+    // V rows of a block that this wave fetched: those that no row of the workgroup sees become zeros, and in the others what is not
+    // finite.  Returns which rows held such values.
+    auto look_at_v = [&](int v, unsigned char* block) -> int {
+        const int key0 = t.block(v) * BLK;
+        int bad = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int key = key0 + 4 * j + ld_row;
+            uint4* at = (uint4*)(block + j * 1024 + lane * 16);
+            const bool hidden = key > t.last || (key < t.low_first && key >= w.sinks);
+            uint4 x = *at;
+            uint32_t d[4] = {x.x, x.y, x.z, x.w};
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool lo = is_finite_bf16(d[e]), hi = is_finite_bf16(d[e] >> 16);
+                odd = odd || !lo || !hi;
+                d[e] = hidden ? 0u : d[e] & ((lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u));
+            }
+            if (hidden || odd) *at = make_uint4(d[0], d[1], d[2], d[3]);
+            const unsigned long long lanes = __builtin_amdgcn_ballot_w64(odd && !hidden);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if ((lanes >> (16 * k)) & 0xffffull) bad |= 1 << (4 * j + k);
+        }
+        return bad;
+    };
+
+    // ---- LDS read addresses
+    const int k_rd = l32 * 256 + ((h32 ^ (l32 & 15)) << 4);                  // step st: ^ (st << 5)
+    const int v_rd = 2 * TILE_BYTES + (8 * h32 + ((lane & 15) >> 2)) * 256 +
+                     ((4 * ((lane & 15) >> 2) + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) + (lane & 1) * 8;       // channel block nb: ^ (nb << 6)
+
+    const float c_log2 = b.softmax_scale * LOG2E;
+    float m = -INFINITY, l = 0.f;                            // reference (times log2 e); sum of this lane's weights
+    f32x16 o[4];
+#pragma unroll
+    for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[nb][v] = 0.f;
+
+    auto attend = [&](int i) {
+        const int buf = i & 1, tile = t_first + i * step;
+        const unsigned char* tiles = my_ring + buf * TILE_BYTES;
+        f32x16 s[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
+#pragma unroll
+        for (int st = 0; st < 8; ++st)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const bf16x8 kf = *(const bf16x8*)(tiles + kb * 32 * 256 + (k_rd ^ (st << 5)));
+                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[kb], 0, 0, 0);
+            }
+        if (!clear(tile)) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int key0 = t.block(tile * TB + 2 * kb + h) * BLK + 8 * h32;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int key = key0 + e;
+                        const bool seen = key <= limit && (key >= low || key < w.sinks);
+                        s[kb][8 * h + e] = seen ? s[kb][8 * h + e] : -INFINITY;
+                    }
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) top = fmaxf(top, s[kb][v]);
+        top *= c_log2;
+        if (__builtin_amdgcn_ballot_w64(top > m + LAG) != 0) {
+            const float both = pair_max(top);                // (both halves of a row decide alike)
+            const bool raise = both > m + LAG;
+            const float alpha = raise ? __builtin_amdgcn_exp2f(m - both) : 1.f;
+            m = raise ? both : m;
+            l *= alpha;
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[nb][v] *= alpha;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;          // a row that has seen no key yet: its weights are zeros
+        uint32_t p[KB][2][4];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; v += 2) {
+                bf16x2 pr;
+                pr[0] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[kb][v], c_log2, -ref));
+                pr[1] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[kb][v + 1], c_log2, -ref));
+                p[kb][v >> 3][(v & 7) >> 1] = __builtin_bit_cast(uint32_t, pr);
+            }
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                sum = sum4_bf16(p[kb][h][0], p[kb][h][1], sum);
+                sum = sum4_bf16(p[kb][h][2], p[kb][h][3], sum);
+            }
+        l += sum[0];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+                const u32x4 pw = {p[kb][h][0], p[kb][h][1], p[kb][h][2], p[kb][h][3]};
+                const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+#pragma unroll
+                for (int nb = 0; nb < 4; ++nb) {
+                    typedef short s16x4 __attribute__((ext_vector_type(4)));
+                    const unsigned char* src = tiles + (32 * kb + 16 * h) * 256 + (v_rd ^ (nb << 6));
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src + 4 * 256));
+                    const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[nb], 0, 0, 0);
+                }
+            }
+    };
+    // What is not finite, to the rows that see it: sums that it is in are infinite or NaN whatever its weight.  Rows `bad` of block v of the list.
+    auto add_odd = [&](int v, int bad) {
+        const int blk = t.block(v);
+        const long long at = slab_of_block(blk) * SLAB;
+        for (int rest = bad; rest != 0; rest &= rest - 1) {
+            const int place = __builtin_ctz(rest), key = blk * BLK + place;
+            const bool seen = key <= limit && (key >= low || key < w.sinks);
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+                for (int v4 = 0; v4 < 4; ++v4) {
+                    const uint2 x = *(const uint2*)(vcb + at + place * 256 + 2 * (32 * nb + 8 * v4 + 4 * h32));
+                    const uint32_t half[4] = {x.x & 0xffffu, x.x >> 16, x.y & 0xffffu, x.y >> 16};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (seen && !is_finite_bf16(half[e])) o[nb][4 * v4 + e] += __uint_as_float(half[e] << 16);
+                }
+        }
+    };
+
+    if (n_mine > 0) {
+        refill(0);
+        fetch(0);
+        for (int i = 0; i < n_mine; ++i) {
+            const int tile = t_first + i * step;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // this wave's share of tile i has landed
+            int bad[PER_TILE] = {};
+            const bool look = !wg_clear(tile);
+            if (look) {
+#pragma unroll
+                for (int which = 0; which < PER_TILE; ++which)
+                    bad[which] = look_at_v(tile * TB + (KEYS ? which : wave), my_ring + 2 * TILE_BYTES + (i & 1) * TILE_BYTES + (KEYS ? which : wave) * SLAB);
+                if (!KEYS && lane == 0) bad_s[i & 1][wave] = bad[0];
+            }
+            if constexpr (KEYS) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // all reads of the other slot are done, and V's zeros are written
+            } else {
+                __syncthreads();                             // everyone's share; and everyone is past its reads of the other slot
+            }
+            if (i + 1 < n_mine) {
+                if (i + 1 - id_base >= IDS) refill(i + 1);
+                fetch(i + 1);
+            }
+            if (active) {
+                attend(i);
+                if (look) {
+                    if constexpr (KEYS) {
+#pragma unroll
+                        for (int which = 0; which < PER_TILE; ++which)
+                            if (bad[which] != 0) add_odd(tile * TB + which, bad[which]);
+                    } else {
+                        for (int k = 0; k < WAVES; ++k) {
+                            const int those = __builtin_amdgcn_readfirstlane(bad_s[i & 1][k]);
+                            if (those != 0) add_odd(tile * TB + k, those);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    const float l_row = pair_sum(l);
+    auto at_row = [&](int row) -> long long {                // row of [T][H]
+        const int token = L.by_G.quotient(row);
+        return ((long long)t.first_row + token) * b.num_q_heads + kvh * G + (row - token * G);
+    };
+    __syncthreads();                                         // the rings are free
+
+    if constexpr (!KEYS) {
+        // out through LDS, so that an instruction stores four whole rows
+        if (!active) return;
+        const float inv = l_row != 0.f ? 1.f / l_row : 0.f;  // (a row sees itself)
+        unsigned char* stage = smem + wave * (32 * OUT_STRIDE);
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4) {
+                bf16x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = (__bf16)(o[nb][4 * v4 + e] * inv);
+                *(bf16x4*)(stage + l32 * OUT_STRIDE + 2 * (32 * nb + 8 * v4 + 4 * h32)) = x;
+            }
+        if (a.lse != nullptr && h32 == 0 && wrow0 + l32 < t.n_rows) a.lse[at_row(wrow0 + l32)] = m * LN2 + logf(l_row);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int row = wrow0 + 4 * j + ld_row;
+            if (row < t.n_rows)
+                *(uint4*)((__bf16*)a.out + at_row(row) * D + ld_p * 8) = *(const uint4*)(stage + (4 * j + ld_row) * OUT_STRIDE + ld_p * 16);
+        }
+    } else {
+        // the waves' sums: rows of REC_STRIDE floats
+        float* mine = (float*)smem + wave * WAVE_ROWS * REC_STRIDE + l32 * REC_STRIDE;
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4)
+                *(f32x4*)(mine + 32 * nb + 8 * v4 + 4 * h32) = f32x4{o[nb][4 * v4], o[nb][4 * v4 + 1], o[nb][4 * v4 + 2], o[nb][4 * v4 + 3]};
+        if (h32 == 0) {
+            mine[D] = m;
+            mine[D + 1] = l_row;
+        }
+        __syncthreads();
+        // 8 threads a row, 16 channels each
+        const int row = tid >> 3, ch = (tid & 7) * 4;
+        if (t.row0 + row >= t.n_rows) return;
+        const float* first = (const float*)smem + row * REC_STRIDE;
+        float top = -INFINITY, total = 0.f, weight[WAVES];
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) top = fmaxf(top, first[k * WAVE_ROWS * REC_STRIDE + D]);
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) {
+            const float mk = first[k * WAVE_ROWS * REC_STRIDE + D];
+            weight[k] = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk - top);
+            total += weight[k] * first[k * WAVE_ROWS * REC_STRIDE + D + 1];
+        }
+        f32x4 sum[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            sum[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) sum[x] += weight[k] * *(const f32x4*)(first + k * WAVE_ROWS * REC_STRIDE + ch + 32 * x);
+        }
+        if (L.parts > 1) {
+            float* rec = (float*)a.workspace + (((long long)(slot * b.num_kv_heads + kvh) * L.parts + part) * WAVE_ROWS + row) * REC_STRIDE;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) *(f32x4*)(rec + ch + 32 * x) = sum[x];
+            if (ch == 0) {
+                rec[D] = top;
+                rec[D + 1] = total;
+            }
+            return;
+        }
+        const float inv = total != 0.f ? 1.f / total : 0.f;
+        const long long at = at_row(t.row0 + row);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            bf16x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (__bf16)(sum[x][e] * inv);
+            *(bf16x4*)((__bf16*)a.out + at * D + ch + 32 * x) = y;
+        }
+        if (a.lse != nullptr && ch == 0) a.lse[at] = top * LN2 + logf(total);
+    }
+}
+
+// Adds the records of a row tile's parts up: a wave for a row, two channels a lane.
+__global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs a, WindowView w, WindowLayout L, int row_groups)
+{
+    const BatchView& b = a.b;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int unit = blockIdx.x / row_groups, row = (blockIdx.x - unit * row_groups) * WAVES + wave;
+    const int slot = L.by_kv_heads.quotient(unit), kvh = unit - slot * b.num_kv_heads;
+    Tile t;
+    if (!find_tile<WAVE_ROWS>(b, L, w, slot, t)) return;
+    if (t.row0 + row >= t.n_rows) return;
+    const float* rec = (const float*)a.workspace + ((long long)unit * L.parts * WAVE_ROWS + row) * REC_STRIDE;
+    const long long stride = (long long)WAVE_ROWS * REC_STRIDE;
+    float top = -INFINITY;
+    for (int k = 0; k < L.parts; ++k) top = fmaxf(top, rec[k * stride + D]);
+    float total = 0.f, x = 0.f, y = 0.f;
+    for (int k = 0; k < L.parts; ++k) {
+        const float mk = rec[k * stride + D];
+        const float weight = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk - top);
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        const f32x2 v = *(const f32x2*)(rec + k * stride + 2 * lane);
+        total += weight * rec[k * stride + D + 1];
+        x += weight * v[0];
+        y += weight * v[1];
+    }
+    const float inv = total != 0.f ? 1.f / total : 0.f;
+    const int token = L.by_G.quotient(t.row0 + row);
+    const long long at = ((long long)t.first_row + token) * b.num_q_heads + kvh * L.G + (t.row0 + row - token * L.G);
+    bf16x2 out;
+    out[0] = (__bf16)(x * inv);
+    out[1] = (__bf16)(y * inv);
+    *(bf16x2*)((__bf16*)a.out + at * D + 2 * lane) = out;
+    if (a.lse != nullptr && lane == 0) a.lse[at] = top * LN2 + logf(total);
+}
+
+constexpr int COMPUTE_UNITS = 256;
+
+// How a batch is dealt, from what the host knows.  keys: which of the two shapes
+struct Shape {
+    bool keys;
+    WindowLayout L;
+    long long items;
+};
+Shape shape_of(const BatchView& b, const WindowView& w)
+{
+    Shape s = {};
+    const int G = b.num_q_heads / b.num_kv_heads;
+    auto slots_of = [&](int rows) { return (long long)b.total_new_tokens * G / rows + b.num_reqs; };
+    const bool single = (long long)b.max_new_len * G <= WAVE_ROWS;
+    const long long wide = ((long long)b.total_new_tokens * G + WIDE_ROWS - 1) / WIDE_ROWS * b.num_kv_heads;     // at least
+    s.keys = single || wide < COMPUTE_UNITS;
+    const long long slots = s.keys ? (single ? b.num_reqs : slots_of(WAVE_ROWS)) : slots_of(WIDE_ROWS);
+    s.L.G = G;
+    s.L.slots = (int)slots;
+    s.L.single = s.keys && single;
+    s.L.parts = 1;
+    if (s.keys) {
+        // as many parts as fill the chip, each of a tile for every wave at least
+        const long long span = std::min((long long)b.max_pages * b.page_size, (long long)w.window + w.sinks + WAVE_ROWS);
+        const long long tiles = (span + 31) / 32;
+        const long long units = std::max(((long long)b.total_new_tokens * G + WAVE_ROWS - 1) / WAVE_ROWS, 1ll) * b.num_kv_heads;
+        const long long real = single ? slots * b.num_kv_heads : units;
+        s.L.parts = (int)std::max(1ll, std::min(COMPUTE_UNITS / std::max(real, 1ll), (tiles + WAVES - 1) / WAVES));
+    }
+    s.items = slots * b.num_kv_heads * s.L.parts;
+    s.L.items = (int)s.items;
+    s.L.per_xcd = s.L.single ? 0 : (int)((s.items + NUM_XCD - 1) / NUM_XCD);
+    s.L.by_G = divisor_of(G);
+    s.L.by_slots = divisor_of((int)slots);
+    s.L.by_parts = divisor_of(s.L.parts);
+    s.L.by_kv_heads = divisor_of(b.num_kv_heads);
+    return s;
+}
+
+}  // namespace
+
+size_t attn_window_workspace_bytes(const BatchView& b, const WindowView& w)
+{
+    if (b.total_new_tokens == 0 || b.num_reqs == 0) return 0;
+    const Shape s = shape_of(b, w);
+    return s.L.parts > 1 ? (size_t)s.items * WAVE_ROWS * REC_STRIDE * sizeof(float) : 0;
+}
+
+hipError_t launch_attn_window(const AttnArgs& a, const WindowView& w, hipStream_t stream)
+{
+    const BatchView& b = a.b;
+    const Shape s = shape_of(b, w);
+    const long long grid = s.L.per_xcd > 0 ? (long long)s.L.per_xcd * NUM_XCD : s.items;
+    if (grid > 0x3fffffff) return hipErrorInvalidValue;
+    if (!s.keys) {
+        hipLaunchKernelGGL((attn_window_kernel<false>), dim3((unsigned)grid), dim3(64 * WAVES), 0, stream, a, w, s.L);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((attn_window_kernel<true>), dim3((unsigned)grid), dim3(64 * WAVES), 0, stream, a, w, s.L);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess || s.L.parts == 1) return err;
+    const int rows = (int)std::min<long long>((long long)b.max_new_len * s.L.G, WAVE_ROWS), groups = (rows + WAVES - 1) / WAVES;
+    hipLaunchKernelGGL(attn_window_merge_kernel, dim3((unsigned)(s.L.slots * b.num_kv_heads * groups)), dim3(64 * WAVES), 0, stream, a, w, s.L, groups);
+    return hipGetLastError();
+}
+
+}  // namespace emm

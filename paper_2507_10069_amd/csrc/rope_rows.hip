@@ -1,7 +1,7 @@
-// Rotary positions of q and k, and the way of new K and V rows into the 8-bit cache (formulas: include/emm.h,
-// include/emm_fp8.h).
+// Rotary positions of q and k, norms of their heads before that, and the way of new K and V rows into a cache (formulas:
+// include/emm.h, include/emm_fp8.h, include/emm_step.h).
 //
-// Both are bound by the bytes of the rows.  A row is one (token, head); a lane holds 16 of its channels, so that a head of
+// All are bound by the bytes of the rows.  A row is one (token, head); a lane holds 16 of its channels, so that a head of
 // 128 is 8 lanes and a wave takes 8 rows at a time.  Of a rotated head they are 8 pairs: channels 8 u .. 8 u + 7 and the 8 that
 // are rotary_dim / 2 further up, or 16 in a row where pairs are neighbours.  A token's cosines and sines are made once by
 // its wave, a lane for each frequency (at most 64), and reach the lanes that need eight of them through LDS.
@@ -11,6 +11,9 @@
 // of 4 heads read back in 24.2 us (108 MB, 4.5 TB/s).  64 tokens' rotation and write takes 3.9 us on the card, an empty kernel 1.7;
 // what a decode step waits for is the launch.
 #include "fp8_device.h"
+#include "step_internal.h"
+
+#include <type_traits>
 
 namespace emm {
 
@@ -81,10 +84,48 @@ __device__ inline uint32_t row_most(uint32_t x)
     return x;
 }
 
-// rows of a token: K heads, then (QUANT) V heads, then q heads
-template <typename T, int D, bool QUANT, bool ROPE>
-__global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, RopeView rope, NewRows rows, Fp8Pools pools, int splits)
+template <int LANES>                                     // sum over them
+__device__ inline float row_sum(float x)
 {
+    auto of = [](float v, auto ctrl) { return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, true)); };
+    x += of(x, std::integral_constant<int, 0xb1>{});
+    x += of(x, std::integral_constant<int, 0x4e>{});
+    if constexpr (LANES == 8) x += of(x, std::integral_constant<int, 0x141>{});
+    return x;
+}
+
+// 1 / sqrt(mean(x^2) + eps) of a row, of which this lane holds 16 channels.  Squares of |x| from 1.8e19 on pass the range of 32 bits:
+// such a row is taken again in units of 2^70, so that the squares of all finite values add up to less than 2^124.
+template <int LANES>
+__device__ inline float row_norm(const float (&x)[8], const float (&y)[8], float eps)
+{
+    constexpr float MEAN = 1.0f / (16 * LANES);
+    auto squares = [&](float unit) {
+        float a = 0.f, c = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            a = fmaf(x[i] * unit, x[i] * unit, a);
+            c = fmaf(y[i] * unit, y[i] * unit, c);
+        }
+        return row_sum<LANES>(a + c);
+    };
+    const float sum = squares(1.0f);
+    float norm = __builtin_amdgcn_rsqf(fmaf(sum, MEAN, eps));
+    if (!(sum < __builtin_inff())) {
+        constexpr float UNIT = 0x1p-70f;
+        norm = __builtin_amdgcn_rsqf(fmaf(squares(UNIT), MEAN, eps * UNIT * UNIT)) * UNIT;
+    }
+    return norm;
+}
+
+enum Cache { NO_CACHE, FP8, PLAIN /* in the batch's dtype */ };
+
+// rows of a token: K heads, then (with a cache) V heads, then q heads
+template <typename T, int D, int CACHE, bool ROPE, bool NORM>
+__device__ __forceinline__ void do_rows(const BatchView& b, const RopeView& rope, const NewRows& rows, const Fp8Pools& pools, const PlainPools& plain,
+                                        const NormView& norm, int splits)
+{
+    constexpr bool QUANT = CACHE == FP8, CACHED = CACHE != NO_CACHE;
     constexpr int UNITS = D / 16, ROWS = 64 / UNITS;
     __shared__ float2 turns[WAVES][D / 2];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -92,7 +133,7 @@ __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, Rope
     const int t = (int)(item / splits), part = (int)(item - (long long)t * splits);
     if (t >= b.total_new_tokens) return;
 
-    const int n_k = rows.k != nullptr ? b.num_kv_heads : 0, n_v = QUANT ? b.num_kv_heads : 0, n_q = rows.q != nullptr ? b.num_q_heads : 0;
+    const int n_k = rows.k != nullptr ? b.num_kv_heads : 0, n_v = CACHED ? b.num_kv_heads : 0, n_q = rows.q != nullptr ? b.num_q_heads : 0;
     const int n_rows = n_k + n_v + n_q, u = lane % UNITS;
     const bool unit_turns = ROPE && u < rope.rotary_dim / 16;
     // a pass: 16 channels of one of the ROWS rows from `base` on, in two eights at a0 and a1
@@ -125,12 +166,17 @@ __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, Rope
 
     TokenPlace place = {0, -1};
     long long row0 = -1;
-    const bool from_batch = ROPE && rope.num_axes == 0;
-    if (QUANT || from_batch) {
+    const bool from_batch = ROPE && rope.num_axes == 0, given = CACHED && norm.slots != nullptr;
+    if ((CACHED && !given) || from_batch) {
         place = place_of_token(b, t);
-        if (place.slot < 0 && (!ROPE || from_batch)) return;     // a row of no request stays as it was; with a given position its q is turned
+        if (place.slot < 0 && ((!ROPE && !NORM) || from_batch)) return;  // a row of no request stays as it was; with a given position its q is turned
     }
-    if (QUANT) row0 = pool_row(b, place);
+    if (given) {
+        const long long slot = norm.slots[t], page = slot >> (4 + b.page_shift);
+        if (slot >= 0 && page < b.num_pages) row0 = page * b.num_kv_heads * b.page_size + (slot & (b.page_size - 1));
+    } else if (CACHED) {
+        row0 = pool_row(b, place);
+    }
     if (ROPE && lane < rope.rotary_dim / 2) {
         long long position = place.slot;
         if (!from_batch) {
@@ -147,14 +193,33 @@ __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, Rope
 #pragma unroll
         for (int i = 0; i < 8; ++i) cs[i] = turns[wave][8 * u + i];
     }
+    float wx[8] = {}, wy[8] = {};                            // weights of the lane's channels
     for (int base = part * ROWS; base < n_rows; base += splits * ROWS) {
         const Place p = place_in(base);
         const bool valid = p.valid, is_k = p.is_k, is_v = p.is_v, turned = p.turned;
         const int head = p.head, a0 = p.a0, a1 = p.a1;
         if (base != part * ROWS) ask(p);
         float x[8], y[8];
+        const typename Row8<T>::Raw held0 = raw0, held1 = raw1;
         Row8<T>::widen(raw0, x);
         Row8<T>::widen(raw1, y);
+        if constexpr (NORM) {
+            // (from the first pass that is all of q's rows on they stay the same)
+            if (base == part * ROWS || base < n_k + n_v + splits * ROWS) {
+                const float* w = is_k ? norm.k_weight : norm.q_weight;
+                typename Row8<float>::Raw w0 = Row8<float>::load(w + a0), w1 = Row8<float>::load(w + a1);
+                Row8<float>::widen(w0, wx);
+                Row8<float>::widen(w1, wy);
+            }
+            if (!is_v) {
+                const float by = row_norm<UNITS>(x, y, norm.eps);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] = x[i] * by * wx[i];
+                    y[i] = y[i] * by * wy[i];
+                }
+            }
+        }
         if (turned) {
             if (rope.interleaved) {
 #pragma unroll
@@ -197,6 +262,17 @@ __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, Rope
                 *(uint2*)(codes + a1) = make_uint2(pack4(y[0], y[1], y[2], y[3]), pack4(y[4], y[5], y[6], y[7]));
                 if (u == 0) (is_k ? pools.k_scale : pools.v_scale)[at] = (unsigned char)byte;
             }
+        } else if (CACHE == PLAIN && (is_k || is_v)) {
+            if (valid && row0 >= 0) {
+                T* dst = (T*)(is_k ? plain.k : plain.v) + (row0 + (long long)head * b.page_size) * D;
+                if (is_k) {
+                    Row8<T>::store(dst + a0, x);
+                    Row8<T>::store(dst + a1, y);
+                } else {
+                    *(typename Row8<T>::Raw*)(dst + a0) = held0;     // bit for bit
+                    *(typename Row8<T>::Raw*)(dst + a1) = held1;
+                }
+            }
         } else if (valid) {
             const int heads = is_k ? b.num_kv_heads : b.num_q_heads;
             T* dst = (T*)(is_k ? rows.k_out : rows.q_out) + ((long long)t * heads + head) * D;
@@ -204,6 +280,20 @@ __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, Rope
             Row8<T>::store(dst + a1, y);
         }
     }
+}
+
+template <typename T, int D, bool QUANT, bool ROPE>
+__global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, RopeView rope, NewRows rows, Fp8Pools pools, int splits)
+{
+    do_rows<T, D, QUANT ? FP8 : NO_CACHE, ROPE, false>(b, rope, rows, pools, PlainPools{}, NormView{}, splits);
+}
+
+// With norms, a cache in the batch's dtype, or given slots
+template <typename T, int D, int CACHE, bool ROPE, bool NORM>
+__global__ __launch_bounds__(64 * WAVES) void norm_rope_rows_kernel(BatchView b, RopeView rope, NewRows rows, Fp8Pools pools, PlainPools plain,
+                                                                    NormView norm, int splits)
+{
+    do_rows<T, D, CACHE, ROPE, NORM>(b, rope, rows, pools, plain, norm, splits);
 }
 
 // 16 codes to the batch's dtype, exact
@@ -263,18 +353,41 @@ __global__ __launch_bounds__(64 * WAVES) void kv_gather_fp8_kernel(BatchView b, 
     }
 }
 
-template <typename T, int D>
-hipError_t launch_rows(const BatchView& b, const RopeView& rope, const NewRows& rows, const Fp8Pools* pools, hipStream_t stream)
+// Few tokens: a wave for each pass over a token's rows, which takes its turns by itself; many: a wave for a token.
+template <int D>
+int splits_of(const BatchView& b, const NewRows& rows, bool cached, dim3& grid)
 {
-    // Few tokens: a wave for each pass over a token's rows, which takes its turns by itself; many: a wave for a token.
-    const int heads = (rows.k != nullptr ? b.num_kv_heads : 0) + (pools != nullptr ? b.num_kv_heads : 0) + (rows.q != nullptr ? b.num_q_heads : 0);
+    const int heads = (rows.k != nullptr ? b.num_kv_heads : 0) + (cached ? b.num_kv_heads : 0) + (rows.q != nullptr ? b.num_q_heads : 0);
     const int passes = (heads * (D / 16) + 63) / 64;
     const int splits = (long long)b.total_new_tokens * passes <= MOST_SPLIT ? passes : 1;
     const long long items = (long long)b.total_new_tokens * splits;
-    const dim3 grid((unsigned)((items + WAVES - 1) / WAVES)), block(64 * WAVES);
+    grid = dim3((unsigned)((items + WAVES - 1) / WAVES));
+    return splits;
+}
+
+template <typename T, int D>
+hipError_t launch_rows(const BatchView& b, const RopeView& rope, const NewRows& rows, const Fp8Pools* pools, hipStream_t stream)
+{
+    dim3 grid;
+    const dim3 block(64 * WAVES);
+    const int splits = splits_of<D>(b, rows, pools != nullptr, grid);
     if (pools == nullptr) hipLaunchKernelGGL((rope_rows_kernel<T, D, false, true>), grid, block, 0, stream, b, rope, rows, Fp8Pools{}, splits);
     else if (rope.rotary_dim > 0) hipLaunchKernelGGL((rope_rows_kernel<T, D, true, true>), grid, block, 0, stream, b, rope, rows, *pools, splits);
     else hipLaunchKernelGGL((rope_rows_kernel<T, D, true, false>), grid, block, 0, stream, b, rope, rows, *pools, splits);
+    return hipGetLastError();
+}
+
+template <typename T, int D, int CACHE>
+hipError_t launch_norm_rows(const BatchView& b, const NormView& norm, const RopeView& rope, const NewRows& rows, const Fp8Pools& fp8, const PlainPools& plain,
+                            hipStream_t stream)
+{
+    dim3 grid;
+    const dim3 block(64 * WAVES);
+    const int splits = splits_of<D>(b, rows, CACHE != NO_CACHE, grid);
+    const bool turns = rope.rotary_dim > 0, norms = norm.q_weight != nullptr;
+    if (turns && norms) hipLaunchKernelGGL((norm_rope_rows_kernel<T, D, CACHE, true, true>), grid, block, 0, stream, b, rope, rows, fp8, plain, norm, splits);
+    else if (norms) hipLaunchKernelGGL((norm_rope_rows_kernel<T, D, CACHE, false, true>), grid, block, 0, stream, b, rope, rows, fp8, plain, norm, splits);
+    else hipLaunchKernelGGL((norm_rope_rows_kernel<T, D, CACHE, true, false>), grid, block, 0, stream, b, rope, rows, fp8, plain, norm, splits);
     return hipGetLastError();
 }
 
@@ -298,6 +411,22 @@ hipError_t launch_rope_rows(const BatchView& b, bool bf16, const RopeView& rope,
 {
     if (bf16) return b.head_dim == 128 ? launch_rows<__bf16, 128>(b, rope, rows, pools, stream) : launch_rows<__bf16, 64>(b, rope, rows, pools, stream);
     return b.head_dim == 128 ? launch_rows<float, 128>(b, rope, rows, pools, stream) : launch_rows<float, 64>(b, rope, rows, pools, stream);
+}
+
+hipError_t launch_norm_rope_rows(const BatchView& b, bool bf16, const NormView& norm, const RopeView& rope, const NewRows& rows, const Fp8Pools* fp8,
+                                 const PlainPools* plain, hipStream_t stream)
+{
+    auto go = [&](auto type, auto d) {
+        typedef decltype(type) T;
+        constexpr int D = decltype(d)::value;
+        if (fp8 != nullptr) return launch_norm_rows<T, D, FP8>(b, norm, rope, rows, *fp8, PlainPools{}, stream);
+        if (plain != nullptr) return launch_norm_rows<T, D, PLAIN>(b, norm, rope, rows, Fp8Pools{}, *plain, stream);
+        return launch_norm_rows<T, D, NO_CACHE>(b, norm, rope, rows, Fp8Pools{}, PlainPools{}, stream);
+    };
+    using wide = std::integral_constant<int, 128>;
+    using narrow = std::integral_constant<int, 64>;
+    if (bf16) return b.head_dim == 128 ? go(__bf16{}, wide{}) : go(__bf16{}, narrow{});
+    return b.head_dim == 128 ? go(float{}, wide{}) : go(float{}, narrow{});
 }
 
 hipError_t launch_kv_gather_fp8(const BatchView& b, bool bf16, const Fp8Pools& pools, void* k_out, void* v_out, hipStream_t stream)

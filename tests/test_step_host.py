@@ -1,0 +1,257 @@
+"""Page steps, norms with rotation and attention with a window on a machine without a GPU: exports, descriptors, refusals before any HIP call."""
+import ctypes
+import math
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+
+from oracle import step_model as M
+from paper_2507_10069_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+OK, FAR = 0x1000, 0x10000000                                 # pointers that are never followed
+
+
+def _batch(arrays=True, **over):
+    kw = dict(num_reqs=2, num_q_heads=8, num_kv_heads=2, head_dim=128, page_size=16, num_pages=10, max_pages_per_req=4,
+              total_new_tokens=20, max_new_len=12, dtype="bf16", softmax_scale=0.1)
+    kw.update(over)
+    b = B.make_batch(**kw)
+    if arrays:
+        b.page_table = b.prefix_lens = b.new_lens = b.cu_new_lens = OK
+    return b
+
+
+def _rope(**over):
+    r = B.emm_rope_params(0, 128, 0, 0, (ctypes.c_int32 * 4)(0, 0, 0, 0), 1.0, 0, OK, None)
+    for k, v in over.items():
+        setattr(r, k, (ctypes.c_int32 * 4)(*v) if k == "sections" else v)
+    return r
+
+
+def _norm(**over):
+    n = B.emm_qk_norm(1e-6, 0, OK, OK)
+    for k, v in over.items():
+        setattr(n, k, v)
+    return n
+
+
+def _row_calls(b, norm, rope, q=OK, k=2 * FAR, v=3 * FAR, q_out=4 * FAR, stride=0, slots=None, k_cache=6 * FAR, v_cache=7 * FAR, cache=True):
+    """The three calls' statuses."""
+    lib = B.load()
+    norm, rope = (None if x is None else ctypes.byref(x) for x in (norm, rope))
+    c = ctypes.byref(B.emm_fp8_cache(k_cache, v_cache, 8 * FAR, 9 * FAR)) if cache else None
+    return (lib.emm_norm_rope(b, norm, rope, q, k, stride, q_out, 5 * FAR, None),
+            lib.emm_norm_rope_kv_scatter(b, norm, rope, q, k, v, stride, slots, q_out, k_cache, v_cache, None),
+            lib.emm_norm_rope_kv_scatter_fp8(b, norm, rope, q, k, v, stride, slots, q_out, c, None))
+
+
+def test_exports_match_the_header():
+    lib = B.load()
+    with open(os.path.join(ROOT, "include", "emm_step.h")) as f:
+        declared = sorted(set(re.findall(r"^emm_status (emm_[a-z_0-9]+)\(", f.read(), re.M)))
+    assert declared == sorted(B.STEP_EXPORTS)
+    for name in declared:
+        assert hasattr(lib, name), name
+
+
+def test_header_is_plain_c99_and_structs_have_its_layout(tmp_path):
+    src = tmp_path / "sizes.c"
+    src.write_text('#include "emm_step.h"\n#include <stddef.h>\n#include <stdio.h>\nint main(void) { printf("%zu %zu %zu %zu", sizeof(emm_qk_norm), '
+                   'sizeof(emm_page_step_params), offsetof(emm_page_step_params, page_table), offsetof(emm_page_step_params, refused)); return 0; }\n')
+    exe = tmp_path / "sizes"
+    subprocess.run(["gcc", "-std=c99", "-pedantic", "-Wall", "-Wextra", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()
+    S = B.emm_page_step_params
+    assert [int(x) for x in out] == [ctypes.sizeof(B.emm_qk_norm), ctypes.sizeof(S), S.page_table.offset, S.refused.offset]
+
+
+BATCHES = [(dict(num_q_heads=7), "INVALID_ARG"), (dict(softmax_scale=0.0), "INVALID_ARG"), (dict(dtype=5), "INVALID_ARG"), (dict(page_size=48), "UNSUPPORTED"),
+           (dict(head_dim=96), "UNSUPPORTED"), (dict(max_new_len=21), "INVALID_ARG"), (dict(total_new_tokens=2 ** 25 + 1), "UNSUPPORTED"),
+           (dict(num_q_heads=4098), "UNSUPPORTED"), (dict(max_pages_per_req=2 ** 27), "UNSUPPORTED")]
+
+
+@pytest.mark.parametrize("over,status", BATCHES)
+def test_bad_batches_are_refused_by_all(over, status):
+    lib, b, want, n = B.load(), _batch(**over), getattr(B, "EMM_ERR_" + status), ctypes.c_size_t()
+    assert _row_calls(b, _norm(), _rope()) == (want,) * 3
+    assert lib.emm_attn_window_workspace_size(b, 8, 0, ctypes.byref(n)) == want
+    assert lib.emm_prefill_attn_window(b, 8, 0, OK, OK, OK, OK, None, OK, 1 << 40, None) == want
+    for name in B.STEP_EXPORTS:
+        fn = getattr(lib, name)
+        numbers = (ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t)
+        assert fn(None, *[0 if t in numbers else ctypes.byref(n) if t is ctypes.POINTER(ctypes.c_size_t) else None for t in fn.argtypes[1:]]) == B.EMM_ERR_NULL
+
+
+NORMS = [(dict(eps=0.0), "INVALID_ARG"), (dict(eps=1e-39), "INVALID_ARG"), (dict(eps=-1.0), "INVALID_ARG"), (dict(eps=math.nan), "INVALID_ARG"),
+         (dict(eps=math.inf), "INVALID_ARG"), (dict(reserved=1), "INVALID_ARG"), (dict(q_weight=None), "NULL"), (dict(k_weight=None), "NULL"),
+         (dict(q_weight=OK + 8), "INVALID_ARG"), (dict(k_weight=OK + 4), "INVALID_ARG")]
+ROPES = [(dict(layout=2), "INVALID_ARG"), (dict(rotary_dim=24), "UNSUPPORTED"), (dict(positions=OK), "INVALID_ARG"), (dict(inv_freq=None), "NULL"),
+         (dict(inv_freq=OK + 4), "INVALID_ARG"), (dict(num_axes=1, sections=(64, 0, 0, 0)), "NULL"), (dict(rotary_dim=136), "INVALID_ARG")]
+
+
+def test_bad_norms_and_rotations_are_refused():
+    for over, status in NORMS:
+        assert _row_calls(_batch(), _norm(**over), _rope()) == (getattr(B, "EMM_ERR_" + status),) * 3, over
+    for over, status in ROPES:
+        assert _row_calls(_batch(), _norm(), _rope(**over)) == (getattr(B, "EMM_ERR_" + status),) * 3, over
+    assert _row_calls(_batch(), None, None) == (B.EMM_ERR_NULL,) * 3
+
+
+def test_rows_strides_overlaps_and_caches():
+    lib, b, n, r = B.load(), _batch(), _norm(), _rope()
+    invalid, null = (B.EMM_ERR_INVALID_ARG,) * 3, (B.EMM_ERR_NULL,) * 3
+    assert _row_calls(b, n, r, q=None, q_out=4 * FAR) == null
+    assert _row_calls(b, n, r, q_out=None) == null
+    assert _row_calls(b, n, r, k=None) == null
+    assert _row_calls(b, n, r, q=OK + 8) == invalid
+    assert _row_calls(b, n, r, stride=8 * 128 - 8) == invalid                # rows would overlap
+    assert _row_calls(b, n, r, stride=8 * 128 + 4) == invalid                # rows would not be aligned
+    assert _row_calls(b, n, r, stride=-4096) == invalid
+    assert _row_calls(b, n, r, stride=2 ** 60) == invalid                    # in no memory
+    assert _row_calls(b, n, r, q_out=OK, stride=12 * 128) == invalid         # in place, but strided
+    assert _row_calls(b, n, r, q_out=OK + 256) == invalid                    # shifted by a head
+    assert _row_calls(b, n, r, q_out=2 * FAR) == invalid                     # q's output over k
+    assert _row_calls(b, n, r, q_out=3 * FAR)[1:] == invalid[1:]             # over v
+    assert _row_calls(_batch(arrays=False), n, r) == null                    # positions come from the batch
+    assert _row_calls(_batch(arrays=False), n, None)[1:] == null[1:]         # slots do
+    assert _row_calls(b, n, r, k_cache=None)[1:] == null[1:]
+    assert _row_calls(b, n, r, v_cache=7 * FAR + 8)[1:] == invalid[1:]
+    assert _row_calls(b, n, r, cache=False)[2] == B.EMM_ERR_NULL
+    assert _row_calls(b, n, r, v=None)[1:] == null[1:]
+    assert _row_calls(b, n, r, slots=OK + 4)[1:] == invalid[1:]
+    assert _row_calls(_batch(num_pages=0), n, r, slots=OK)[1:] == invalid[1:]
+    assert _row_calls(_batch(max_pages_per_req=0), n, r)[1:] == invalid[1:]
+    ref = ctypes.byref
+    assert lib.emm_norm_rope(b, ref(n), ref(r), None, None, 0, None, None, None) == B.EMM_ERR_NULL
+    assert lib.emm_norm_rope(b, ref(n), ref(r), OK, 2 * FAR, 0, 4 * FAR, 4 * FAR + 512, None) == B.EMM_ERR_INVALID_ARG       # both outputs
+
+
+def test_windows_and_workspaces():
+    lib, b, n = B.load(), _batch(), ctypes.c_size_t()
+    for window, sinks in ((0, 0), (-1, 0), (5, -1)):
+        assert lib.emm_attn_window_workspace_size(b, window, sinks, ctypes.byref(n)) == B.EMM_ERR_INVALID_ARG
+        assert lib.emm_prefill_attn_window(b, window, sinks, OK, OK, OK, OK, None, OK, 1 << 40, None) == B.EMM_ERR_INVALID_ARG
+    assert lib.emm_attn_window_workspace_size(b, 8, 0, None) == B.EMM_ERR_NULL
+    assert lib.emm_decode_attn_window(b, 8, 0, OK, OK, OK, OK, None, OK, 1 << 40, None) == B.EMM_ERR_INVALID_ARG             # more than one new token
+    call = lambda bb=b, q=OK, k=OK, v=OK, out=OK, lse=None, ws=OK, nb=1 << 40: lib.emm_prefill_attn_window(bb, 8, 0, q, k, v, out, lse, ws, nb, None)
+    for name in ("q", "k", "v", "out"):
+        assert call(**{name: None}) == B.EMM_ERR_NULL and call(**{name: OK + 8}) == B.EMM_ERR_INVALID_ARG
+    assert call(ws=OK + 8) == B.EMM_ERR_INVALID_ARG and call(lse=OK + 2) == B.EMM_ERR_INVALID_ARG
+    assert call(_batch(arrays=False)) == B.EMM_ERR_NULL
+    assert call(_batch(num_pages=0)) == B.EMM_ERR_INVALID_ARG and call(_batch(max_pages_per_req=0)) == B.EMM_ERR_INVALID_ARG
+    assert call(_batch(head_dim=64)) == B.EMM_ERR_UNSUPPORTED
+    at = dict(num_reqs=2 ** 19, total_new_tokens=2 ** 19, max_new_len=1)
+    assert lib.emm_attn_window_workspace_size(_batch(**at), 8, 0, ctypes.byref(n)) == B.EMM_OK               # 2^20 pairs
+    at["num_reqs"] += 1
+    assert lib.emm_attn_window_workspace_size(_batch(**at), 8, 0, ctypes.byref(n)) == B.EMM_ERR_UNSUPPORTED
+    big = _batch(num_reqs=1, num_pages=4096, max_pages_per_req=2048, total_new_tokens=1, max_new_len=1)
+    need = B.emm_attn_window_workspace_size(big, 4096, 4)
+    assert need > 0
+    assert lib.emm_decode_attn_window(big, 4096, 4, OK, OK, OK, OK, None, None, 0, None) == B.EMM_ERR_NULL
+    assert lib.emm_decode_attn_window(big, 4096, 4, OK, OK, OK, OK, None, OK, need - 1, None) == B.EMM_ERR_WORKSPACE
+    assert B.emm_attn_window_workspace_size(_batch(dtype="f32"), 8, 0) == 0
+    # any window is taken, and what is asked for stays small
+    for window in (1, 2 ** 31 - 1):
+        for sinks in (0, 2 ** 31 - 1):
+            assert B.emm_attn_window_workspace_size(_batch(num_reqs=4, max_pages_per_req=2 ** 26), window, sinks) < 64 << 20
+
+
+def test_empty_batches_are_no_ops():
+    lib, n, r = B.load(), ctypes.byref(_norm()), ctypes.byref(_rope())
+    for b in (_batch(arrays=False, num_reqs=0, total_new_tokens=0, max_new_len=0), _batch(arrays=False, total_new_tokens=0, max_new_len=0)):
+        assert lib.emm_norm_rope(b, n, r, None, None, 0, None, None, None) == B.EMM_OK
+        assert lib.emm_norm_rope_kv_scatter(b, n, r, None, None, None, 0, None, None, None, None, None) == B.EMM_OK
+        assert lib.emm_norm_rope_kv_scatter_fp8(b, n, r, None, None, None, 0, None, None, None, None) == B.EMM_OK
+        for name in ("emm_prefill_attn_window", "emm_decode_attn_window"):
+            assert getattr(lib, name)(b, 8, 0, None, None, None, None, None, None, 0, None) == B.EMM_OK
+
+
+ARRAYS = ("page_table", "free_pages", "lens", "add_lens", "held_from", "free_count", "prefix_lens", "new_lens", "cu_new_lens", "lens_out", "held_out",
+          "free_count_out", "slots", "positions", "refused")
+
+
+def _step(**over):
+    s = B.emm_page_step_params(2, 16, 10, 4, 20, 0, 0, 0, *[FAR * (i + 1) for i in range(len(ARRAYS))])
+    for k, v in over.items():
+        setattr(s, k, v)
+    return s
+
+
+def test_bad_page_steps_are_refused():
+    lib = B.load()
+    call = lambda **over: lib.emm_page_step(ctypes.byref(_step(**over)), None)
+    for over in (dict(num_reqs=-1), dict(num_pages=0), dict(max_pages_per_req=0), dict(max_tokens=-1), dict(window=-1), dict(sinks=-1), dict(reserved=1),
+                 dict(slots=OK + 4), dict(lens=OK + 2), dict(refused=OK + 1)):
+        assert call(**over) == B.EMM_ERR_INVALID_ARG, over
+    for over in (dict(page_size=48), dict(num_reqs=4097), dict(num_pages=2 ** 28 + 1), dict(max_tokens=2 ** 25 + 1), dict(max_pages_per_req=2 ** 27)):
+        assert call(**over) == B.EMM_ERR_UNSUPPORTED, over
+    for name in ARRAYS[:-3]:
+        assert call(**{name: None}) == B.EMM_ERR_NULL, name
+    at = {n: FAR * (i + 1) for i, n in enumerate(ARRAYS)}
+    outs = ("page_table", "free_pages", "prefix_lens", "new_lens", "cu_new_lens", "lens_out", "held_out", "free_count_out", "slots", "positions", "refused")
+    mate = {"lens_out": "lens", "held_out": "held_from", "free_count_out": "free_count"}
+    for o in outs:
+        for x in ARRAYS:
+            if x != o and mate.get(o) != x:
+                assert call(**{o: at[x]}) == B.EMM_ERR_INVALID_ARG, (o, x)   # an output over another array
+    for o, x in mate.items():
+        if o != "free_count_out":
+            assert call(**{o: at[x] + 4}) == B.EMM_ERR_INVALID_ARG           # over its input, but shifted
+
+
+def test_binding_checks_tensors():
+    import torch
+    w = torch.ones(128)
+    for bad in ((w.double(), w), (w, w[:64]), (w[::2], w[::2]), (w.view(1, 128), w.view(1, 128))):
+        with pytest.raises(ValueError):
+            B.make_qk_norm(*bad, eps=1e-6)
+    norm = B.make_qk_norm(w[:64].clone(), w[:64].clone(), eps=1e-6)
+    with pytest.raises(ValueError):                          # weights of 64 channels, heads of 128
+        B.emm_norm_rope(_batch(), norm, None, None, None, None, None)
+    norm = B.make_qk_norm(w, w, eps=1e-6)
+    for slots in (torch.zeros(20, dtype=torch.int32), torch.zeros(19, dtype=torch.int64), torch.zeros(40, dtype=torch.int64)[::2]):
+        with pytest.raises(ValueError):
+            B.emm_norm_rope_kv_scatter(_batch(), norm, None, None, None, None, None, None, None, slots=slots)
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)
+    good = dict(page_table=i32(8), free_pages=i32(10), lens=i32(2), add_lens=i32(2), held_from=i32(2), free_count=i32(1), prefix_lens=i32(2), new_lens=i32(2),
+                cu_new_lens=i32(3), lens_out=i32(2), held_out=i32(2), free_count_out=i32(1), slots=torch.zeros(20, dtype=torch.int64), positions=i32(20),
+                refused=i32(1))
+    make = lambda **over: B.make_page_step(num_reqs=2, page_size=16, num_pages=10, max_pages_per_req=4, max_tokens=20, **dict(good, **over))
+    make()
+    for name, t in good.items():
+        for bad in (t[:-1], t.float(), torch.zeros(2 * t.numel() + 2, dtype=t.dtype)[::2]):
+            with pytest.raises(ValueError):
+                make(**{name: bad})
+
+
+# ---- the model that the GPU tests compare with, against itself written another way ----------------------------------
+
+def test_model_of_the_window():
+    rng = np.random.default_rng(0)
+    k, v = (rng.standard_normal((5, 1, 16, 8)) for _ in range(2))
+    table, q = np.array([[3, 0, 4, 1]]), rng.standard_normal((7, 2, 8))
+    out, lse, _ = M.window_attention(table, [45], [7], [0, 7], q, k, v, 16, 10, 3, 0.3, 7)
+    ks, vs = (x[table[0]].transpose(0, 2, 1, 3).reshape(-1, 8) for x in (k, v))
+    for j in range(7):
+        seen = [i for i in range(46 + j) if i < 3 or i > 45 + j - 10]
+        assert len(seen) == 13
+        for h in range(2):
+            s = 0.3 * ks[seen] @ q[j, h]
+            assert np.allclose(out[j, h], np.exp(s) @ vs[seen] / np.exp(s).sum()) and np.isclose(lse[j, h], np.log(np.exp(s).sum()))
+
+
+def test_model_of_the_step_keeps_every_page_once():
+    rng = np.random.default_rng(3)
+    page, width, n, pages = 16, 40, 6, 60
+    table, free = np.full((n, width), -1), rng.permutation(pages)
+    lens, held, count = [0] * n, [0] * n, pages
+    for step in range(60):
+        add = rng.integers(0, 30, n)
+        w = M.page_step(table, free, count, lens, add, held, page, 100, 4, 200)
+        table, free, count, lens, held = np.array(w["page_table"]), np.array(w["free_pages"]), w["free_count_out"][0], w["lens_out"], w["held_out"]
+        own = [table[r, e] for r in range(n) for e in list(range(min(1, -(-lens[r] // page)))) + list(range(max(1, held[r]), -(-lens[r] // page)))]
+        assert sorted(own + list(free[:count])) == list(range(pages)), step
