@@ -305,24 +305,20 @@ __global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(A
         }
         const float ref = m == -INFINITY ? 0.f : m;          // a row that has seen no key yet: its weights are zeros
         uint32_t p[KB][2][4];
+        float sum0 = 0.f, sum1 = 0.f;                        // of the weights as they are, before they are rounded for the product: lse has 32 bits
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int v = 0; v < 16; v += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kb][v], c_log2, -ref)), p1 = __builtin_amdgcn_exp2f(fmaf(s[kb][v + 1], c_log2, -ref));
+                sum0 += p0;
+                sum1 += p1;
                 bf16x2 pr;
-                pr[0] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[kb][v], c_log2, -ref));
-                pr[1] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[kb][v + 1], c_log2, -ref));
+                pr[0] = (__bf16)p0;
+                pr[1] = (__bf16)p1;
                 p[kb][v >> 3][(v & 7) >> 1] = __builtin_bit_cast(uint32_t, pr);
             }
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                sum = sum4_bf16(p[kb][h][0], p[kb][h][1], sum);
-                sum = sum4_bf16(p[kb][h][2], p[kb][h][3], sum);
-            }
-        l += sum[0];
+        l += sum0 + sum1;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -486,7 +482,20 @@ __global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(A
     }
 }
 
-// Adds the records of a row tile's parts up: a wave for a row, two channels a lane.
+// over all lanes of a wave
+__device__ inline float wave_max(float x)
+{
+    for (int n = 1; n < 64; n *= 2) x = fmaxf(x, __shfl_xor(x, n));
+    return x;
+}
+__device__ inline float wave_sum(float x)
+{
+    for (int n = 1; n < 64; n *= 2) x += __shfl_xor(x, n);
+    return x;
+}
+
+// Adds the records of a row tile's parts up: a wave for a row, two channels a lane, AT_ONCE parts' rows on their way at a time.
+constexpr int AT_ONCE = 16;
 __global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs a, WindowView w, WindowLayout L, int row_groups)
 {
     const BatchView& b = a.b;
@@ -497,18 +506,34 @@ __global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs 
     if (!find_tile<WAVE_ROWS>(b, L, w, slot, t)) return;
     if (t.row0 + row >= t.n_rows) return;
     const float* rec = (const float*)a.workspace + ((long long)unit * L.parts * WAVE_ROWS + row) * REC_STRIDE;
-    const long long stride = (long long)WAVE_ROWS * REC_STRIDE;
-    float top = -INFINITY;
-    for (int k = 0; k < L.parts; ++k) top = fmaxf(top, rec[k * stride + D]);
-    float total = 0.f, x = 0.f, y = 0.f;
-    for (int k = 0; k < L.parts; ++k) {
-        const float mk = rec[k * stride + D];
-        const float weight = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk - top);
-        typedef float f32x2 __attribute__((ext_vector_type(2)));
-        const f32x2 v = *(const f32x2*)(rec + k * stride + 2 * lane);
-        total += weight * rec[k * stride + D + 1];
-        x += weight * v[0];
-        y += weight * v[1];
+    constexpr int STRIDE = WAVE_ROWS * REC_STRIDE;
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    float top = -INFINITY, total = 0.f, x = 0.f, y = 0.f;
+    for (int k0 = 0; k0 < L.parts; k0 += 64) {
+        // lane k has the reference and the sum of part k0 + k
+        const f32x2 ml = *(const f32x2*)(rec + (long long)min(k0 + lane, L.parts - 1) * STRIDE + D);
+        const float m = k0 + lane < L.parts ? ml[0] : -INFINITY;
+        f32x2 v[AT_ONCE];
+        auto ask = [&](int k) {
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) v[u] = *(const f32x2*)(rec + (long long)min(k + u, L.parts - 1) * STRIDE + 2 * lane);
+        };
+        ask(k0);
+        const float most = fmaxf(top, wave_max(m));
+        const float before = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - most), weight = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - most);
+        top = most;
+        total = total * before + wave_sum(k0 + lane < L.parts ? weight * ml[1] : 0.f);
+        x *= before;
+        y *= before;
+        for (int k = k0; k < min(k0 + 64, L.parts); k += AT_ONCE) {
+            if (k > k0) ask(k);
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const float w_u = k + u < L.parts ? __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(weight), (k + u - k0) & 63)) : 0.f;
+                x = w_u != 0.f ? fmaf(w_u, v[u][0], x) : x;
+                y = w_u != 0.f ? fmaf(w_u, v[u][1], y) : y;
+            }
+        }
     }
     const float inv = total != 0.f ? 1.f / total : 0.f;
     const int token = L.by_G.quotient(t.row0 + row);

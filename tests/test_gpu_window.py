@@ -1,10 +1,10 @@
 """Attention with a window and sinks on the GPU against oracle/step_model.py in 64 bits.
 
-Tolerances.  bf16: weights are rounded to bf16, at most 2^-8 of themselves, in numerator and denominator: 2^-8 (sum of p |v| + |out|); the
-result is rounded: 2^-8 |out|.  A score is off by at most e = (d + 2) 2^-24 scale |q| |k| (sums of exact products in 32 bits), and
+Tolerances.  bf16: weights are rounded to bf16, at most 2^-8 of themselves, for the numerator: 2^-8 (sum of p |v|); the result is rounded:
+2^-8 |out|.  A score is off by at most e = (d + 2) 2^-24 scale |q| |k| (sums of exact products in 32 bits), and
 its exponential by 2^-20 (its argument, below 2^6 in powers of two, is rounded in 32 bits: 2^-19 ln 2; 1 unit in the last place): a
-weight changes by e + 2^-19, in numerator and denominator.  Sums over n keys in 32 bits: n 2^-24 of sum of p |v|.  lse: e + 2^-19, the denominator's
-2^-8 (bf16) and n 2^-24, 2^-22 of itself.  fp32: the same without the 2^-8, and 2^-22 |out| for the division and the result."""
+weight changes by e + 2^-19, in numerator and denominator.  Sums over n keys in 32 bits: n 2^-24 of sum of p |v|.  lse: e + 2^-19,
+n 2^-24, 2^-22 of itself.  fp32: the same without the 2^-8, and 2^-22 |out| for the division and the result."""
 import numpy as np
 import pytest
 import torch
@@ -100,13 +100,13 @@ class Case:
         e = ((self.d + 2) * 2.0 ** -24 * self.scale * np.linalg.norm(q, axis=-1) * longest)      # [T][H]
         weight = (e + 2.0 ** -19 + keys * 2.0 ** -24)
         bf16 = self.dtype == "bf16"
-        tol = (2.0 ** -8 * bf16 + weight)[..., None] * (size + np.abs(want)) + (2.0 ** -8 if bf16 else 2.0 ** -22) * np.abs(want) + 1e-30
+        tol = 2.0 ** -8 * bf16 * size + weight[..., None] * (size + np.abs(want)) + (2.0 ** -8 if bf16 else 2.0 ** -22) * np.abs(want) + 1e-30
         finite = np.isfinite(want)
         assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want)), "infinities and NaN elsewhere"
         assert np.array_equal(np.sign(got[np.isinf(want)]), np.sign(want[np.isinf(want)]))
         worst = np.where(finite, np.abs(np.where(finite, got, 0) - np.where(finite, want, 0)) / tol, 0)
         assert worst.max() <= 1, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
-        tol = 2.0 ** -8 * bf16 + weight + 2.0 ** -22 * np.abs(want_lse)
+        tol = weight + 2.0 ** -22 * np.abs(want_lse)
         ok = np.isfinite(want_lse)
         assert (np.abs(got_lse - want_lse)[ok] <= tol[ok]).all(), (np.abs(got_lse - want_lse)[ok] / tol[ok]).max()
 
