@@ -44,12 +44,15 @@ constexpr float LAG = 16.0f;                             // log2 of the largest 
 constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
 
 struct WindowLayout {
-    int G, slots;                                        // row tiles per KV head that the grid has room for
+    int G;
+    Divisor by_G, by_kv_heads;
+    // keys shape
+    int slots;                                           // row tiles per KV head that the grid has room for
     int single;                                          // 1: a request has one row tile at most, and slot r is request r's
-    int parts;                                           // of a row tile's keys (keys shape)
+    int parts;                                           // of a row tile's keys
     int per_xcd;                                         // items of an XCD, in order; 0: item i is workgroup i
     int items;
-    Divisor by_G, by_slots, by_parts, by_kv_heads;
+    Divisor by_slots, by_parts;
 };
 
 // A row tile: which request's, and the list of blocks that its rows look at
@@ -62,13 +65,34 @@ struct Tile {
     __device__ int block(int v) const { return v + (v >= sink_blocks ? gap : 0); }
 };
 
-// First row tile of request r: its ceil(rows / ROWS) tiles fit between this and the next request's, whatever cu_new_lens[r] is.
+// The tile of `rows` rows from row0 on of a request with these lengths; false: it has no such rows.
+__device__ inline bool make_tile(const BatchView& b, const WindowLayout& L, const WindowView& w, int r, long long row0, int rows, int new_len,
+                                 int prefix_len, int cu, Tile& t)
+{
+    t.r = r;
+    t.N = clamp_new_len(b, new_len, true);
+    t.n_rows = t.N * L.G;                                // (at most 2^30: see check_rows)
+    if (row0 < 0 || row0 >= t.n_rows) return false;
+    t.row0 = (int)row0;
+    t.P = clamp_prefix_len(b, prefix_len, t.N);
+    t.first_row = clamp_first_row(b, cu, t.N);
+    t.last = t.P + L.by_G.quotient(min(t.row0 + rows, t.n_rows) - 1);
+    t.low_first = window_low(w, t.P + L.by_G.quotient(t.row0));
+    t.low_last = window_low(w, t.last);
+    const int first_block = t.low_first / BLK;
+    t.sink_blocks = min((int)(((uint32_t)w.sinks + BLK - 1) / BLK), first_block);
+    t.gap = first_block - t.sink_blocks;
+    t.blocks = t.last / BLK + 1 - t.gap;
+    return true;
+}
+
+// ---- Keys shape: slots.  First row tile of request r: its ceil(rows / ROWS) tiles fit between this and the next request's, whatever cu_new_lens[r] is.
 template <int ROWS> __device__ inline long long first_slot(int cu_new, int G, int r) { return (long long)max(cu_new, 0) * G / ROWS + r; }
 
 // The tile in `slot`; false: there is none.  Uniform over the workgroup.
 template <int ROWS> __device__ inline bool find_tile(const BatchView& b, const WindowLayout& L, const WindowView& w, int slot, Tile& t)
 {
-    int r = slot, row0 = 0;
+    int r = slot;
     if (!L.single) {
         int lo = 0, hi = b.num_reqs;
         while (hi - lo > 1) {
@@ -78,65 +102,103 @@ template <int ROWS> __device__ inline bool find_tile(const BatchView& b, const W
         r = lo;
     }
     const int new_len = b.new_lens[r], prefix_len = b.prefix_lens[r], cu = b.cu_new_lens[r];
-    t.r = r;
-    t.N = clamp_new_len(b, new_len, true);
-    t.n_rows = t.N * L.G;                                // (at most 2^30: see check_rows)
-    if (!L.single) {
-        const long long at = ((long long)slot - first_slot<ROWS>(cu, L.G, r)) * ROWS;
-        if (at < 0 || at >= t.n_rows) return false;
-        row0 = (int)at;
-    }
-    if (row0 >= t.n_rows) return false;
-    t.row0 = row0;
-    t.P = clamp_prefix_len(b, prefix_len, t.N);
-    t.first_row = clamp_first_row(b, cu, t.N);
-    t.last = t.P + L.by_G.quotient(min(row0 + ROWS, t.n_rows) - 1);
-    t.low_first = window_low(w, t.P + L.by_G.quotient(row0));
-    t.low_last = window_low(w, t.last);
-    const int first_block = t.low_first / BLK;
-    t.sink_blocks = min((int)(((uint32_t)w.sinks + BLK - 1) / BLK), first_block);
-    t.gap = first_block - t.sink_blocks;
-    t.blocks = t.last / BLK + 1 - t.gap;
-    return true;
+    const long long row0 = L.single ? 0 : ((long long)slot - first_slot<ROWS>(cu, L.G, r)) * ROWS;
+    return make_tile(b, L, w, r, row0, ROWS, new_len, prefix_len, cu, t);
 }
+
+// ---- Rows shape: units.  A unit is a row tile of a KV head; they are counted head by head, request by request, and each XCD has an eighth of
+// them, neighbours, which mostly read the same keys.  It holds SLOTS workgroups at once, and units take about equally long (a window), so that with
+// few units in the last round most of its places would idle: such units are halved.  A workgroup then has 64 rows, two waves to 32 of them, which take a half
+// of each tile's keys each and meet in LDS.  Everybody derives the same plan from the lengths.
+constexpr int SLOTS = 64, MOST_HALVED = 32;
+struct RowsPlan {
+    int first, units, whole;                             // of an XCD: its first unit, all of them, those that are not halved
+};
+__device__ inline RowsPlan rows_plan(int total, int xcd)
+{
+    RowsPlan p;
+    p.first = (int)((long long)xcd * total / NUM_XCD);
+    p.units = (int)((long long)(xcd + 1) * total / NUM_XCD) - p.first;
+    const int full = p.units / SLOTS * SLOTS;
+    p.whole = p.units - full <= MOST_HALVED ? full : p.units;
+    return p;
+}
+// running sums over the wave's lanes, inclusive
+__device__ inline int scan64(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // row 0's sum to row 1, row 2's to row 3,
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);     // and row 1's to rows 2 and 3
+    return x;
+}
+// The row tiles of 64 requests from `from` on, as the lanes see them
+struct Lines {
+    const BatchView& b;
+    int new_len, prefix_len, cu, incl;
+    __device__ int look(const WindowLayout& L, int from) // returns their number
+    {
+        const int lane = threadIdx.x & 63, r = min(from + lane, b.num_reqs - 1);
+        new_len = b.new_lens[r];
+        prefix_len = b.prefix_lens[r];
+        cu = b.cu_new_lens[r];
+        incl = scan64(from + lane < b.num_reqs ? (clamp_new_len(b, new_len, true) * L.G + WIDE_ROWS - 1) / WIDE_ROWS : 0);
+        return __builtin_amdgcn_readlane(incl, 63);
+    }
+    __device__ int total(const WindowLayout& L)
+    {
+        int sum = 0;
+        for (int from = 0; from < b.num_reqs; from += 64) sum += look(L, from);
+        return sum;
+    }
+    // the n-th row tile of all, n < total(); half 0 or 1: that half of its rows
+    __device__ bool take(const WindowLayout& L, const WindowView& w, int n, int half, Tile& t)
+    {
+        int from = 0;
+        if (b.num_reqs > 64) {
+            for (int count = look(L, 0); n >= count && from + 64 < b.num_reqs; count = look(L, from)) {
+                n -= count;
+                from += 64;
+            }
+        }
+        const unsigned long long hit = __builtin_amdgcn_ballot_w64(incl > n);
+        if (hit == 0) return false;
+        const int at = __builtin_ctzll(hit);
+        const int length = __builtin_amdgcn_readlane(new_len, at), tiles = (clamp_new_len(b, length, true) * L.G + WIDE_ROWS - 1) / WIDE_ROWS;
+        const int tile = n - (__builtin_amdgcn_readlane(incl, at) - tiles);
+        return make_tile(b, L, w, from + at, (long long)tile * WIDE_ROWS + max(half, 0) * (WIDE_ROWS / 2), half >= 0 ? WIDE_ROWS / 2 : WIDE_ROWS, length,
+                         __builtin_amdgcn_readlane(prefix_len, at), __builtin_amdgcn_readlane(cu, at), t);
+    }
+};
 
 __device__ inline bool is_finite_bf16(uint32_t half) { return (half & 0x7f80u) != 0x7f80u; }
 
-template <bool KEYS>
-__global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(AttnArgs a, WindowView w, WindowLayout L)
+enum Shape { ROWS, HALVED /* rows, of half a unit */, KEYS };
+template <int SHAPE> struct Sizes {
+    static constexpr int TILE = SHAPE == KEYS ? 32 : 64;                     // keys of a tile
+    static constexpr int TILE_BYTES = TILE * D * 2;                          // of K, or of V
+    static constexpr int RING = 4 * TILE_BYTES;                              // two slots of K and V
+    static constexpr int LDS = SHAPE == KEYS ? WAVES * RING : RING;
+};
+
+// The rows of tile t by the workgroup.  KEYS: part `part` of its keys, of a row tile in `slot`.  bad_s: rows shape, keys of a tile's blocks whose V holds
+// an infinity or NaN.
+template <int SHAPE>
+__device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView& w, const WindowLayout& L, const Tile& t, int kvh, int slot, int part,
+                                            unsigned char* smem, int (*bad_s)[WAVES])
 {
-    constexpr int ROWS = KEYS ? WAVE_ROWS : WIDE_ROWS;
-    constexpr int BC_ = KEYS ? 32 : 64;                  // keys of a tile
-    constexpr int KB = BC_ / 32, TB = BC_ / BLK;         // 32-key parts and blocks of a tile
-    constexpr int TILE_BYTES = BC_ * D * 2;              // of K, or of V
-    constexpr int RING = 4 * TILE_BYTES;                 // two slots of K and V
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[KEYS ? WAVES * RING : RING];
-    __shared__ int bad_s[2][WAVES];                      // rows shape: keys of a tile's blocks whose V holds an infinity or NaN
+    constexpr bool KEYS = SHAPE == Shape::KEYS, HALVED = SHAPE == Shape::HALVED;
+    constexpr int TB = Sizes<SHAPE>::TILE / BLK, TILE_BYTES = Sizes<SHAPE>::TILE_BYTES, RING = Sizes<SHAPE>::RING;
+    constexpr int KB = SHAPE == ROWS ? 2 : 1;            // 32-key parts of a tile that a wave takes
     const BatchView& b = a.b;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, h32 = lane >> 5;
-
-    int item = blockIdx.x;
-    if (L.per_xcd > 0) item = (blockIdx.x % NUM_XCD) * L.per_xcd + blockIdx.x / NUM_XCD;
-    if (item >= L.items) return;
-    int part = 0, slot, kvh;
-    if (L.per_xcd > 0) {                                 // neighbours share a KV head, and mostly a request
-        const int group = L.by_slots.quotient(item);
-        slot = item - group * L.slots;
-        kvh = KEYS ? L.by_parts.quotient(group) : group;
-        if (KEYS) part = group - kvh * L.parts;
-    } else {
-        const int pair = KEYS ? L.by_parts.quotient(item) : item;
-        if (KEYS) part = item - pair * L.parts;
-        slot = L.by_kv_heads.quotient(pair);
-        kvh = pair - slot * b.num_kv_heads;
-    }
-    Tile t;
-    if (!find_tile<ROWS>(b, L, w, slot, t)) return;
     const int G = L.G;
 
-    // this workgroup's tiles (KEYS: of its part), and of those this wave's
+    // this workgroup's tiles, and of those this wave's
     const int all_tiles = (t.blocks + TB - 1) / TB;
     int t_begin = 0, t_end = all_tiles;
     if (KEYS) {
@@ -147,7 +209,8 @@ __global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(A
     const int step = KEYS ? WAVES : 1, t_first = KEYS ? t_begin + wave : 0;
     const int n_mine = t_end > t_first ? (t_end - t_first + step - 1) / step : 0;
 
-    const int wrow0 = t.row0 + (KEYS ? 0 : wave * WAVE_ROWS);
+    const int wrow0 = t.row0 + (KEYS ? 0 : HALVED ? wave >> 1 : wave) * WAVE_ROWS;
+    const int kb0 = HALVED ? wave & 1 : 0;               // of a tile's 32-key parts the first that this wave takes
     const bool active = wrow0 < t.n_rows;                // (a wave without rows only fetches)
     const int row_c = min(wrow0 + l32, t.n_rows - 1);
     const int tok = L.by_G.quotient(row_c);
@@ -259,7 +322,7 @@ __global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(A
 
     auto attend = [&](int i) {
         const int buf = i & 1, tile = t_first + i * step;
-        const unsigned char* tiles = my_ring + buf * TILE_BYTES;
+        const unsigned char* tiles = my_ring + buf * TILE_BYTES + kb0 * 32 * 256;
         f32x16 s[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -277,7 +340,7 @@ __global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(A
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int key0 = t.block(tile * TB + 2 * kb + h) * BLK + 8 * h32;
+                    const int key0 = t.block(tile * TB + 2 * (kb0 + kb) + h) * BLK + 8 * h32;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const int key = key0 + e;
@@ -388,7 +451,7 @@ __global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(A
                         for (int which = 0; which < PER_TILE; ++which)
                             if (bad[which] != 0) add_odd(tile * TB + which, bad[which]);
                     } else {
-                        for (int k = 0; k < WAVES; ++k) {
+                        for (int k = 2 * kb0; k < (HALVED ? 2 * kb0 + 2 : TB); ++k) {
                             const int those = __builtin_amdgcn_readfirstlane(bad_s[i & 1][k]);
                             if (those != 0) add_odd(tile * TB + k, those);
                         }
@@ -406,8 +469,39 @@ __global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(A
 
     if constexpr (!KEYS) {
         // out through LDS, so that an instruction stores four whole rows
-        if (!active) return;
-        const float inv = l_row != 0.f ? 1.f / l_row : 0.f;  // (a row sees itself)
+        float l_all = l_row;
+        if constexpr (HALVED) {
+            // the second wave's sums to the first, lane by lane
+            float* theirs = (float*)smem + (wave >> 1) * 64 * 66;
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            if (kb0 == 1) {
+#pragma unroll
+                for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+                    for (int v4 = 0; v4 < 4; ++v4)
+                        *(f32x4*)(theirs + ((4 * nb + v4) * 64 + lane) * 4) = f32x4{o[nb][4 * v4], o[nb][4 * v4 + 1], o[nb][4 * v4 + 2], o[nb][4 * v4 + 3]};
+                *(f32x2*)(theirs + 64 * 64 + 2 * lane) = f32x2{m, l_row};
+            }
+            __syncthreads();
+            if (kb0 == 0) {
+                const f32x2 ml = *(const f32x2*)(theirs + 64 * 64 + 2 * lane);
+                const float top = fmaxf(m, ml[0]);
+                const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), other = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
+                m = top;
+                l_all = l_row * mine + ml[1] * other;
+#pragma unroll
+                for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+                    for (int v4 = 0; v4 < 4; ++v4) {
+                        const f32x4 x = *(const f32x4*)(theirs + ((4 * nb + v4) * 64 + lane) * 4);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[nb][4 * v4 + e] = o[nb][4 * v4 + e] * mine + x[e] * other;
+                    }
+            }
+            __syncthreads();                                 // what is staged next lies there
+        }
+        if (!active || kb0 != 0) return;
+        const float inv = l_all != 0.f ? 1.f / l_all : 0.f;  // (a row sees itself)
         unsigned char* stage = smem + wave * (32 * OUT_STRIDE);
 #pragma unroll
         for (int nb = 0; nb < 4; ++nb)
@@ -418,7 +512,7 @@ __global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(A
                 for (int e = 0; e < 4; ++e) x[e] = (__bf16)(o[nb][4 * v4 + e] * inv);
                 *(bf16x4*)(stage + l32 * OUT_STRIDE + 2 * (32 * nb + 8 * v4 + 4 * h32)) = x;
             }
-        if (a.lse != nullptr && h32 == 0 && wrow0 + l32 < t.n_rows) a.lse[at_row(wrow0 + l32)] = m * LN2 + logf(l_row);
+        if (a.lse != nullptr && h32 == 0 && wrow0 + l32 < t.n_rows) a.lse[at_row(wrow0 + l32)] = m * LN2 + logf(l_all);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -479,6 +573,43 @@ __global__ __launch_bounds__(64 * WAVES, KEYS ? 1 : 2) void attn_window_kernel(A
             *(bf16x4*)((__bf16*)a.out + at * D + ch + 32 * x) = y;
         }
         if (a.lse != nullptr && ch == 0) a.lse[at] = top * LN2 + logf(total);
+    }
+}
+
+template <bool BY_KEYS>
+__global__ __launch_bounds__(64 * WAVES, BY_KEYS ? 1 : 2) void attn_window_kernel(AttnArgs a, WindowView w, WindowLayout L)
+{
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[Sizes<BY_KEYS ? KEYS : ROWS>::LDS];
+    const BatchView& b = a.b;
+    Tile t;
+    if constexpr (BY_KEYS) {
+        int item = blockIdx.x, slot, part, kvh;
+        if (L.per_xcd > 0) item = (blockIdx.x % NUM_XCD) * L.per_xcd + blockIdx.x / NUM_XCD;
+        if (item >= L.items) return;
+        if (L.per_xcd > 0) {                             // neighbours share a KV head, and mostly a request
+            const int group = L.by_slots.quotient(item);
+            slot = item - group * L.slots;
+            kvh = L.by_parts.quotient(group);
+            part = group - kvh * L.parts;
+        } else {
+            const int pair = L.by_parts.quotient(item);
+            part = item - pair * L.parts;
+            slot = L.by_kv_heads.quotient(pair);
+            kvh = pair - slot * b.num_kv_heads;
+        }
+        if (find_tile<WAVE_ROWS>(b, L, w, slot, t)) attend_tile<KEYS>(a, w, L, t, kvh, slot, part, smem, nullptr);
+    } else {
+        __shared__ int bad_s[2][WAVES];
+        Lines lines = {b};
+        const int tiles = lines.total(L), i = blockIdx.x / NUM_XCD;
+        const RowsPlan plan = rows_plan(tiles * b.num_kv_heads, blockIdx.x % NUM_XCD);
+        const bool whole = i < plan.whole;
+        const int nth = whole ? i : plan.whole + ((i - plan.whole) >> 1);
+        if (nth >= plan.units) return;
+        const int unit = plan.first + nth, kvh = unit / tiles;
+        if (!lines.take(L, w, unit - kvh * tiles, whole ? -1 : (i - plan.whole) & 1, t)) return;
+        if (whole) attend_tile<ROWS>(a, w, L, t, kvh, 0, 0, smem, bad_s);
+        else attend_tile<HALVED>(a, w, L, t, kvh, 0, 0, smem, bad_s);
     }
 }
 
@@ -548,39 +679,44 @@ __global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs 
 constexpr int COMPUTE_UNITS = 256;
 
 // How a batch is dealt, from what the host knows.  keys: which of the two shapes
-struct Shape {
+struct Deal {
     bool keys;
     WindowLayout L;
-    long long items;
+    long long grid;
+    size_t workspace;
 };
-Shape shape_of(const BatchView& b, const WindowView& w)
+Deal deal_of(const BatchView& b, const WindowView& w)
 {
-    Shape s = {};
+    Deal s = {};
     const int G = b.num_q_heads / b.num_kv_heads;
-    auto slots_of = [&](int rows) { return (long long)b.total_new_tokens * G / rows + b.num_reqs; };
+    const long long rows = (long long)b.total_new_tokens * G;
     const bool single = (long long)b.max_new_len * G <= WAVE_ROWS;
-    const long long wide = ((long long)b.total_new_tokens * G + WIDE_ROWS - 1) / WIDE_ROWS * b.num_kv_heads;     // at least
-    s.keys = single || wide < COMPUTE_UNITS;
-    const long long slots = s.keys ? (single ? b.num_reqs : slots_of(WAVE_ROWS)) : slots_of(WIDE_ROWS);
+    const long long wide = (rows + WIDE_ROWS - 1) / WIDE_ROWS * b.num_kv_heads;     // units of the rows shape, at least
     s.L.G = G;
-    s.L.slots = (int)slots;
-    s.L.single = s.keys && single;
-    s.L.parts = 1;
-    if (s.keys) {
-        // as many parts as fill the chip, each of a tile for every wave at least
-        const long long span = std::min((long long)b.max_pages * b.page_size, (long long)w.window + w.sinks + WAVE_ROWS);
-        const long long tiles = (span + 31) / 32;
-        const long long units = std::max(((long long)b.total_new_tokens * G + WAVE_ROWS - 1) / WAVE_ROWS, 1ll) * b.num_kv_heads;
-        const long long real = single ? slots * b.num_kv_heads : units;
-        s.L.parts = (int)std::max(1ll, std::min(COMPUTE_UNITS / std::max(real, 1ll), (tiles + WAVES - 1) / WAVES));
-    }
-    s.items = slots * b.num_kv_heads * s.L.parts;
-    s.L.items = (int)s.items;
-    s.L.per_xcd = s.L.single ? 0 : (int)((s.items + NUM_XCD - 1) / NUM_XCD);
     s.L.by_G = divisor_of(G);
+    s.L.by_kv_heads = divisor_of(b.num_kv_heads);
+    s.keys = single || wide < COMPUTE_UNITS;
+    // the most that a row tile looks at
+    const long long span = std::min((long long)b.max_pages * b.page_size, (long long)w.window + w.sinks + WAVE_ROWS / G + 1);
+    if (!s.keys) {
+        // (a halved unit is two workgroups)
+        const long long units = (rows / WIDE_ROWS + b.num_reqs) * b.num_kv_heads;
+        s.grid = ((units + NUM_XCD - 1) / NUM_XCD + MOST_HALVED) * NUM_XCD;
+        return s;
+    }
+    const long long slots = single ? b.num_reqs : rows / WAVE_ROWS + b.num_reqs;
+    s.L.slots = (int)slots;
+    s.L.single = single;
+    // as many parts as fill the chip, each of a tile for every wave at least
+    const long long tiles = (span + 31) / 32, units = (single ? slots : std::max((rows + WAVE_ROWS - 1) / WAVE_ROWS, 1ll)) * b.num_kv_heads;
+    s.L.parts = (int)std::max(1ll, std::min(COMPUTE_UNITS / units, (tiles + WAVES - 1) / WAVES));
+    const long long items = slots * b.num_kv_heads * s.L.parts;
+    s.L.items = (int)items;
+    s.L.per_xcd = single ? 0 : (int)((items + NUM_XCD - 1) / NUM_XCD);
     s.L.by_slots = divisor_of((int)slots);
     s.L.by_parts = divisor_of(s.L.parts);
-    s.L.by_kv_heads = divisor_of(b.num_kv_heads);
+    s.grid = single ? items : (long long)s.L.per_xcd * NUM_XCD;
+    s.workspace = s.L.parts > 1 ? (size_t)items * WAVE_ROWS * REC_STRIDE * sizeof(float) : 0;
     return s;
 }
 
@@ -588,26 +724,21 @@ Shape shape_of(const BatchView& b, const WindowView& w)
 
 size_t attn_window_workspace_bytes(const BatchView& b, const WindowView& w)
 {
-    if (b.total_new_tokens == 0 || b.num_reqs == 0) return 0;
-    const Shape s = shape_of(b, w);
-    return s.L.parts > 1 ? (size_t)s.items * WAVE_ROWS * REC_STRIDE * sizeof(float) : 0;
+    return b.total_new_tokens == 0 || b.num_reqs == 0 ? 0 : deal_of(b, w).workspace;
 }
 
 hipError_t launch_attn_window(const AttnArgs& a, const WindowView& w, hipStream_t stream)
 {
     const BatchView& b = a.b;
-    const Shape s = shape_of(b, w);
-    const long long grid = s.L.per_xcd > 0 ? (long long)s.L.per_xcd * NUM_XCD : s.items;
-    if (grid > 0x3fffffff) return hipErrorInvalidValue;
-    if (!s.keys) {
-        hipLaunchKernelGGL((attn_window_kernel<false>), dim3((unsigned)grid), dim3(64 * WAVES), 0, stream, a, w, s.L);
-        return hipGetLastError();
-    }
-    hipLaunchKernelGGL((attn_window_kernel<true>), dim3((unsigned)grid), dim3(64 * WAVES), 0, stream, a, w, s.L);
+    const Deal s = deal_of(b, w);
+    if (s.grid > 0x3fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)s.grid), block(64 * WAVES);
+    if (s.keys) hipLaunchKernelGGL((attn_window_kernel<true>), grid, block, 0, stream, a, w, s.L);
+    else hipLaunchKernelGGL((attn_window_kernel<false>), grid, block, 0, stream, a, w, s.L);
     const hipError_t err = hipGetLastError();
-    if (err != hipSuccess || s.L.parts == 1) return err;
+    if (err != hipSuccess || s.workspace == 0) return err;
     const int rows = (int)std::min<long long>((long long)b.max_new_len * s.L.G, WAVE_ROWS), groups = (rows + WAVES - 1) / WAVES;
-    hipLaunchKernelGGL(attn_window_merge_kernel, dim3((unsigned)(s.L.slots * b.num_kv_heads * groups)), dim3(64 * WAVES), 0, stream, a, w, s.L, groups);
+    hipLaunchKernelGGL(attn_window_merge_kernel, dim3((unsigned)(s.L.slots * b.num_kv_heads * groups)), block, 0, stream, a, w, s.L, groups);
     return hipGetLastError();
 }
 

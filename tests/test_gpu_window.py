@@ -148,10 +148,15 @@ def test_head_layouts_and_pages(heads, kv_heads, page):
 @pytest.mark.parametrize("window,sinks,page", [(1, 0, 16), (40, 4, 16), (128, 0, 64), (500, 130, 32), (1000, 16, 256), (HUGE, 0, 16)])
 @pytest.mark.parametrize("heads,kv_heads", [(28, 4), (32, 8), (16, 16)])
 def test_large_prompts(window, sinks, page, heads, kv_heads):
-    """Row tiles of 128 rows whose waves share their keys."""
-    case = Case([700, 0, 33], [400, 900, 801], window, sinks, heads=heads, kv_heads=kv_heads, page=page, seed=heads + window % 13, extra_rows=5).to_device()
-    assert case.workspace is None
-    case.run_and_check()
+    """Row tiles of 128 rows whose waves share their keys; the last ones of an XCD are cut where they are few."""
+    Case([700, 0, 33], [400, 900, 801], window, sinks, heads=heads, kv_heads=kv_heads, page=page, seed=heads + window % 13, extra_rows=5).run_and_check()
+
+
+@pytest.mark.parametrize("new,window", [([1180, 1180, 1180], 300), ([2400, 5, 77], 200), ([40] * 70, 500), ([1200] * 2 + [0] * 200, 700)])
+def test_cut_tails_and_many_requests(new, window):
+    """65 to 96 row tiles on an XCD, of which the last are cut into many parts or few; requests beyond those that a wave sees at a time."""
+    rng = np.random.default_rng(len(new))
+    Case(rng.integers(0, 900, len(new)).tolist(), new, window, 7, seed=len(new)).run_and_check()
 
 
 def test_one_context_is_cut_into_parts():
