@@ -173,6 +173,19 @@ struct Lines {
     }
 };
 
+// compile-time loop: f(integral_constant<int, I>) for I = BEGIN .. END-1
+template <int BEGIN, int END, class F>
+__device__ __forceinline__ void static_for(F&& f)
+{
+    if constexpr (BEGIN < END) {
+        f(std::integral_constant<int, BEGIN>{});
+        static_for<BEGIN + 1, END>(f);
+    }
+}
+// Ties a value to the place where it is written: the optimiser would gather such work in one clump elsewhere.  Emits nothing.
+__device__ __forceinline__ void pin(float& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
 __device__ inline bool is_finite_bf16(uint32_t half) { return (half & 0x7f80u) != 0x7f80u; }
 
 enum Shape { ROWS, HALVED /* rows, of half a unit */, KEYS };
@@ -256,16 +269,23 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
         const uint32_t lo = __builtin_amdgcn_readlane((int)id_vec, at), hi = __builtin_amdgcn_readlane((int)(id_vec >> 32), at);
         return (long long)(((unsigned long long)hi << 32) | lo) * SLAB;
     };
-    auto fetch = [&](int i) {                                // this wave's share of its tile i (KEYS: all of it)
-        const int buf = i & 1;
+    // this wave's share of its tile i (KEYS: all of it), into slot i % 2
+    auto fetch_k = [&](int i) {
 #pragma unroll
         for (int which = 0; which < PER_TILE; ++which) {
-            const long long at = slab(i, which);
-            const uint32_t to = ring + buf * TILE_BYTES + (KEYS ? which : wave) * SLAB;
+            const unsigned char* from = kcb + slab(i, which);
+            const uint32_t to = ring + (i & 1) * TILE_BYTES + (KEYS ? which : wave) * SLAB;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) lds_dma16(kcb + at, k_goff[j], to + j * 1024);
+            for (int j = 0; j < 4; ++j) lds_dma16(from, k_goff[j], to + j * 1024);
+        }
+    };
+    auto fetch_v = [&](int i) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) lds_dma16(vcb + at, v_goff + j * 1024, to + 2 * TILE_BYTES + j * 1024);
+        for (int which = 0; which < PER_TILE; ++which) {
+            const unsigned char* from = vcb + slab(i, which);
+            const uint32_t to = ring + (2 + (i & 1)) * TILE_BYTES + (KEYS ? which : wave) * SLAB;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) lds_dma16(from, v_goff + j * 1024, to + j * 1024);
         }
     };
     // is block v of the list seen whole by all rows of this wave?  (by all of a tile's blocks: no masks)
@@ -320,54 +340,63 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[nb][v] = 0.f;
 
-    auto attend = [&](int i) {
-        const int buf = i & 1, tile = t_first + i * step;
-        const unsigned char* tiles = my_ring + buf * TILE_BYTES + kb0 * 32 * 256;
-        f32x16 s[KB];
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
+    // S^T = K Q^T of this wave's tile i
+    auto multiply_k = [&](int i, f32x16 (&s)[KB]) {
+        const unsigned char* k = my_ring + (i & 1) * TILE_BYTES + kb0 * 32 * 256;
 #pragma unroll
         for (int st = 0; st < 8; ++st)
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const bf16x8 kf = *(const bf16x8*)(tiles + kb * 32 * 256 + (k_rd ^ (st << 5)));
-                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[kb], 0, 0, 0);
-            }
-        if (!clear(tile)) {
+                const bf16x8 kf = *(const bf16x8*)(k + kb * 32 * 256 + (k_rd ^ (st << 5)));
+                if (st == 0) {
+                    f32x16 zero;
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int key0 = t.block(tile * TB + 2 * (kb0 + kb) + h) * BLK + 8 * h32;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int key = key0 + e;
-                        const bool seen = key <= limit && (key >= low || key < w.sinks);
-                        s[kb][8 * h + e] = seen ? s[kb][8 * h + e] : -INFINITY;
-                    }
+                    for (int v = 0; v < 16; ++v) zero[v] = 0.f;
+                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], zero, 0, 0, 0);
+                } else {
+                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[kb], 0, 0, 0);
                 }
-        }
+            }
+    };
+    auto mask = [&](int tile, f32x16 (&s)[KB]) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int key0 = t.block(tile * TB + 2 * (kb0 + kb) + h) * BLK + 8 * h32;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int key = key0 + e;
+                    const bool seen = key <= limit && (key >= low || key < w.sinks);
+                    s[kb][8 * h + e] = seen ? s[kb][8 * h + e] : -INFINITY;
+                }
+            }
+    };
+    auto top_of = [&](const f32x16 (&s)[KB]) {               // the largest of this lane's scores
         float top = s[0][0];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int v = 0; v < 16; ++v) top = fmaxf(top, s[kb][v]);
-        top *= c_log2;
+        return top * c_log2;
+    };
+    // scores whose largest in this lane is `top` are next: is the reference far enough up?
+    auto raise = [&](float top) {
         if (__builtin_amdgcn_ballot_w64(top > m + LAG) != 0) {
             const float both = pair_max(top);                // (both halves of a row decide alike)
-            const bool raise = both > m + LAG;
-            const float alpha = raise ? __builtin_amdgcn_exp2f(m - both) : 1.f;
-            m = raise ? both : m;
+            const bool up = both > m + LAG;
+            const float alpha = up ? __builtin_amdgcn_exp2f(m - both) : 1.f;
+            m = up ? both : m;
             l *= alpha;
 #pragma unroll
             for (int nb = 0; nb < 4; ++nb)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) o[nb][v] *= alpha;
         }
+    };
+    typedef uint32_t Weights[KB][2][4];
+    auto weigh = [&](const f32x16 (&s)[KB], Weights& p) {
         const float ref = m == -INFINITY ? 0.f : m;          // a row that has seen no key yet: its weights are zeros
-        uint32_t p[KB][2][4];
         float sum0 = 0.f, sum1 = 0.f;                        // of the weights as they are, before they are rounded for the product: lse has 32 bits
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -382,6 +411,10 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
                 p[kb][v >> 3][(v & 7) >> 1] = __builtin_bit_cast(uint32_t, pr);
             }
         l += sum0 + sum1;
+    };
+    // O^T += V^T P^T
+    auto multiply_v = [&](int i, const Weights& p) {
+        const unsigned char* tile = my_ring + (i & 1) * TILE_BYTES + kb0 * 32 * 256;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -392,7 +425,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
 #pragma unroll
                 for (int nb = 0; nb < 4; ++nb) {
                     typedef short s16x4 __attribute__((ext_vector_type(4)));
-                    const unsigned char* src = tiles + (32 * kb + 16 * h) * 256 + (v_rd ^ (nb << 6));
+                    const unsigned char* src = tile + (32 * kb + 16 * h) * 256 + (v_rd ^ (nb << 6));
                     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src));
                     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src + 4 * 256));
                     const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -421,43 +454,181 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     };
 
     if (n_mine > 0) {
+        // Tile i + 1's scores are made while tile i's become weights: K is a tile ahead of V.
+        f32x16 s0[KB], s1[KB];
+        float top = 0.f;
         refill(0);
-        fetch(0);
-        for (int i = 0; i < n_mine; ++i) {
+        fetch_k(0);
+        fetch_v(0);
+        if (n_mine > 1) fetch_k(1);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if constexpr (!KEYS) __syncthreads();
+        if (active) {
+            multiply_k(0, s0);
+            if (!clear(t_first)) mask(t_first, s0);
+            top = top_of(s0);
+        }
+        // V(i) and K(i + 1) are there, the next ones are asked for; returns the keys of V(i) whose values are not all finite
+        struct Bad { int of[PER_TILE]; bool look; };
+        auto arrive = [&](int i) -> Bad {
             const int tile = t_first + i * step;
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // this wave's share of tile i has landed
-            int bad[PER_TILE] = {};
-            const bool look = !wg_clear(tile);
-            if (look) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            Bad bad = {};
+            bad.look = !wg_clear(tile);
+            if (bad.look) {
 #pragma unroll
                 for (int which = 0; which < PER_TILE; ++which)
-                    bad[which] = look_at_v(tile * TB + (KEYS ? which : wave), my_ring + 2 * TILE_BYTES + (i & 1) * TILE_BYTES + (KEYS ? which : wave) * SLAB);
-                if (!KEYS && lane == 0) bad_s[i & 1][wave] = bad[0];
+                    bad.of[which] = look_at_v(tile * TB + (KEYS ? which : wave), my_ring + (2 + (i & 1)) * TILE_BYTES + (KEYS ? which : wave) * SLAB);
+                if (!KEYS && lane == 0) bad_s[i & 1][wave] = bad.of[0];
             }
             if constexpr (KEYS) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // all reads of the other slot are done, and V's zeros are written
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // all reads of the other slots are done, and V's zeros are written
             } else {
-                __syncthreads();                             // everyone's share; and everyone is past its reads of the other slot
+                __syncthreads();                             // everyone's share; and everyone is past its reads of the other slots
             }
-            if (i + 1 < n_mine) {
-                if (i + 1 - id_base >= IDS) refill(i + 1);
-                fetch(i + 1);
-            }
-            if (active) {
-                attend(i);
-                if (look) {
-                    if constexpr (KEYS) {
+            if (i + 2 < n_mine && i + 2 - id_base >= IDS) refill(i + 1);
+            if (i + 1 < n_mine) fetch_v(i + 1);
+            if (i + 2 < n_mine) fetch_k(i + 2);
+            return bad;
+        };
+        auto add_bad = [&](int i, const Bad& bad) {
+            if (!bad.look) return;
+            const int tile = t_first + i * step;
+            if constexpr (KEYS) {
 #pragma unroll
-                        for (int which = 0; which < PER_TILE; ++which)
-                            if (bad[which] != 0) add_odd(tile * TB + which, bad[which]);
-                    } else {
-                        for (int k = 2 * kb0; k < (HALVED ? 2 * kb0 + 2 : TB); ++k) {
-                            const int those = __builtin_amdgcn_readfirstlane(bad_s[i & 1][k]);
-                            if (those != 0) add_odd(tile * TB + k, those);
-                        }
-                    }
+                for (int which = 0; which < PER_TILE; ++which)
+                    if (bad.of[which] != 0) add_odd(tile * TB + which, bad.of[which]);
+            } else {
+                for (int k = 2 * kb0; k < (HALVED ? 2 * kb0 + 2 : TB); ++k) {
+                    const int those = __builtin_amdgcn_readfirstlane(bad_s[i & 1][k]);
+                    if (those != 0) add_odd(tile * TB + k, those);
                 }
             }
+        };
+        // One MFMA a slice, fenced, so that the order is the one written here: the matrix pipe has an instruction in every slice, its operand
+        // was read from LDS AHEAD slices before, and the softmax fills the slots between.
+        //   8 KB slices   S^T(i + 1) = K Q^T, and tile i's weights, a pair a slice: scaled, exponentials, then sums and rounding, a slice apart each
+        //   8 KB slices   O^T += V^T P^T, and the largest of the new scores
+        auto iteration = [&](int i, auto parity, f32x16 (&now)[KB], f32x16 (&next)[KB]) {
+            constexpr int R = decltype(parity)::value, N = 8 * KB, AHEAD = 2;
+            const Bad bad = arrive(i);
+            if (!active) return;
+            const unsigned char* k_tile = my_ring + (R ^ 1) * TILE_BYTES + kb0 * 32 * 256;
+            const unsigned char* v_tile = my_ring + R * TILE_BYTES + kb0 * 32 * 256;
+            auto read = [&](auto n) -> bf16x8 {              // operand of slice n
+                constexpr int k = decltype(n)::value;
+                if constexpr (k < N) {
+                    return *(const bf16x8*)(k_tile + (k % KB) * 32 * 256 + (k_rd ^ ((k / KB) << 5)));
+                } else {
+                    typedef short s16x4 __attribute__((ext_vector_type(4)));
+                    constexpr int block = (k - N) / 4, nb = (k - N) % 4;
+                    const unsigned char* src = v_tile + 16 * block * 256 + (v_rd ^ (nb << 6));
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src + 4 * 256));
+                    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+            };
+            bf16x8 operand[2 * N + AHEAD];
+            static_for<0, AHEAD>([&](auto n) { operand[decltype(n)::value] = read(n); });
+            raise(top);
+            const float ref = m == -INFINITY ? 0.f : m;      // a row that has seen no key yet: its weights are zeros
+            uint32_t p[KB][2][4];
+            float x[2][N], sum0 = 0.f, sum1 = 0.f;           // sums of the weights as they are, before they are rounded for the product: lse has 32 bits
+            auto scaled = [&](auto n) {
+                constexpr int u = decltype(n)::value;
+                x[0][u] = fmaf(now[u >> 3][2 * (u & 7)], c_log2, -ref);
+                x[1][u] = fmaf(now[u >> 3][2 * (u & 7) + 1], c_log2, -ref);
+                pin(x[0][u]);
+                pin(x[1][u]);
+            };
+            auto raised = [&](auto n) {
+                constexpr int u = decltype(n)::value;
+                x[0][u] = __builtin_amdgcn_exp2f(x[0][u]);
+                x[1][u] = __builtin_amdgcn_exp2f(x[1][u]);
+                pin(x[0][u]);
+                pin(x[1][u]);
+            };
+            auto rounded = [&](auto n) {
+                constexpr int u = decltype(n)::value;
+                sum0 += x[0][u];
+                sum1 += x[1][u];
+                bf16x2 pr;
+                pr[0] = (__bf16)x[0][u];
+                pr[1] = (__bf16)x[1][u];
+                uint32_t& to = p[u >> 3][(u >> 2) & 1][u & 3];
+                to = __builtin_bit_cast(uint32_t, pr);
+                pin(to);
+                pin(sum0);
+                pin(sum1);
+            };
+            scaled(std::integral_constant<int, 0>{});
+            __builtin_amdgcn_sched_barrier(0);
+            static_for<0, N>([&](auto n) {
+                constexpr int k = decltype(n)::value, kb = k % KB, st = k / KB;
+                operand[k + AHEAD] = read(std::integral_constant<int, k + AHEAD>{});
+                if constexpr (st == 0) {
+                    f32x16 zero;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) zero[v] = 0.f;
+                    next[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand[k], qf[st], zero, 0, 0, 0);
+                } else {
+                    next[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand[k], qf[st], next[kb], 0, 0, 0);
+                }
+                raised(n);
+                if constexpr (k > 0) rounded(std::integral_constant<int, k - 1>{});
+                if constexpr (k + 1 < N) scaled(std::integral_constant<int, k + 1>{});
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            rounded(std::integral_constant<int, N - 1>{});
+            l += sum0 + sum1;
+            __builtin_amdgcn_sched_barrier(0);
+            auto product = [&](auto n) {
+                constexpr int k = decltype(n)::value, block = k / 4, nb = k % 4;
+                if constexpr (N + k + AHEAD < 2 * N) operand[N + k + AHEAD] = read(std::integral_constant<int, N + k + AHEAD>{});
+                typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+                const u32x4 pw = {p[block >> 1][block & 1][0], p[block >> 1][block & 1][1], p[block >> 1][block & 1][2], p[block >> 1][block & 1][3]};
+                o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand[N + k], __builtin_bit_cast(bf16x8, pw), o[nb], 0, 0, 0);
+            };
+            constexpr int FIRST = 4;                         // value products before the new scores are looked at
+            static_for<0, FIRST>([&](auto n) {
+                product(n);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            if (!clear(t_first + (i + 1) * step)) {
+                mask(t_first + (i + 1) * step, next);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            float most = -INFINITY;
+            static_for<FIRST, N>([&](auto n) {
+                constexpr int k = decltype(n)::value, VALUES = 16 * KB, lo = (k - FIRST) * VALUES / (N - FIRST), hi = (k + 1 - FIRST) * VALUES / (N - FIRST);
+                product(n);
+                static_for<lo, hi>([&](auto v) { most = fmaxf(most, next[decltype(v)::value >> 4][decltype(v)::value & 15]); });
+                pin(most);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            top = most * c_log2;
+            add_bad(i, bad);
+        };
+        using even = std::integral_constant<int, 0>;
+        using odd = std::integral_constant<int, 1>;
+        int i = 0;
+        for (; i + 2 < n_mine; i += 2) {
+            iteration(i, even{}, s0, s1);
+            iteration(i + 1, odd{}, s1, s0);
+        }
+        if (i + 1 < n_mine) {
+            iteration(i, even{}, s0, s1);
+            ++i;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) s0[kb] = s1[kb];
+        }
+        const Bad bad = arrive(i);
+        if (active) {
+            Weights p;
+            raise(top);
+            weigh(s0, p);
+            multiply_v(i, p);
+            add_bad(i, bad);
         }
     }
     const float l_row = pair_sum(l);
