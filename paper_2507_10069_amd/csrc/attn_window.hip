@@ -33,8 +33,9 @@ namespace {
 
 using namespace bf16attn;
 
-constexpr int WAVES = 4;
-constexpr int WIDE_ROWS = 32 * WAVES;                    // rows of a workgroup of the rows shape
+constexpr int WAVES = 4;                                 // of a workgroup of the keys shape
+constexpr int ROWS_WAVES = 8;                            // of the rows shape
+constexpr int WIDE_ROWS = 32 * ROWS_WAVES;               // rows of one
 constexpr int WAVE_ROWS = 32;
 constexpr int BLK = 16;                                  // slots of a block
 constexpr int SLAB = BLK * D * 2;                        // bytes of a block of one KV head
@@ -110,7 +111,7 @@ template <int ROWS> __device__ inline bool find_tile(const BatchView& b, const W
 // them, neighbours, which mostly read the same keys.  It holds SLOTS workgroups at once, and units take about equally long (a window), so that with
 // few units in the last round most of its places would idle: such units are halved.  A workgroup then has 64 rows, two waves to 32 of them, which take a half
 // of each tile's keys each and meet in LDS.  Everybody derives the same plan from the lengths.
-constexpr int SLOTS = 64, MOST_HALVED = 32;
+constexpr int SLOTS = 256 / ROWS_WAVES, MOST_HALVED = SLOTS / 2;
 struct RowsPlan {
     int first, units, whole;                             // of an XCD: its first unit, all of them, those that are not halved
 };
@@ -193,18 +194,21 @@ template <int SHAPE> struct Sizes {
     static constexpr int TILE = SHAPE == KEYS ? 32 : 64;                     // keys of a tile
     static constexpr int TILE_BYTES = TILE * D * 2;                          // of K, or of V
     static constexpr int RING = 4 * TILE_BYTES;                              // two slots of K and V
-    static constexpr int LDS = SHAPE == KEYS ? WAVES * RING : RING;
+    static constexpr int OUT = ROWS_WAVES * WAVE_ROWS * OUT_STRIDE;          // rows shapes: what is staged at the end; a halved unit's sums are less
+    static constexpr int LDS = SHAPE == KEYS ? WAVES * RING : RING > OUT ? RING : OUT;
 };
 
 // The rows of tile t by the workgroup.  KEYS: part `part` of its keys, of a row tile in `slot`.  bad_s: rows shape, keys of a tile's blocks whose V holds
 // an infinity or NaN.
 template <int SHAPE>
 __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView& w, const WindowLayout& L, const Tile& t, int kvh, int slot, int part,
-                                            unsigned char* smem, int (*bad_s)[WAVES])
+                                            unsigned char* smem, int (*bad_s)[ROWS_WAVES])
 {
     constexpr bool KEYS = SHAPE == Shape::KEYS, HALVED = SHAPE == Shape::HALVED;
     constexpr int TB = Sizes<SHAPE>::TILE / BLK, TILE_BYTES = Sizes<SHAPE>::TILE_BYTES, RING = Sizes<SHAPE>::RING;
     constexpr int KB = SHAPE == ROWS ? 2 : 1;            // 32-key parts of a tile that a wave takes
+    // rows shapes: the waves of a block of the tile bring 4 INSTR rows of it each
+    constexpr int PER_BLOCK = KEYS ? 1 : ROWS_WAVES / TB, INSTR = 4 / PER_BLOCK;
     const BatchView& b = a.b;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -240,10 +244,11 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     //        K: row = 16 block + swap23(key in block), chunk c of it at c ^ (row & 15)    (read with ds_read_b128)
     //        V: row = key,                             chunk c of it at c ^ ((row & 3) << 2)      (read with ds_read_tr16_b64)
     const int ld_row = lane >> 4, ld_p = lane & 15;
-    int k_goff[4];
+    const int my_block = KEYS ? 0 : wave / PER_BLOCK, j0 = KEYS ? 0 : wave % PER_BLOCK * INSTR;      // of a tile; its first 4 j0 rows are another wave's
+    int k_goff[INSTR];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) k_goff[j] = swap23(4 * j + ld_row) * 256 + ((ld_p ^ (4 * j + ld_row)) << 4);
-    const int v_goff = ld_row * 256 + ((ld_p ^ (ld_row << 2)) << 4);
+    for (int j = 0; j < INSTR; ++j) k_goff[j] = swap23(4 * (j0 + j) + ld_row) * 256 + ((ld_p ^ (4 * (j0 + j) + ld_row)) << 4);
+    const int v_goff = (4 * j0 + ld_row) * 256 + ((ld_p ^ (ld_row << 2)) << 4);
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem + (KEYS ? wave * RING : 0);
     unsigned char* const my_ring = smem + (KEYS ? wave * RING : 0);
     const int32_t* __restrict__ pt = b.page_table + (long long)t.r * b.max_pages;
@@ -260,7 +265,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     long long id_vec = 0;
     auto refill = [&](int i) {
         const int tile = t_first + (i + lane / PER_TILE) * step;
-        const int v = min(tile * TB + (KEYS ? lane % PER_TILE : wave), t.blocks - 1);
+        const int v = min(tile * TB + (KEYS ? lane % PER_TILE : my_block), t.blocks - 1);
         id_vec = slab_of_block(t.block(v));
         id_base = i;
     };
@@ -274,18 +279,18 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
 #pragma unroll
         for (int which = 0; which < PER_TILE; ++which) {
             const unsigned char* from = kcb + slab(i, which);
-            const uint32_t to = ring + (i & 1) * TILE_BYTES + (KEYS ? which : wave) * SLAB;
+            const uint32_t to = ring + (i & 1) * TILE_BYTES + (KEYS ? which : my_block) * SLAB + j0 * 1024;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) lds_dma16(from, k_goff[j], to + j * 1024);
+            for (int j = 0; j < INSTR; ++j) lds_dma16(from, k_goff[j], to + j * 1024);
         }
     };
     auto fetch_v = [&](int i) {
 #pragma unroll
         for (int which = 0; which < PER_TILE; ++which) {
             const unsigned char* from = vcb + slab(i, which);
-            const uint32_t to = ring + (2 + (i & 1)) * TILE_BYTES + (KEYS ? which : wave) * SLAB;
+            const uint32_t to = ring + (2 + (i & 1)) * TILE_BYTES + (KEYS ? which : my_block) * SLAB + j0 * 1024;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) lds_dma16(from, v_goff + j * 1024, to + j * 1024);
+            for (int j = 0; j < INSTR; ++j) lds_dma16(from, v_goff + j * 1024, to + j * 1024);
         }
     };
     // is block v of the list seen whole by all rows of this wave?  (by all of a tile's blocks: no masks)
@@ -305,8 +310,8 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
         const int key0 = t.block(v) * BLK;
         int bad = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int key = key0 + 4 * j + ld_row;
+        for (int jj = 0; jj < INSTR; ++jj) {
+            const int j = j0 + jj, key = key0 + 4 * j + ld_row;
             uint4* at = (uint4*)(block + j * 1024 + lane * 16);
             const bool hidden = key > t.last || (key < t.low_first && key >= w.sinks);
             uint4 x = *at;
@@ -478,7 +483,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
             if (bad.look) {
 #pragma unroll
                 for (int which = 0; which < PER_TILE; ++which)
-                    bad.of[which] = look_at_v(tile * TB + (KEYS ? which : wave), my_ring + (2 + (i & 1)) * TILE_BYTES + (KEYS ? which : wave) * SLAB);
+                    bad.of[which] = look_at_v(tile * TB + (KEYS ? which : my_block), my_ring + (2 + (i & 1)) * TILE_BYTES + (KEYS ? which : my_block) * SLAB);
                 if (!KEYS && lane == 0) bad_s[i & 1][wave] = bad.of[0];
             }
             if constexpr (KEYS) {
@@ -486,9 +491,11 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
             } else {
                 __syncthreads();                             // everyone's share; and everyone is past its reads of the other slots
             }
-            if (i + 2 < n_mine && i + 2 - id_base >= IDS) refill(i + 1);
-            if (i + 1 < n_mine) fetch_v(i + 1);
-            if (i + 2 < n_mine) fetch_k(i + 2);
+            if (i + 2 - id_base >= IDS && i + 2 < n_mine + 2) refill(i + 1);
+            if (KEYS || !active) {
+                if (i + 1 < n_mine) fetch_v(i + 1);
+                if (i + 2 < n_mine) fetch_k(i + 2);
+            }
             return bad;
         };
         auto add_bad = [&](int i, const Bad& bad) {
@@ -500,7 +507,9 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
                     if (bad.of[which] != 0) add_odd(tile * TB + which, bad.of[which]);
             } else {
                 for (int k = 2 * kb0; k < (HALVED ? 2 * kb0 + 2 : TB); ++k) {
-                    const int those = __builtin_amdgcn_readfirstlane(bad_s[i & 1][k]);
+                    int those = 0;
+#pragma unroll
+                    for (int x = 0; x < PER_BLOCK; ++x) those |= __builtin_amdgcn_readfirstlane(bad_s[i & 1][k * PER_BLOCK + x]);
                     if (those != 0) add_odd(tile * TB + k, those);
                 }
             }
@@ -574,6 +583,9 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
                 } else {
                     next[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand[k], qf[st], next[kb], 0, 0, 0);
                 }
+                // (rows shapes: in between, and past the last tile the list's last blocks again, which costs less than a branch)
+                if constexpr (!KEYS && k == 1) fetch_v(i + 1);
+                if constexpr (!KEYS && k == 3) fetch_k(i + 2);
                 raised(n);
                 if constexpr (k > 0) rounded(std::integral_constant<int, k - 1>{});
                 if constexpr (k + 1 < N) scaled(std::integral_constant<int, k + 1>{});
@@ -631,6 +643,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
             add_bad(i, bad);
         }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was fetched past the last tile)
     const float l_row = pair_sum(l);
     auto at_row = [&](int row) -> long long {                // row of [T][H]
         const int token = L.by_G.quotient(row);
@@ -748,7 +761,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
 }
 
 template <bool BY_KEYS>
-__global__ __launch_bounds__(64 * WAVES, BY_KEYS ? 1 : 2) void attn_window_kernel(AttnArgs a, WindowView w, WindowLayout L)
+__global__ __launch_bounds__(64 * (BY_KEYS ? WAVES : ROWS_WAVES), BY_KEYS ? 1 : 2) void attn_window_kernel(AttnArgs a, WindowView w, WindowLayout L)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char smem[Sizes<BY_KEYS ? KEYS : ROWS>::LDS];
     const BatchView& b = a.b;
@@ -770,7 +783,7 @@ __global__ __launch_bounds__(64 * WAVES, BY_KEYS ? 1 : 2) void attn_window_kerne
         }
         if (find_tile<WAVE_ROWS>(b, L, w, slot, t)) attend_tile<KEYS>(a, w, L, t, kvh, slot, part, smem, nullptr);
     } else {
-        __shared__ int bad_s[2][WAVES];
+        __shared__ int bad_s[2][ROWS_WAVES];
         Lines lines = {b};
         const int tiles = lines.total(L), i = blockIdx.x / NUM_XCD;
         const RowsPlan plan = rows_plan(tiles * b.num_kv_heads, blockIdx.x % NUM_XCD);
@@ -847,7 +860,7 @@ __global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs 
     if (a.lse != nullptr && lane == 0) a.lse[at] = top * LN2 + logf(total);
 }
 
-constexpr int COMPUTE_UNITS = 256;
+constexpr int COMPUTE_UNITS = 256, ROWS_UNITS = 64;
 
 // How a batch is dealt, from what the host knows.  keys: which of the two shapes
 struct Deal {
@@ -866,7 +879,7 @@ Deal deal_of(const BatchView& b, const WindowView& w)
     s.L.G = G;
     s.L.by_G = divisor_of(G);
     s.L.by_kv_heads = divisor_of(b.num_kv_heads);
-    s.keys = single || wide < COMPUTE_UNITS;
+    s.keys = single || wide < ROWS_UNITS;
     // the most that a row tile looks at
     const long long span = std::min((long long)b.max_pages * b.page_size, (long long)w.window + w.sinks + WAVE_ROWS / G + 1);
     if (!s.keys) {
@@ -905,7 +918,7 @@ hipError_t launch_attn_window(const AttnArgs& a, const WindowView& w, hipStream_
     if (s.grid > 0x3fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)s.grid), block(64 * WAVES);
     if (s.keys) hipLaunchKernelGGL((attn_window_kernel<true>), grid, block, 0, stream, a, w, s.L);
-    else hipLaunchKernelGGL((attn_window_kernel<false>), grid, block, 0, stream, a, w, s.L);
+    else hipLaunchKernelGGL((attn_window_kernel<false>), grid, dim3(64 * ROWS_WAVES), 0, stream, a, w, s.L);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess || s.workspace == 0) return err;
     const int rows = (int)std::min<long long>((long long)b.max_new_len * s.L.G, WAVE_ROWS), groups = (rows + WAVES - 1) / WAVES;
