@@ -34,8 +34,6 @@ namespace {
 using namespace bf16attn;
 
 constexpr int WAVES = 4;                                 // of a workgroup of the keys shape
-constexpr int ROWS_WAVES = 8;                            // of the rows shape
-constexpr int WIDE_ROWS = 32 * ROWS_WAVES;               // rows of one
 constexpr int WAVE_ROWS = 32;
 constexpr int BLK = 16;                                  // slots of a block
 constexpr int SLAB = BLK * D * 2;                        // bytes of a block of one KV head
@@ -47,6 +45,8 @@ constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
 struct WindowLayout {
     int G;
     Divisor by_G, by_kv_heads;
+    // rows shape
+    int most_parts;                                      // into how many parts the units of an XCD's last round may be cut: see RowsPlan
     // keys shape
     int slots;                                           // row tiles per KV head that the grid has room for
     int single;                                          // 1: a request has one row tile at most, and slot r is request r's
@@ -107,23 +107,34 @@ template <int ROWS> __device__ inline bool find_tile(const BatchView& b, const W
     return make_tile(b, L, w, r, row0, ROWS, new_len, prefix_len, cu, t);
 }
 
-// ---- Rows shape: units.  A unit is a row tile of a KV head; they are counted head by head, request by request, and each XCD has an eighth of
-// them, neighbours, which mostly read the same keys.  It holds SLOTS workgroups at once, and units take about equally long (a window), so that with
-// few units in the last round most of its places would idle: such units are halved.  A workgroup then has 64 rows, two waves to 32 of them, which take a half
-// of each tile's keys each and meet in LDS.  Everybody derives the same plan from the lengths.
-constexpr int SLOTS = 256 / ROWS_WAVES, MOST_HALVED = SLOTS / 2;
+// ---- Rows shape, NW waves a workgroup.  A unit is a row tile of 32 NW rows of a KV head; units are counted head by head, request by request, and
+// each XCD has an eighth of them, neighbours, which mostly read the same keys.  It holds 256 / NW workgroups at once, and units take about equally
+// long (a window), so that with few units in the last round most of its places would idle.  Such units are
+//   cut     along their keys into as many parts as there are places for, which leave records for a second kernel, or, where that may not be,
+//   halved  a workgroup then has half of the rows, two waves to 32 of them, which take a half of each tile's keys each and meet in LDS.
+// Everybody derives the same plan from the lengths.
+constexpr int MOST_PARTS = 16;
 struct RowsPlan {
-    int first, units, whole;                             // of an XCD: its first unit, all of them, those that are not halved
+    int first, units, whole;                             // of an XCD: its first unit, all of them, those that are neither cut nor halved
+    int parts;                                           // of each of the others; 0: halves
 };
-__device__ inline RowsPlan rows_plan(int total, int xcd)
+template <int NW> __device__ inline RowsPlan rows_plan(const WindowLayout& L, int total, int xcd)
 {
+    constexpr int SLOTS = 256 / NW;
     RowsPlan p;
     p.first = (int)((long long)xcd * total / NUM_XCD);
     p.units = (int)((long long)(xcd + 1) * total / NUM_XCD) - p.first;
-    const int full = p.units / SLOTS * SLOTS;
-    p.whole = p.units - full <= MOST_HALVED ? full : p.units;
+    const int full = p.units / SLOTS * SLOTS, rem = p.units - full;
+    p.whole = rem <= SLOTS / 2 ? full : p.units;
+    p.parts = rem > 0 && rem <= SLOTS / 2 ? min(SLOTS / rem, L.most_parts) : 0;
+    if (p.parts == 1) p.parts = 0;
     return p;
 }
+// a part's record: per thread 64 sums, in groups of four, then m, l
+template <int NW> struct Record {
+    static constexpr int THREADS = 64 * NW, FLOATS = THREADS * (64 + 2);
+    static __device__ float* at(void* workspace, int xcd, int place) { return (float*)workspace + (size_t)(xcd * (256 / NW) + place) * FLOATS; }
+};
 // running sums over the wave's lanes, inclusive
 __device__ inline int scan64(int x)
 {
@@ -136,7 +147,8 @@ __device__ inline int scan64(int x)
     return x;
 }
 // The row tiles of 64 requests from `from` on, as the lanes see them
-struct Lines {
+template <int NW> struct Lines {
+    static constexpr int WIDE_ROWS = NW * WAVE_ROWS;
     const BatchView& b;
     int new_len, prefix_len, cu, incl;
     __device__ int look(const WindowLayout& L, int from) // returns their number
@@ -190,25 +202,26 @@ __device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
 __device__ inline bool is_finite_bf16(uint32_t half) { return (half & 0x7f80u) != 0x7f80u; }
 
 enum Shape { ROWS, HALVED /* rows, of half a unit */, KEYS };
-template <int SHAPE> struct Sizes {
+template <int SHAPE, int NW> struct Sizes {
     static constexpr int TILE = SHAPE == KEYS ? 32 : 64;                     // keys of a tile
     static constexpr int TILE_BYTES = TILE * D * 2;                          // of K, or of V
     static constexpr int RING = 4 * TILE_BYTES;                              // two slots of K and V
-    static constexpr int OUT = ROWS_WAVES * WAVE_ROWS * OUT_STRIDE;          // rows shapes: what is staged at the end; a halved unit's sums are less
-    static constexpr int LDS = SHAPE == KEYS ? WAVES * RING : RING > OUT ? RING : OUT;
+    static constexpr int OUT = NW * WAVE_ROWS * OUT_STRIDE;          // rows shapes: what is staged at the end; a halved unit's sums are less
+    static constexpr int LDS = SHAPE == KEYS ? NW * RING : RING > OUT ? RING : OUT;
 };
 
-// The rows of tile t by the workgroup.  KEYS: part `part` of its keys, of a row tile in `slot`.  bad_s: rows shape, keys of a tile's blocks whose V holds
+// The rows of tile t by the workgroup, or, of `parts`, part `part` of their keys, whose record is number `place` (of those that the keys shape leaves,
+// or of the XCD's).  bad_s: rows shape, keys of a tile's blocks whose V holds
 // an infinity or NaN.
-template <int SHAPE>
-__device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView& w, const WindowLayout& L, const Tile& t, int kvh, int slot, int part,
-                                            unsigned char* smem, int (*bad_s)[ROWS_WAVES])
+template <int SHAPE, int NW>
+__device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView& w, const WindowLayout& L, const Tile& t, int kvh, int parts, int part, int place,
+                                            unsigned char* smem, int (*bad_s)[NW])
 {
     constexpr bool KEYS = SHAPE == Shape::KEYS, HALVED = SHAPE == Shape::HALVED;
-    constexpr int TB = Sizes<SHAPE>::TILE / BLK, TILE_BYTES = Sizes<SHAPE>::TILE_BYTES, RING = Sizes<SHAPE>::RING;
+    constexpr int TB = Sizes<SHAPE, NW>::TILE / BLK, TILE_BYTES = Sizes<SHAPE, NW>::TILE_BYTES, RING = Sizes<SHAPE, NW>::RING;
     constexpr int KB = SHAPE == ROWS ? 2 : 1;            // 32-key parts of a tile that a wave takes
     // rows shapes: the waves of a block of the tile bring 4 INSTR rows of it each
-    constexpr int PER_BLOCK = KEYS ? 1 : ROWS_WAVES / TB, INSTR = 4 / PER_BLOCK;
+    constexpr int PER_BLOCK = KEYS ? 1 : NW / TB, INSTR = 4 / PER_BLOCK;
     const BatchView& b = a.b;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -218,12 +231,12 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     // this workgroup's tiles, and of those this wave's
     const int all_tiles = (t.blocks + TB - 1) / TB;
     int t_begin = 0, t_end = all_tiles;
-    if (KEYS) {
-        const int share = L.by_parts.quotient(all_tiles + L.parts - 1);
+    if (KEYS || (SHAPE == ROWS && NW == 8 && parts > 1)) {
+        const int share = KEYS ? L.by_parts.quotient(all_tiles + parts - 1) : (all_tiles + parts - 1) / parts;
         t_begin = min(part * share, all_tiles);
         t_end = min(t_begin + share, all_tiles);
     }
-    const int step = KEYS ? WAVES : 1, t_first = KEYS ? t_begin + wave : 0;
+    const int step = KEYS ? NW : 1, t_first = KEYS ? t_begin + wave : t_begin;
     const int n_mine = t_end > t_first ? (t_end - t_first + step - 1) / step : 0;
 
     const int wrow0 = t.row0 + (KEYS ? 0 : HALVED ? wave >> 1 : wave) * WAVE_ROWS;
@@ -685,6 +698,17 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
             __syncthreads();                                 // what is staged next lies there
         }
         if (!active || kb0 != 0) return;
+        if (SHAPE == ROWS && NW == 8 && parts > 1) {
+            float* rec = Record<NW>::at(a.workspace, blockIdx.x % NUM_XCD, place);
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+                for (int v4 = 0; v4 < 4; ++v4)
+                    *(f32x4*)(rec + ((4 * nb + v4) * Record<NW>::THREADS + tid) * 4) = f32x4{o[nb][4 * v4], o[nb][4 * v4 + 1], o[nb][4 * v4 + 2], o[nb][4 * v4 + 3]};
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            *(f32x2*)(rec + 64 * Record<NW>::THREADS + 2 * tid) = f32x2{m, l_all};
+            return;
+        }
         const float inv = l_all != 0.f ? 1.f / l_all : 0.f;  // (a row sees itself)
         unsigned char* stage = smem + wave * (32 * OUT_STRIDE);
 #pragma unroll
@@ -737,8 +761,8 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
 #pragma unroll
             for (int k = 0; k < WAVES; ++k) sum[x] += weight[k] * *(const f32x4*)(first + k * WAVE_ROWS * REC_STRIDE + ch + 32 * x);
         }
-        if (L.parts > 1) {
-            float* rec = (float*)a.workspace + (((long long)(slot * b.num_kv_heads + kvh) * L.parts + part) * WAVE_ROWS + row) * REC_STRIDE;
+        if (parts > 1) {
+            float* rec = (float*)a.workspace + ((long long)place * WAVE_ROWS + row) * REC_STRIDE;
 #pragma unroll
             for (int x = 0; x < 4; ++x) *(f32x4*)(rec + ch + 32 * x) = sum[x];
             if (ch == 0) {
@@ -760,41 +784,48 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     }
 }
 
-template <bool BY_KEYS>
-__global__ __launch_bounds__(64 * (BY_KEYS ? WAVES : ROWS_WAVES), BY_KEYS ? 1 : 2) void attn_window_kernel(AttnArgs a, WindowView w, WindowLayout L)
+__global__ __launch_bounds__(64 * WAVES, 1) void attn_window_keys_kernel(AttnArgs a, WindowView w, WindowLayout L)
 {
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[Sizes<BY_KEYS ? KEYS : ROWS>::LDS];
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[Sizes<KEYS, WAVES>::LDS];
     const BatchView& b = a.b;
-    Tile t;
-    if constexpr (BY_KEYS) {
-        int item = blockIdx.x, slot, part, kvh;
-        if (L.per_xcd > 0) item = (blockIdx.x % NUM_XCD) * L.per_xcd + blockIdx.x / NUM_XCD;
-        if (item >= L.items) return;
-        if (L.per_xcd > 0) {                             // neighbours share a KV head, and mostly a request
-            const int group = L.by_slots.quotient(item);
-            slot = item - group * L.slots;
-            kvh = L.by_parts.quotient(group);
-            part = group - kvh * L.parts;
-        } else {
-            const int pair = L.by_parts.quotient(item);
-            part = item - pair * L.parts;
-            slot = L.by_kv_heads.quotient(pair);
-            kvh = pair - slot * b.num_kv_heads;
-        }
-        if (find_tile<WAVE_ROWS>(b, L, w, slot, t)) attend_tile<KEYS>(a, w, L, t, kvh, slot, part, smem, nullptr);
+    int item = blockIdx.x, slot, part, kvh;
+    if (L.per_xcd > 0) item = (blockIdx.x % NUM_XCD) * L.per_xcd + blockIdx.x / NUM_XCD;
+    if (item >= L.items) return;
+    if (L.per_xcd > 0) {                                 // neighbours share a KV head, and mostly a request
+        const int group = L.by_slots.quotient(item);
+        slot = item - group * L.slots;
+        kvh = L.by_parts.quotient(group);
+        part = group - kvh * L.parts;
     } else {
-        __shared__ int bad_s[2][ROWS_WAVES];
-        Lines lines = {b};
-        const int tiles = lines.total(L), i = blockIdx.x / NUM_XCD;
-        const RowsPlan plan = rows_plan(tiles * b.num_kv_heads, blockIdx.x % NUM_XCD);
-        const bool whole = i < plan.whole;
-        const int nth = whole ? i : plan.whole + ((i - plan.whole) >> 1);
-        if (nth >= plan.units) return;
-        const int unit = plan.first + nth, kvh = unit / tiles;
-        if (!lines.take(L, w, unit - kvh * tiles, whole ? -1 : (i - plan.whole) & 1, t)) return;
-        if (whole) attend_tile<ROWS>(a, w, L, t, kvh, 0, 0, smem, bad_s);
-        else attend_tile<HALVED>(a, w, L, t, kvh, 0, 0, smem, bad_s);
+        const int pair = L.by_parts.quotient(item);
+        part = item - pair * L.parts;
+        slot = L.by_kv_heads.quotient(pair);
+        kvh = pair - slot * b.num_kv_heads;
     }
+    Tile t;
+    if (find_tile<WAVE_ROWS>(b, L, w, slot, t))
+        attend_tile<KEYS, WAVES>(a, w, L, t, kvh, L.parts, part, (slot * b.num_kv_heads + kvh) * L.parts + part, smem, nullptr);
+}
+
+template <int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_window_rows_kernel(AttnArgs a, WindowView w, WindowLayout L)
+{
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[Sizes<ROWS, NW>::LDS];
+    __shared__ int bad_s[2][NW];
+    const BatchView& b = a.b;
+    Lines<NW> lines = {b};
+    const int tiles = lines.total(L), i = blockIdx.x / NUM_XCD;
+    const RowsPlan plan = rows_plan<NW>(L, tiles * b.num_kv_heads, blockIdx.x % NUM_XCD);
+    const bool whole = i < plan.whole;
+    const int share = whole || plan.parts == 0 ? 2 : plan.parts, place = i - plan.whole;             // workgroups of a unit
+    const int nth = whole ? i : plan.whole + place / share, part = whole ? 0 : place % share;
+    if (nth >= plan.units) return;
+    const int unit = plan.first + nth, kvh = unit / tiles;
+    const bool halved = !whole && plan.parts == 0;
+    Tile t;
+    if (!lines.take(L, w, unit - kvh * tiles, halved ? part : -1, t)) return;
+    if (halved) attend_tile<HALVED, NW>(a, w, L, t, kvh, 1, 0, 0, smem, bad_s);
+    else attend_tile<ROWS, NW>(a, w, L, t, kvh, whole ? 1 : plan.parts, part, place, smem, bad_s);
 }
 
 // over all lanes of a wave
@@ -860,11 +891,67 @@ __global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs 
     if (a.lse != nullptr && lane == 0) a.lse[at] = top * LN2 + logf(total);
 }
 
-constexpr int COMPUTE_UNITS = 256, ROWS_UNITS = 64;
+// The same for the rows shape's cut units.  SUB workgroups for each of a unit's parts share its sums: 16 groups of four of each of its threads.
+constexpr int SUB = 4;
+template <int NW>
+__global__ __launch_bounds__(256) void attn_window_rows_merge_kernel(AttnArgs a, WindowView w, WindowLayout L)
+{
+    constexpr int THREADS = Record<NW>::THREADS;
+    const BatchView& b = a.b;
+    const int xcd = blockIdx.x % NUM_XCD, at_place = blockIdx.x / NUM_XCD / SUB, sub = blockIdx.x / NUM_XCD % SUB;
+    Lines<NW> lines = {b};
+    const int tiles = lines.total(L);
+    const RowsPlan plan = rows_plan<NW>(L, tiles * b.num_kv_heads, xcd);
+    if (plan.parts == 0 || at_place >= (plan.units - plan.whole) * plan.parts) return;
+    const int nth = at_place / plan.parts, share = at_place - nth * plan.parts;
+    const int unit = plan.first + plan.whole + nth, kvh = unit / tiles;
+    Tile t;
+    if (!lines.take(L, w, unit - kvh * tiles, -1, t)) return;
+    const float* rec = Record<NW>::at(a.workspace, xcd, nth * plan.parts);
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    for (int item = (share * SUB + sub) * 256 + threadIdx.x; item < 16 * THREADS; item += plan.parts * SUB * 256) {
+        const int group = item / THREADS, col = item % THREADS, row = (col >> 6) * WAVE_ROWS + (col & 31), h32 = (col >> 5) & 1;
+        if (t.row0 + row >= t.n_rows) continue;
+        f32x4 v[MOST_PARTS];
+        f32x2 ml[MOST_PARTS];
+#pragma unroll
+        for (int k = 0; k < MOST_PARTS; ++k)
+            if (k < plan.parts) {
+                ml[k] = *(const f32x2*)(rec + (size_t)k * Record<NW>::FLOATS + 64 * THREADS + 2 * col);
+                v[k] = *(const f32x4*)(rec + (size_t)k * Record<NW>::FLOATS + item * 4);
+            }
+        float top = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int k = 0; k < MOST_PARTS; ++k)
+            if (k < plan.parts) top = fmaxf(top, ml[k][0]);
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < MOST_PARTS; ++k)
+            if (k < plan.parts) {
+                const float weight = ml[k][0] != -INFINITY ? __builtin_amdgcn_exp2f(ml[k][0] - top) : 0.f;
+                total += weight * ml[k][1];
+                if (weight != 0.f) sum += weight * v[k];
+            }
+        const float inv = total != 0.f ? 1.f / total : 0.f;
+        const int token = L.by_G.quotient(t.row0 + row);
+        const long long at = ((long long)t.first_row + token) * b.num_q_heads + kvh * L.G + (t.row0 + row - token * L.G);
+        bf16x4 out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = (__bf16)(sum[e] * inv);
+        *(bf16x4*)((__bf16*)a.out + at * D + 32 * (group >> 2) + 8 * (group & 3) + 4 * h32) = out;
+        if (a.lse != nullptr && group == 0 && h32 == 0) a.lse[at] = top * LN2 + logf(total);
+    }
+}
 
-// How a batch is dealt, from what the host knows.  keys: which of the two shapes
+constexpr int COMPUTE_UNITS = 256;
+constexpr int ROWS_UNITS = 32;                           // units of 128 rows from which the rows shape is taken
+constexpr int LONG_TILES = 32;                           // tiles of 64 keys from which on its workgroups have eight waves, and their last units are cut
+constexpr int CUT_ROUNDS = 4;                            // ... unless there are so many rounds that the last one is a small part
+constexpr int MIN_TILES = 4;                             // of a part
+
+// How a batch is dealt, from what the host knows.
 struct Deal {
-    bool keys;
+    int rows_waves;                                      // of a workgroup of the rows shape, 0: keys shape
     WindowLayout L;
     long long grid;
     size_t workspace;
@@ -875,17 +962,25 @@ Deal deal_of(const BatchView& b, const WindowView& w)
     const int G = b.num_q_heads / b.num_kv_heads;
     const long long rows = (long long)b.total_new_tokens * G;
     const bool single = (long long)b.max_new_len * G <= WAVE_ROWS;
-    const long long wide = (rows + WIDE_ROWS - 1) / WIDE_ROWS * b.num_kv_heads;     // units of the rows shape, at least
     s.L.G = G;
     s.L.by_G = divisor_of(G);
     s.L.by_kv_heads = divisor_of(b.num_kv_heads);
-    s.keys = single || wide < ROWS_UNITS;
-    // the most that a row tile looks at
+    // the most that 32 rows look at
     const long long span = std::min((long long)b.max_pages * b.page_size, (long long)w.window + w.sinks + WAVE_ROWS / G + 1);
-    if (!s.keys) {
-        // (a halved unit is two workgroups)
-        const long long units = (rows / WIDE_ROWS + b.num_reqs) * b.num_kv_heads;
-        s.grid = ((units + NUM_XCD - 1) / NUM_XCD + MOST_HALVED) * NUM_XCD;
+    if (!single && (rows + 127) / 128 * b.num_kv_heads >= ROWS_UNITS) {
+        const bool lengthy = (span + 63) / 64 >= LONG_TILES;
+        s.rows_waves = lengthy ? 8 : 4;
+        const int tile_rows = 32 * s.rows_waves, slots = 256 / s.rows_waves;
+        const bool uniform = (long long)b.num_reqs * b.max_new_len == b.total_new_tokens;
+        long long units = (rows / tile_rows + b.num_reqs) * b.num_kv_heads;
+        if (uniform) units = ((long long)b.max_new_len * G + tile_rows - 1) / tile_rows * b.num_reqs * b.num_kv_heads;
+        s.L.most_parts = lengthy && units <= (long long)CUT_ROUNDS * slots * NUM_XCD ? (int)std::min((long long)MOST_PARTS, (span + 63) / 64 / MIN_TILES) : 1;
+        if (uniform) {                                       // the plans are known: is any unit cut?
+            auto cut = [&](long long n) { return n % slots > 0 && n % slots <= slots / 2; };
+            if (!cut(units / NUM_XCD) && !cut((units + NUM_XCD - 1) / NUM_XCD)) s.L.most_parts = 1;
+        }
+        s.grid = ((units + NUM_XCD - 1) / NUM_XCD + slots) * NUM_XCD;        // (units of the last round are `slots` workgroups at most)
+        s.workspace = s.L.most_parts > 1 ? (size_t)NUM_XCD * slots * Record<8>::FLOATS * sizeof(float) : 0;
         return s;
     }
     const long long slots = single ? b.num_reqs : rows / WAVE_ROWS + b.num_reqs;
@@ -916,13 +1011,18 @@ hipError_t launch_attn_window(const AttnArgs& a, const WindowView& w, hipStream_
     const BatchView& b = a.b;
     const Deal s = deal_of(b, w);
     if (s.grid > 0x3fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)s.grid), block(64 * WAVES);
-    if (s.keys) hipLaunchKernelGGL((attn_window_kernel<true>), grid, block, 0, stream, a, w, s.L);
-    else hipLaunchKernelGGL((attn_window_kernel<false>), grid, dim3(64 * ROWS_WAVES), 0, stream, a, w, s.L);
+    const dim3 grid((unsigned)s.grid);
+    if (s.rows_waves == 8) hipLaunchKernelGGL((attn_window_rows_kernel<8>), grid, dim3(64 * 8), 0, stream, a, w, s.L);
+    else if (s.rows_waves == 4) hipLaunchKernelGGL((attn_window_rows_kernel<4>), grid, dim3(64 * 4), 0, stream, a, w, s.L);
+    else hipLaunchKernelGGL(attn_window_keys_kernel, grid, dim3(64 * WAVES), 0, stream, a, w, s.L);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess || s.workspace == 0) return err;
-    const int rows = (int)std::min<long long>((long long)b.max_new_len * s.L.G, WAVE_ROWS), groups = (rows + WAVES - 1) / WAVES;
-    hipLaunchKernelGGL(attn_window_merge_kernel, dim3((unsigned)(s.L.slots * b.num_kv_heads * groups)), block, 0, stream, a, w, s.L, groups);
+    if (s.rows_waves > 0) {
+        hipLaunchKernelGGL((attn_window_rows_merge_kernel<8>), dim3(NUM_XCD * 32 * SUB), dim3(256), 0, stream, a, w, s.L);
+    } else {
+        const int rows = (int)std::min<long long>((long long)b.max_new_len * s.L.G, WAVE_ROWS), groups = (rows + WAVES - 1) / WAVES;
+        hipLaunchKernelGGL(attn_window_merge_kernel, dim3((unsigned)(s.L.slots * b.num_kv_heads * groups)), dim3(64 * WAVES), 0, stream, a, w, s.L, groups);
+    }
     return hipGetLastError();
 }
 

@@ -159,6 +159,15 @@ def test_cut_tails_and_many_requests(new, window):
     Case(rng.integers(0, 900, len(new)).tolist(), new, window, 7, seed=len(new)).run_and_check()
 
 
+@pytest.mark.parametrize("prefix,new,window,heads,kv_heads", [([3000], [300], 2100, 28, 4), ([2500, 40, 9000], [290, 30, 77], 2048, 28, 4),
+                                                              ([2600, 2600], [128, 128], HUGE, 32, 8), ([4000], [1100], 2500, 28, 4), ([2500] * 66, [20] * 66, 2400, 8, 2)])
+def test_long_windows_cut_into_parts(prefix, new, window, heads, kv_heads):
+    """Row tiles of 256 rows, the last of which are cut along their keys: none, all, or those behind full rounds."""
+    case = Case(prefix, new, window, 20, heads=heads, kv_heads=kv_heads, seed=len(prefix)).to_device()
+    assert case.workspace is not None
+    case.run_and_check()
+
+
 def test_one_context_is_cut_into_parts():
     case = Case([5000], [1], 4096, 64, seed=5).to_device()
     assert case.workspace is not None
