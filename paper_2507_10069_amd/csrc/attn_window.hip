@@ -113,7 +113,7 @@ template <int ROWS> __device__ inline bool find_tile(const BatchView& b, const W
 //   cut     along their keys into as many parts as there are places for, which leave records for a second kernel, or, where that may not be,
 //   halved  a workgroup then has half of the rows, two waves to 32 of them, which take a half of each tile's keys each and meet in LDS.
 // Everybody derives the same plan from the lengths.
-constexpr int MOST_PARTS = 16;
+constexpr int MOST_PARTS = 16, PLACES = 32;              // parts of a unit; of all of an XCD's
 struct RowsPlan {
     int first, units, whole;                             // of an XCD: its first unit, all of them, those that are neither cut nor halved
     int parts;                                           // of each of the others; 0: halves
@@ -126,14 +126,14 @@ template <int NW> __device__ inline RowsPlan rows_plan(const WindowLayout& L, in
     p.units = (int)((long long)(xcd + 1) * total / NUM_XCD) - p.first;
     const int full = p.units / SLOTS * SLOTS, rem = p.units - full;
     p.whole = rem <= SLOTS / 2 ? full : p.units;
-    p.parts = rem > 0 && rem <= SLOTS / 2 ? min(SLOTS / rem, L.most_parts) : 0;
-    if (p.parts == 1) p.parts = 0;
+    p.parts = rem > 0 && rem <= SLOTS / 2 ? min(PLACES / rem, L.most_parts) : 0;
+    if (p.parts < (NW == 8 ? 2 : 4)) p.parts = 0;        // fewer are no quicker than halves, which leave no records
     return p;
 }
 // a part's record: per thread 64 sums, in groups of four, then m, l
 template <int NW> struct Record {
     static constexpr int THREADS = 64 * NW, FLOATS = THREADS * (64 + 2);
-    static __device__ float* at(void* workspace, int xcd, int place) { return (float*)workspace + (size_t)(xcd * (256 / NW) + place) * FLOATS; }
+    static __device__ float* at(void* workspace, int xcd, int place) { return (float*)workspace + (size_t)(xcd * PLACES + place) * FLOATS; }
 };
 // running sums over the wave's lanes, inclusive
 __device__ inline int scan64(int x)
@@ -231,7 +231,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     // this workgroup's tiles, and of those this wave's
     const int all_tiles = (t.blocks + TB - 1) / TB;
     int t_begin = 0, t_end = all_tiles;
-    if (KEYS || (SHAPE == ROWS && NW == 8 && parts > 1)) {
+    if (KEYS || (SHAPE == ROWS && parts > 1)) {
         const int share = KEYS ? L.by_parts.quotient(all_tiles + parts - 1) : (all_tiles + parts - 1) / parts;
         t_begin = min(part * share, all_tiles);
         t_end = min(t_begin + share, all_tiles);
@@ -698,7 +698,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
             __syncthreads();                                 // what is staged next lies there
         }
         if (!active || kb0 != 0) return;
-        if (SHAPE == ROWS && NW == 8 && parts > 1) {
+        if (SHAPE == ROWS && parts > 1) {
             float* rec = Record<NW>::at(a.workspace, blockIdx.x % NUM_XCD, place);
 #pragma unroll
             for (int nb = 0; nb < 4; ++nb)
@@ -944,9 +944,9 @@ __global__ __launch_bounds__(256) void attn_window_rows_merge_kernel(AttnArgs a,
 }
 
 constexpr int COMPUTE_UNITS = 256;
-constexpr int ROWS_UNITS = 32;                           // units of 128 rows from which the rows shape is taken
+constexpr int ROWS_UNITS = 24;                          // units of 128 rows from which the rows shape is taken
 constexpr int LONG_TILES = 32;                           // tiles of 64 keys from which on its workgroups have eight waves, and their last units are cut
-constexpr int CUT_ROUNDS = 4;                            // ... unless there are so many rounds that the last one is a small part
+constexpr int CUT_ROUNDS = 4;                            // ... unless there are so many rounds that the last one is a small part; short ones' only if they are all there is
 constexpr int MIN_TILES = 4;                             // of a part
 
 // How a batch is dealt, from what the host knows.
@@ -967,20 +967,24 @@ Deal deal_of(const BatchView& b, const WindowView& w)
     s.L.by_kv_heads = divisor_of(b.num_kv_heads);
     // the most that 32 rows look at
     const long long span = std::min((long long)b.max_pages * b.page_size, (long long)w.window + w.sinks + WAVE_ROWS / G + 1);
+    const bool lengthy = (span + 63) / 64 >= LONG_TILES;
     if (!single && (rows + 127) / 128 * b.num_kv_heads >= ROWS_UNITS) {
-        const bool lengthy = (span + 63) / 64 >= LONG_TILES;
         s.rows_waves = lengthy ? 8 : 4;
         const int tile_rows = 32 * s.rows_waves, slots = 256 / s.rows_waves;
         const bool uniform = (long long)b.num_reqs * b.max_new_len == b.total_new_tokens;
         long long units = (rows / tile_rows + b.num_reqs) * b.num_kv_heads;
         if (uniform) units = ((long long)b.max_new_len * G + tile_rows - 1) / tile_rows * b.num_reqs * b.num_kv_heads;
-        s.L.most_parts = lengthy && units <= (long long)CUT_ROUNDS * slots * NUM_XCD ? (int)std::min((long long)MOST_PARTS, (span + 63) / 64 / MIN_TILES) : 1;
+        s.L.most_parts = units <= (lengthy ? (long long)CUT_ROUNDS * slots : PLACES / 4) * NUM_XCD ? (int)std::min((long long)MOST_PARTS, (span + 63) / 64 / MIN_TILES) : 1;
+        if (s.L.most_parts < (lengthy ? 2 : 4)) s.L.most_parts = 1;
         if (uniform) {                                       // the plans are known: is any unit cut?
-            auto cut = [&](long long n) { return n % slots > 0 && n % slots <= slots / 2; };
+            auto cut = [&](long long n) {
+                const long long rem = n % slots;
+                return rem > 0 && rem <= slots / 2 && std::min<long long>(PLACES / rem, s.L.most_parts) >= (lengthy ? 2 : 4);
+            };
             if (!cut(units / NUM_XCD) && !cut((units + NUM_XCD - 1) / NUM_XCD)) s.L.most_parts = 1;
         }
         s.grid = ((units + NUM_XCD - 1) / NUM_XCD + slots) * NUM_XCD;        // (units of the last round are `slots` workgroups at most)
-        s.workspace = s.L.most_parts > 1 ? (size_t)NUM_XCD * slots * Record<8>::FLOATS * sizeof(float) : 0;
+        s.workspace = s.L.most_parts > 1 ? (size_t)NUM_XCD * PLACES * (lengthy ? Record<8>::FLOATS : Record<4>::FLOATS) * sizeof(float) : 0;
         return s;
     }
     const long long slots = single ? b.num_reqs : rows / WAVE_ROWS + b.num_reqs;
@@ -1018,7 +1022,9 @@ hipError_t launch_attn_window(const AttnArgs& a, const WindowView& w, hipStream_
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess || s.workspace == 0) return err;
     if (s.rows_waves > 0) {
-        hipLaunchKernelGGL((attn_window_rows_merge_kernel<8>), dim3(NUM_XCD * 32 * SUB), dim3(256), 0, stream, a, w, s.L);
+        const dim3 merge(NUM_XCD * PLACES * SUB);
+        if (s.rows_waves == 8) hipLaunchKernelGGL((attn_window_rows_merge_kernel<8>), merge, dim3(256), 0, stream, a, w, s.L);
+        else hipLaunchKernelGGL((attn_window_rows_merge_kernel<4>), merge, dim3(256), 0, stream, a, w, s.L);
     } else {
         const int rows = (int)std::min<long long>((long long)b.max_new_len * s.L.G, WAVE_ROWS), groups = (rows + WAVES - 1) / WAVES;
         hipLaunchKernelGGL(attn_window_merge_kernel, dim3((unsigned)(s.L.slots * b.num_kv_heads * groups)), dim3(64 * WAVES), 0, stream, a, w, s.L, groups);
