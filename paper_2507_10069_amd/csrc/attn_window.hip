@@ -213,7 +213,7 @@ template <int SHAPE, int NW> struct Sizes {
 // The rows of tile t by the workgroup, or, of `parts`, part `part` of their keys, whose record is number `place` (of those that the keys shape leaves,
 // or of the XCD's).  bad_s: rows shape, keys of a tile's blocks whose V holds
 // an infinity or NaN.
-template <int SHAPE, int NW>
+template <int SHAPE, int NW, bool STREAM = false>
 __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView& w, const WindowLayout& L, const Tile& t, int kvh, int parts, int part, int place,
                                             unsigned char* smem, int (*bad_s)[NW])
 {
@@ -287,6 +287,10 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
         const uint32_t lo = __builtin_amdgcn_readlane((int)id_vec, at), hi = __builtin_amdgcn_readlane((int)(id_vec >> 32), at);
         return (long long)(((unsigned long long)hi << 32) | lo) * SLAB;
     };
+    auto bring = [](const unsigned char* from, int offset, uint32_t to) {
+        if constexpr (STREAM) lds_dma16_streamed(from, offset, to);
+        else lds_dma16(from, offset, to);
+    };
     // this wave's share of its tile i (KEYS: all of it), into slot i % 2
     auto fetch_k = [&](int i) {
 #pragma unroll
@@ -294,7 +298,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
             const unsigned char* from = kcb + slab(i, which);
             const uint32_t to = ring + (i & 1) * TILE_BYTES + (KEYS ? which : my_block) * SLAB + j0 * 1024;
 #pragma unroll
-            for (int j = 0; j < INSTR; ++j) lds_dma16(from, k_goff[j], to + j * 1024);
+            for (int j = 0; j < INSTR; ++j) bring(from, k_goff[j], to + j * 1024);
         }
     };
     auto fetch_v = [&](int i) {
@@ -303,7 +307,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
             const unsigned char* from = vcb + slab(i, which);
             const uint32_t to = ring + (2 + (i & 1)) * TILE_BYTES + (KEYS ? which : my_block) * SLAB + j0 * 1024;
 #pragma unroll
-            for (int j = 0; j < INSTR; ++j) lds_dma16(from, v_goff + j * 1024, to + j * 1024);
+            for (int j = 0; j < INSTR; ++j) bring(from, v_goff + j * 1024, to + j * 1024);
         }
     };
     // is block v of the list seen whole by all rows of this wave?  (by all of a tile's blocks: no masks)
@@ -784,6 +788,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     }
 }
 
+template <bool STREAM>
 __global__ __launch_bounds__(64 * WAVES, 1) void attn_window_keys_kernel(AttnArgs a, WindowView w, WindowLayout L)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char smem[Sizes<KEYS, WAVES>::LDS];
@@ -804,7 +809,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attn_window_keys_kernel(AttnArg
     }
     Tile t;
     if (find_tile<WAVE_ROWS>(b, L, w, slot, t))
-        attend_tile<KEYS, WAVES>(a, w, L, t, kvh, L.parts, part, (slot * b.num_kv_heads + kvh) * L.parts + part, smem, nullptr);
+        attend_tile<KEYS, WAVES, STREAM>(a, w, L, t, kvh, L.parts, part, (slot * b.num_kv_heads + kvh) * L.parts + part, smem, nullptr);
 }
 
 template <int NW>
@@ -944,6 +949,7 @@ __global__ __launch_bounds__(256) void attn_window_rows_merge_kernel(AttnArgs a,
 }
 
 constexpr int COMPUTE_UNITS = 256;
+constexpr long long STREAM_BYTES = 96ll << 20;           // of K and V, each read once: more than the last-level cache keeps for a next call
 constexpr int ROWS_UNITS = 24;                          // units of 128 rows from which the rows shape is taken
 constexpr int LONG_TILES = 32;                           // tiles of 64 keys from which on its workgroups have eight waves, and their last units are cut
 constexpr int CUT_ROUNDS = 4;                            // ... unless there are so many rounds that the last one is a small part; short ones' only if they are all there is
@@ -952,6 +958,7 @@ constexpr int MIN_TILES = 4;                             // of a part
 // How a batch is dealt, from what the host knows.
 struct Deal {
     int rows_waves;                                      // of a workgroup of the rows shape, 0: keys shape
+    bool stream;                                         // keys shape: K and V past the caches
     WindowLayout L;
     long long grid;
     size_t workspace;
@@ -990,6 +997,7 @@ Deal deal_of(const BatchView& b, const WindowView& w)
     const long long slots = single ? b.num_reqs : rows / WAVE_ROWS + b.num_reqs;
     s.L.slots = (int)slots;
     s.L.single = single;
+    s.stream = single && slots * b.num_kv_heads * span * (4 * D) > STREAM_BYTES;
     // as many parts as fill the chip, each of a tile for every wave at least
     const long long tiles = (span + 31) / 32, units = (single ? slots : std::max((rows + WAVE_ROWS - 1) / WAVE_ROWS, 1ll)) * b.num_kv_heads;
     s.L.parts = (int)std::max(1ll, std::min(COMPUTE_UNITS / units, (tiles + WAVES - 1) / WAVES));
@@ -1018,7 +1026,8 @@ hipError_t launch_attn_window(const AttnArgs& a, const WindowView& w, hipStream_
     const dim3 grid((unsigned)s.grid);
     if (s.rows_waves == 8) hipLaunchKernelGGL((attn_window_rows_kernel<8>), grid, dim3(64 * 8), 0, stream, a, w, s.L);
     else if (s.rows_waves == 4) hipLaunchKernelGGL((attn_window_rows_kernel<4>), grid, dim3(64 * 4), 0, stream, a, w, s.L);
-    else hipLaunchKernelGGL(attn_window_keys_kernel, grid, dim3(64 * WAVES), 0, stream, a, w, s.L);
+    else if (s.stream) hipLaunchKernelGGL((attn_window_keys_kernel<true>), grid, dim3(64 * WAVES), 0, stream, a, w, s.L);
+    else hipLaunchKernelGGL((attn_window_keys_kernel<false>), grid, dim3(64 * WAVES), 0, stream, a, w, s.L);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess || s.workspace == 0) return err;
     if (s.rows_waves > 0) {
