@@ -213,7 +213,7 @@ template <int SHAPE, int NW> struct Sizes {
 // The rows of tile t by the workgroup, or, of `parts`, part `part` of their keys, whose record is number `place` (of those that the keys shape leaves,
 // or of the XCD's).  bad_s: rows shape, keys of a tile's blocks whose V holds
 // an infinity or NaN.
-template <int SHAPE, int NW, bool STREAM = false>
+template <int SHAPE, int NW>
 __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView& w, const WindowLayout& L, const Tile& t, int kvh, int parts, int part, int place,
                                             unsigned char* smem, int (*bad_s)[NW])
 {
@@ -287,10 +287,6 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
         const uint32_t lo = __builtin_amdgcn_readlane((int)id_vec, at), hi = __builtin_amdgcn_readlane((int)(id_vec >> 32), at);
         return (long long)(((unsigned long long)hi << 32) | lo) * SLAB;
     };
-    auto bring = [](const unsigned char* from, int offset, uint32_t to) {
-        if constexpr (STREAM) lds_dma16_streamed(from, offset, to);
-        else lds_dma16(from, offset, to);
-    };
     // this wave's share of its tile i (KEYS: all of it), into slot i % 2
     auto fetch_k = [&](int i) {
 #pragma unroll
@@ -298,7 +294,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
             const unsigned char* from = kcb + slab(i, which);
             const uint32_t to = ring + (i & 1) * TILE_BYTES + (KEYS ? which : my_block) * SLAB + j0 * 1024;
 #pragma unroll
-            for (int j = 0; j < INSTR; ++j) bring(from, k_goff[j], to + j * 1024);
+            for (int j = 0; j < INSTR; ++j) lds_dma16(from, k_goff[j], to + j * 1024);
         }
     };
     auto fetch_v = [&](int i) {
@@ -307,7 +303,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
             const unsigned char* from = vcb + slab(i, which);
             const uint32_t to = ring + (2 + (i & 1)) * TILE_BYTES + (KEYS ? which : my_block) * SLAB + j0 * 1024;
 #pragma unroll
-            for (int j = 0; j < INSTR; ++j) bring(from, v_goff + j * 1024, to + j * 1024);
+            for (int j = 0; j < INSTR; ++j) lds_dma16(from, v_goff + j * 1024, to + j * 1024);
         }
     };
     // is block v of the list seen whole by all rows of this wave?  (by all of a tile's blocks: no masks)
@@ -788,7 +784,6 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     }
 }
 
-template <bool STREAM>
 __global__ __launch_bounds__(64 * WAVES, 1) void attn_window_keys_kernel(AttnArgs a, WindowView w, WindowLayout L)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char smem[Sizes<KEYS, WAVES>::LDS];
@@ -809,7 +804,221 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attn_window_keys_kernel(AttnArg
     }
     Tile t;
     if (find_tile<WAVE_ROWS>(b, L, w, slot, t))
-        attend_tile<KEYS, WAVES, STREAM>(a, w, L, t, kvh, L.parts, part, (slot * b.num_kv_heads + kvh) * L.parts + part, smem, nullptr);
+        attend_tile<KEYS, WAVES>(a, w, L, t, kvh, L.parts, part, (slot * b.num_kv_heads + kvh) * L.parts + part, smem, nullptr);
+}
+
+// ---- Decode shape: a request's one new token, at most 16 query heads on a KV head.  As the keys shape, with 16 rows in place of 32
+// (v_mfma_f32_16x16x32_bf16: half of the products and exponentials) and without what only rows of several tokens need: all rows see the same keys.
+// Scores: lane (query lane % 16, g = lane / 16) has keys 4 g .. 4 g + 3 of a block.  Two blocks' are its 8 of the value product's 32 keys, whatever order
+// these have; V's operand is read to match.
+constexpr int DECODE_ROWS = 16;
+__device__ inline float quad_max(float x)                    // over the four lanes of a query
+{
+    const uint32_t u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ inline float quad_sum(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+template <bool STREAM>
+__global__ __launch_bounds__(64 * WAVES, 1) void attn_window_decode_kernel(AttnArgs a, WindowView w, WindowLayout L)
+{
+    constexpr int TB = 2, TILE_BYTES = TB * SLAB, RING = 4 * TILE_BYTES;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[WAVES * RING];
+    const BatchView& b = a.b;
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int pair = L.by_parts.quotient(blockIdx.x), part = blockIdx.x - pair * L.parts;
+    const int slot = L.by_kv_heads.quotient(pair), kvh = pair - slot * b.num_kv_heads, G = L.G;
+    const int new_len = b.new_lens[slot], prefix_len = b.prefix_lens[slot], cu = b.cu_new_lens[slot];
+    // every argument that is needed further down travels with the lengths
+    asm volatile("" ::"s"(a.q), "s"(a.k_cache), "s"(a.v_cache), "s"(a.out), "s"(a.lse), "s"(a.workspace), "s"(b.page_table), "s"(new_len), "s"(prefix_len), "s"(cu));
+    Tile t;
+    if (!make_tile(b, L, w, slot, 0, DECODE_ROWS, min(new_len, 1), prefix_len, cu, t)) return;
+    const int32_t* __restrict__ pt = b.page_table + (long long)slot * b.max_pages;
+
+    const int all_tiles = (t.blocks + TB - 1) / TB, share = L.by_parts.quotient(all_tiles + L.parts - 1);
+    const int t_begin = min(part * share, all_tiles), t_end = min(t_begin + share, all_tiles), t_first = t_begin + wave;
+    const int n_mine = t_end > t_first ? (t_end - t_first + WAVES - 1) / WAVES : 0;
+
+    // where this wave's blocks lie, in slabs of the pool: lane k has that of the k-th it fetches from its tile id_base on
+    constexpr int IDS = 64 / TB;
+    int id_base = 0;
+    long long id_vec = 0;
+    auto refill = [&](int i) {
+        const int blk = t.block(min((t_first + (i + lane / TB) * WAVES) * TB + lane % TB, t.blocks - 1));
+        const int page = min(max(pt[min(blk >> b.page_shift, b.max_pages - 1)], 0), b.num_pages - 1);
+        id_vec = (((long long)page * b.num_kv_heads + kvh) << b.page_shift) + (blk & ((1 << b.page_shift) - 1));
+        id_base = i;
+    };
+    if (n_mine > 0) refill(0);
+
+    const __bf16* __restrict__ qp = (const __bf16*)a.q + ((long long)t.first_row * b.num_q_heads + kvh * G + min(l16, G - 1)) * D + 8 * g;
+    bf16x8 qf[4];
+#pragma unroll
+    for (int st = 0; st < 4; ++st) qf[st] = *(const bf16x8*)(qp + 32 * st);
+
+    // an instruction brings 4 rows of 256 bytes; chunk c of K's row lies at c ^ row, of V's at c ^ ((row & 3) << 2)
+    const int ld_row = lane >> 4, ld_p = lane & 15;
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem + wave * RING;
+    unsigned char* const my_ring = smem + wave * RING;
+    const int k_goff = ld_row * 256 + ((ld_p ^ ld_row) << 4), v_goff = ld_row * 256 + ((ld_p ^ (ld_row << 2)) << 4);
+    const unsigned char* const kcb = (const unsigned char*)a.k_cache;
+    const unsigned char* const vcb = (const unsigned char*)a.v_cache;
+    auto bring = [](const unsigned char* from, int offset, uint32_t to) {
+        if constexpr (STREAM) lds_dma16_streamed(from, offset, to);
+        else lds_dma16(from, offset, to);
+    };
+    auto fetch = [&](int i) {                                // tile i into slot i % 2
+#pragma unroll
+        for (int which = 0; which < TB; ++which) {
+            const int at = (i - id_base) * TB + which;
+            const uint32_t lo = __builtin_amdgcn_readlane((int)id_vec, at), hi = __builtin_amdgcn_readlane((int)(id_vec >> 32), at);
+            const long long slab = (long long)(((unsigned long long)hi << 32) | lo) * SLAB;
+            const uint32_t to = ring + (i & 1) * TILE_BYTES + which * SLAB;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) bring(kcb + slab, (k_goff ^ (j << 6)) + j * 1024, to + j * 1024);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) bring(vcb + slab, v_goff + j * 1024, to + 2 * TILE_BYTES + j * 1024);
+        }
+    };
+    const int k_rd = l16 * 256 + ((g ^ l16) << 4);           // step st: ^ (st << 6)
+    const int v_rd = 2 * TILE_BYTES + (4 * g + (l16 >> 2)) * 256 + ((4 * (l16 >> 2) + ((l16 & 3) >> 1)) << 4) + (l16 & 1) * 8;    // channel block nb: ^ (nb << 5)
+    const int limit = t.last, low = t.low_first;
+    auto seen = [&](int key) { return key <= limit && (key >= low || key < w.sinks); };
+    auto seen_whole = [&](int key) { return key + BLK - 1 <= limit && (key >= low || key + BLK - 1 < w.sinks); };    // a block
+    const float c_log2 = b.softmax_scale * LOG2E;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o[8];
+#pragma unroll
+    for (int nb = 0; nb < 8; ++nb) o[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    if (n_mine > 0) {
+        // (q is here before the first tile is asked for: the waits below count a tile's loads)
+        asm volatile("" ::"v"(qf[0]), "v"(qf[1]), "v"(qf[2]), "v"(qf[3]) : "memory");
+        fetch(0);
+        for (int i = 0; i < n_mine; ++i) {
+            const int tile = t_first + i * WAVES;
+            // (reads of the other slot are done: their values have been used)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (i + 1 < n_mine) {
+                if (i + 1 - id_base >= IDS) refill(i + 1);
+                fetch(i + 1);
+                asm volatile("s_waitcnt vmcnt(16)" ::: "memory");            // tile i's 16 loads are those before
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+            const int key0 = t.block(tile * TB) * BLK, key1 = t.block(tile * TB + 1) * BLK;
+            const bool whole = seen_whole(key0) && seen_whole(key1);
+            const unsigned char* at = my_ring + (i & 1) * TILE_BYTES;
+            if (!whole) {
+                // V of slots that are not seen: whatever they hold, times a weight of 0, must be 0
+#pragma unroll
+                for (int j = 0; j < 4 * TB; ++j) {
+                    const int key = (j < 4 ? key0 : key1) + 4 * (j & 3) + ld_row;
+                    if (!seen(key)) *(uint4*)(my_ring + (2 + (i & 1)) * TILE_BYTES + j * 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+            f32x4 s[TB];
+#pragma unroll
+            for (int st = 0; st < 4; ++st)
+#pragma unroll
+                for (int u = 0; u < TB; ++u) {
+                    const bf16x8 kf = *(const bf16x8*)(at + u * SLAB + (k_rd ^ (st << 6)));
+                    s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[st], st == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[u], 0, 0, 0);
+                }
+            if (!whole)
+#pragma unroll
+                for (int u = 0; u < TB; ++u)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        if (!seen((u == 0 ? key0 : key1) + 4 * g + v)) s[u][v] = -INFINITY;
+            float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * c_log2;
+            if (__builtin_amdgcn_ballot_w64(top > m + LAG) != 0) {
+                top = quad_max(top);                         // (all four lanes decide alike)
+                const bool up = top > m + LAG;
+                const float alpha = up ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+                m = up ? top : m;
+                l *= alpha;
+#pragma unroll
+                for (int nb = 0; nb < 8; ++nb) o[nb] *= alpha;
+            }
+            const float ref = m == -INFINITY ? 0.f : m;
+            bf16x8 pf;
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], c_log2, -ref));
+                sum += p;                                    // (as it is, before it is rounded for the product)
+                pf[e] = (__bf16)p;
+            }
+            l += sum;
+#pragma unroll
+            for (int nb = 0; nb < 8; ++nb) {
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                const unsigned char* src = at + (v_rd ^ (nb << 5));
+                const s16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src));
+                const s16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(src + SLAB));
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(first, second, 0, 1, 2, 3, 4, 5, 6, 7));
+                o[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[nb], 0, 0, 0);
+            }
+        }
+    }
+    // ---- the waves' sums: rows of REC_STRIDE floats
+    l = quad_sum(l);
+    __syncthreads();                                         // the rings are free
+    float* mine = (float*)smem + (wave * DECODE_ROWS + l16) * REC_STRIDE;
+#pragma unroll
+    for (int nb = 0; nb < 8; ++nb) *(f32x4*)(mine + 16 * nb + 4 * g) = o[nb];
+    if (g == 0) {
+        mine[D] = m;
+        mine[D + 1] = l;
+    }
+    __syncthreads();
+    const int row = tid >> 4, ch = (tid & 15) * 4;           // 16 threads a row, 8 channels each
+    if (row >= G) return;
+    const float* first = (const float*)smem + row * REC_STRIDE;
+    float top = -INFINITY, total = 0.f, weight[WAVES];
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) top = fmaxf(top, first[k * DECODE_ROWS * REC_STRIDE + D]);
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) {
+        const float mk = first[k * DECODE_ROWS * REC_STRIDE + D];
+        weight[k] = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk - top);
+        total += weight[k] * first[k * DECODE_ROWS * REC_STRIDE + D + 1];
+    }
+    f32x4 sum[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        sum[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) sum[x] += weight[k] * *(const f32x4*)(first + k * DECODE_ROWS * REC_STRIDE + ch + 64 * x);
+    }
+    if (L.parts > 1) {
+        float* rec = (float*)a.workspace + ((long long)(pair * L.parts + part) * DECODE_ROWS + row) * REC_STRIDE;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) *(f32x4*)(rec + ch + 64 * x) = sum[x];
+        if (ch == 0) {
+            rec[D] = top;
+            rec[D + 1] = total;
+        }
+        return;
+    }
+    const float inv = total != 0.f ? 1.f / total : 0.f;
+    const long long at = (long long)t.first_row * b.num_q_heads + kvh * G + row;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        bf16x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (__bf16)(sum[x][e] * inv);
+        *(bf16x4*)((__bf16*)a.out + at * D + ch + 64 * x) = y;
+    }
+    if (a.lse != nullptr && ch == 0) a.lse[at] = top * LN2 + logf(total);
 }
 
 template <int NW>
@@ -847,6 +1056,7 @@ __device__ inline float wave_sum(float x)
 
 // Adds the records of a row tile's parts up: a wave for a row, two channels a lane, AT_ONCE parts' rows on their way at a time.
 constexpr int AT_ONCE = 16;
+template <int ROWS>                                      // of a record
 __global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs a, WindowView w, WindowLayout L, int row_groups)
 {
     const BatchView& b = a.b;
@@ -854,10 +1064,10 @@ __global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs 
     const int unit = blockIdx.x / row_groups, row = (blockIdx.x - unit * row_groups) * WAVES + wave;
     const int slot = L.by_kv_heads.quotient(unit), kvh = unit - slot * b.num_kv_heads;
     Tile t;
-    if (!find_tile<WAVE_ROWS>(b, L, w, slot, t)) return;
+    if (!find_tile<ROWS>(b, L, w, slot, t)) return;
     if (t.row0 + row >= t.n_rows) return;
-    const float* rec = (const float*)a.workspace + ((long long)unit * L.parts * WAVE_ROWS + row) * REC_STRIDE;
-    constexpr int STRIDE = WAVE_ROWS * REC_STRIDE;
+    const float* rec = (const float*)a.workspace + ((long long)unit * L.parts * ROWS + row) * REC_STRIDE;
+    constexpr int STRIDE = ROWS * REC_STRIDE;
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     float top = -INFINITY, total = 0.f, x = 0.f, y = 0.f;
     for (int k0 = 0; k0 < L.parts; k0 += 64) {
@@ -957,8 +1167,8 @@ constexpr int MIN_TILES = 4;                             // of a part
 
 // How a batch is dealt, from what the host knows.
 struct Deal {
-    int rows_waves;                                      // of a workgroup of the rows shape, 0: keys shape
-    bool stream;                                         // keys shape: K and V past the caches
+    int rows_waves;                                      // of a workgroup of the rows shape, 0: the others
+    bool decode, stream;                                 // decode shape; its K and V past the caches
     WindowLayout L;
     long long grid;
     size_t workspace;
@@ -997,7 +1207,8 @@ Deal deal_of(const BatchView& b, const WindowView& w)
     const long long slots = single ? b.num_reqs : rows / WAVE_ROWS + b.num_reqs;
     s.L.slots = (int)slots;
     s.L.single = single;
-    s.stream = single && slots * b.num_kv_heads * span * (4 * D) > STREAM_BYTES;
+    s.decode = single && b.max_new_len == 1 && G <= DECODE_ROWS;
+    s.stream = s.decode && slots * b.num_kv_heads * span * (4 * D) > STREAM_BYTES;
     // as many parts as fill the chip, each of a tile for every wave at least
     const long long tiles = (span + 31) / 32, units = (single ? slots : std::max((rows + WAVE_ROWS - 1) / WAVE_ROWS, 1ll)) * b.num_kv_heads;
     s.L.parts = (int)std::max(1ll, std::min(COMPUTE_UNITS / units, (tiles + WAVES - 1) / WAVES));
@@ -1007,7 +1218,7 @@ Deal deal_of(const BatchView& b, const WindowView& w)
     s.L.by_slots = divisor_of((int)slots);
     s.L.by_parts = divisor_of(s.L.parts);
     s.grid = single ? items : (long long)s.L.per_xcd * NUM_XCD;
-    s.workspace = s.L.parts > 1 ? (size_t)items * WAVE_ROWS * REC_STRIDE * sizeof(float) : 0;
+    s.workspace = s.L.parts > 1 ? (size_t)items * (s.decode ? DECODE_ROWS : WAVE_ROWS) * REC_STRIDE * sizeof(float) : 0;
     return s;
 }
 
@@ -1026,8 +1237,9 @@ hipError_t launch_attn_window(const AttnArgs& a, const WindowView& w, hipStream_
     const dim3 grid((unsigned)s.grid);
     if (s.rows_waves == 8) hipLaunchKernelGGL((attn_window_rows_kernel<8>), grid, dim3(64 * 8), 0, stream, a, w, s.L);
     else if (s.rows_waves == 4) hipLaunchKernelGGL((attn_window_rows_kernel<4>), grid, dim3(64 * 4), 0, stream, a, w, s.L);
-    else if (s.stream) hipLaunchKernelGGL((attn_window_keys_kernel<true>), grid, dim3(64 * WAVES), 0, stream, a, w, s.L);
-    else hipLaunchKernelGGL((attn_window_keys_kernel<false>), grid, dim3(64 * WAVES), 0, stream, a, w, s.L);
+    else if (s.stream) hipLaunchKernelGGL((attn_window_decode_kernel<true>), grid, dim3(64 * WAVES), 0, stream, a, w, s.L);
+    else if (s.decode) hipLaunchKernelGGL((attn_window_decode_kernel<false>), grid, dim3(64 * WAVES), 0, stream, a, w, s.L);
+    else hipLaunchKernelGGL(attn_window_keys_kernel, grid, dim3(64 * WAVES), 0, stream, a, w, s.L);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess || s.workspace == 0) return err;
     if (s.rows_waves > 0) {
@@ -1036,7 +1248,9 @@ hipError_t launch_attn_window(const AttnArgs& a, const WindowView& w, hipStream_
         else hipLaunchKernelGGL((attn_window_rows_merge_kernel<4>), merge, dim3(256), 0, stream, a, w, s.L);
     } else {
         const int rows = (int)std::min<long long>((long long)b.max_new_len * s.L.G, WAVE_ROWS), groups = (rows + WAVES - 1) / WAVES;
-        hipLaunchKernelGGL(attn_window_merge_kernel, dim3((unsigned)(s.L.slots * b.num_kv_heads * groups)), dim3(64 * WAVES), 0, stream, a, w, s.L, groups);
+        const dim3 merge((unsigned)(s.L.slots * b.num_kv_heads * groups));
+        if (s.decode) hipLaunchKernelGGL((attn_window_merge_kernel<DECODE_ROWS>), merge, dim3(64 * WAVES), 0, stream, a, w, s.L, groups);
+        else hipLaunchKernelGGL((attn_window_merge_kernel<WAVE_ROWS>), merge, dim3(64 * WAVES), 0, stream, a, w, s.L, groups);
     }
     return hipGetLastError();
 }
