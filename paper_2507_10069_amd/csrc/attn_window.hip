@@ -322,7 +322,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     auto look_at_v = [&](int v, unsigned char* block) -> int {
         const int key0 = t.block(v) * BLK;
         int bad = 0;
-#pragma unroll
+#pragma unroll 1
         for (int jj = 0; jj < INSTR; ++jj) {
             const int j = j0 + jj, key = key0 + 4 * j + ld_row;
             uint4* at = (uint4*)(block + j * 1024 + lane * 16);
@@ -352,6 +352,9 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
 
     const float c_log2 = b.softmax_scale * LOG2E;
     float m = -INFINITY, l = 0.f;                            // reference (times log2 e); sum of this lane's weights
+    // Lane n: which rows of V that this wave brought of the n-th tile looked at held what is not finite, 16 bits a block.  (Tiles looked at hold a slot that some
+    // rows see and others do not: at most 31 + 2 blocks' at either end of a window, and one at the sinks' end.)
+    int odd_rows = 0, looked = 0;
     f32x16 o[4];
 #pragma unroll
     for (int nb = 0; nb < 4; ++nb)
@@ -381,13 +384,12 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                // bit e: is key key0 + e seen?  The first `upto` are not behind the row's own, the first `before` are before its window, `first` are sinks.
                 const int key0 = t.block(tile * TB + 2 * (kb0 + kb) + h) * BLK + 8 * h32;
+                auto bits = [](int n) { return (1u << min(max(n, 0), 8)) - 1u; };
+                const uint32_t seen = bits(limit - key0 + 1) & (~bits(low - key0) | bits(w.sinks - key0));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int key = key0 + e;
-                    const bool seen = key <= limit && (key >= low || key < w.sinks);
-                    s[kb][8 * h + e] = seen ? s[kb][8 * h + e] : -INFINITY;
-                }
+                for (int e = 0; e < 8; ++e) s[kb][8 * h + e] = (seen & (1u << e)) != 0 ? s[kb][8 * h + e] : -INFINITY;
             }
     };
     auto top_of = [&](const f32x16 (&s)[KB]) {               // the largest of this lane's scores
@@ -486,45 +488,27 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
             if (!clear(t_first)) mask(t_first, s0);
             top = top_of(s0);
         }
-        // V(i) and K(i + 1) are there, the next ones are asked for; returns the keys of V(i) whose values are not all finite
-        struct Bad { int of[PER_TILE]; bool look; };
-        auto arrive = [&](int i) -> Bad {
+        // V(i) and K(i + 1) are there, the next ones are asked for
+        auto arrive = [&](int i) {
             const int tile = t_first + i * step;
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            Bad bad = {};
-            bad.look = !wg_clear(tile);
-            if (bad.look) {
-#pragma unroll
+            if (!wg_clear(tile)) {
+                int bad = 0;
+#pragma unroll 1
                 for (int which = 0; which < PER_TILE; ++which)
-                    bad.of[which] = look_at_v(tile * TB + (KEYS ? which : my_block), my_ring + (2 + (i & 1)) * TILE_BYTES + (KEYS ? which : my_block) * SLAB);
-                if (!KEYS && lane == 0) bad_s[i & 1][wave] = bad.of[0];
+                    bad |= look_at_v(tile * TB + (KEYS ? which : my_block), my_ring + (2 + (i & 1)) * TILE_BYTES + (KEYS ? which : my_block) * SLAB) << (16 * which);
+                odd_rows = lane == looked ? bad : odd_rows;
+                ++looked;
             }
             if constexpr (KEYS) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // all reads of the other slots are done, and V's zeros are written
             } else {
                 __syncthreads();                             // everyone's share; and everyone is past its reads of the other slots
             }
-            if (i + 2 - id_base >= IDS && i + 2 < n_mine + 2) refill(i + 1);
+            if (i + 2 - id_base >= IDS) refill(i + 1);
             if (KEYS || !active) {
                 if (i + 1 < n_mine) fetch_v(i + 1);
                 if (i + 2 < n_mine) fetch_k(i + 2);
-            }
-            return bad;
-        };
-        auto add_bad = [&](int i, const Bad& bad) {
-            if (!bad.look) return;
-            const int tile = t_first + i * step;
-            if constexpr (KEYS) {
-#pragma unroll
-                for (int which = 0; which < PER_TILE; ++which)
-                    if (bad.of[which] != 0) add_odd(tile * TB + which, bad.of[which]);
-            } else {
-                for (int k = 2 * kb0; k < (HALVED ? 2 * kb0 + 2 : TB); ++k) {
-                    int those = 0;
-#pragma unroll
-                    for (int x = 0; x < PER_BLOCK; ++x) those |= __builtin_amdgcn_readfirstlane(bad_s[i & 1][k * PER_BLOCK + x]);
-                    if (those != 0) add_odd(tile * TB + k, those);
-                }
             }
         };
         // One MFMA a slice, fenced, so that the order is the one written here: the matrix pipe has an instruction in every slice, its operand
@@ -533,7 +517,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
         //   8 KB slices   O^T += V^T P^T, and the largest of the new scores
         auto iteration = [&](int i, auto parity, f32x16 (&now)[KB], f32x16 (&next)[KB]) {
             constexpr int R = decltype(parity)::value, N = 8 * KB, AHEAD = 2;
-            const Bad bad = arrive(i);
+            arrive(i);
             if (!active) return;
             const unsigned char* k_tile = my_ring + (R ^ 1) * TILE_BYTES + kb0 * 32 * 256;
             const unsigned char* v_tile = my_ring + R * TILE_BYTES + kb0 * 32 * 256;
@@ -632,7 +616,6 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
                 __builtin_amdgcn_sched_barrier(0);
             });
             top = most * c_log2;
-            add_bad(i, bad);
         };
         using even = std::integral_constant<int, 0>;
         using odd = std::integral_constant<int, 1>;
@@ -647,16 +630,46 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) s0[kb] = s1[kb];
         }
-        const Bad bad = arrive(i);
+        arrive(i);
         if (active) {
             Weights p;
             raise(top);
             weigh(s0, p);
             multiply_v(i, p);
-            add_bad(i, bad);
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was fetched past the last tile)
+    // what was not finite and taken out, to the rows that see it
+    bool any = __builtin_amdgcn_ballot_w64(odd_rows != 0) != 0;
+    if constexpr (!KEYS) {
+        if (lane == 0) bad_s[0][wave] = any ? 1 : 0;
+        __syncthreads();                                     // (and the rings are free)
+        any = false;
+#pragma unroll
+        for (int k = 0; k < NW; ++k) any = any || __builtin_amdgcn_readfirstlane(bad_s[0][k]) != 0;
+    }
+    if (any) {
+        int* list = (int*)my_ring;                           // [waves that brought blocks][64]
+        if constexpr (!KEYS) {
+            list[wave * 64 + lane] = odd_rows;
+            __syncthreads();
+        }
+        int n = 0;
+        for (int i = 0; i < n_mine; ++i) {
+            const int tile = t_first + i * step;
+            if (wg_clear(tile)) continue;
+            for (int k = KEYS ? 0 : 2 * kb0; k < (HALVED ? 2 * kb0 + 2 : TB); ++k) {
+                int rows = 0;
+                if constexpr (KEYS) {
+                    rows = __builtin_amdgcn_readlane(odd_rows, n) >> (16 * k) & 0xffff;
+                } else {
+                    for (int x = 0; x < PER_BLOCK; ++x) rows |= __builtin_amdgcn_readfirstlane(list[(k * PER_BLOCK + x) * 64 + n]);
+                }
+                if (rows != 0 && active) add_odd(tile * TB + k, rows);
+            }
+            ++n;
+        }
+    }
     const float l_row = pair_sum(l);
     auto at_row = [&](int row) -> long long {                // row of [T][H]
         const int token = L.by_G.quotient(row);
@@ -1025,7 +1038,7 @@ template <int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_window_rows_kernel(AttnArgs a, WindowView w, WindowLayout L)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char smem[Sizes<ROWS, NW>::LDS];
-    __shared__ int bad_s[2][NW];
+    __shared__ int bad_s[1][NW];
     const BatchView& b = a.b;
     Lines<NW> lines = {b};
     const int tiles = lines.total(L), i = blockIdx.x / NUM_XCD;
