@@ -157,29 +157,57 @@ template <int NW> struct Lines {
         new_len = b.new_lens[r];
         prefix_len = b.prefix_lens[r];
         cu = b.cu_new_lens[r];
-        incl = scan64(from + lane < b.num_reqs ? (clamp_new_len(b, new_len, true) * L.G + WIDE_ROWS - 1) / WIDE_ROWS : 0);
+        incl = scan64(from + lane < b.num_reqs ? tiles_of(L, new_len) : 0);
         return __builtin_amdgcn_readlane(incl, 63);
     }
+    // of one request
+    __device__ int tiles_of(const WindowLayout& L, int length) const { return (clamp_new_len(b, length, true) * L.G + WIDE_ROWS - 1) / WIDE_ROWS; }
     __device__ int total(const WindowLayout& L)
     {
-        int sum = 0;
-        for (int from = 0; from < b.num_reqs; from += 64) sum += look(L, from);
-        return sum;
+        if (b.num_reqs <= 64) return look(L, 0);
+        int sum = 0;                                     // of this lane's requests: their lengths travel together
+        for (int r = threadIdx.x & 63; r < b.num_reqs; r += 64) sum += tiles_of(L, b.new_lens[r]);
+        return __builtin_amdgcn_readlane(scan64(sum), 63);
     }
     // the n-th row tile of all, n < total(); half 0 or 1: that half of its rows
     __device__ bool take(const WindowLayout& L, const WindowView& w, int n, int half, Tile& t)
     {
         int from = 0;
         if (b.num_reqs > 64) {
-            for (int count = look(L, 0); n >= count && from + 64 < b.num_reqs; count = look(L, from)) {
-                n -= count;
-                from += 64;
+            // which 64 requests it is among, 256 at a time
+            const int lane = threadIdx.x & 63;
+            for (;; from += 256) {
+                int count[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int r = from + 64 * k + lane;
+                    count[k] = r < b.num_reqs ? tiles_of(L, b.new_lens[r]) : 0;
+                }
+                bool here = from + 256 >= b.num_reqs;
+#pragma unroll
+                for (int k = 3; k >= 0; --k) count[k] = __builtin_amdgcn_readlane(scan64(count[k]), 63);
+                if (n < count[0] + count[1] + count[2] + count[3]) here = true;
+                if (!here) {
+                    n -= count[0] + count[1] + count[2] + count[3];
+                    continue;
+                }
+                int at = 0;
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    if (at == k && n >= count[k]) {
+                        n -= count[k];
+                        ++at;
+                    }
+                from += 64 * at;
+                break;
             }
+            if (from >= b.num_reqs) return false;
+            look(L, from);
         }
         const unsigned long long hit = __builtin_amdgcn_ballot_w64(incl > n);
         if (hit == 0) return false;
         const int at = __builtin_ctzll(hit);
-        const int length = __builtin_amdgcn_readlane(new_len, at), tiles = (clamp_new_len(b, length, true) * L.G + WIDE_ROWS - 1) / WIDE_ROWS;
+        const int length = __builtin_amdgcn_readlane(new_len, at), tiles = tiles_of(L, length);
         const int tile = n - (__builtin_amdgcn_readlane(incl, at) - tiles);
         return make_tile(b, L, w, from + at, (long long)tile * WIDE_ROWS + max(half, 0) * (WIDE_ROWS / 2), half >= 0 ? WIDE_ROWS / 2 : WIDE_ROWS, length,
                          __builtin_amdgcn_readlane(prefix_len, at), __builtin_amdgcn_readlane(cu, at), t);
@@ -1173,7 +1201,7 @@ __global__ __launch_bounds__(256) void attn_window_rows_merge_kernel(AttnArgs a,
 
 constexpr int COMPUTE_UNITS = 256;
 constexpr long long STREAM_BYTES = 96ll << 20;           // of K and V, each read once: more than the last-level cache keeps for a next call
-constexpr int ROWS_UNITS = 24;                          // units of 128 rows from which the rows shape is taken
+constexpr int ROWS_UNITS = 16;                          // units of 128 rows from which the rows shape is taken
 constexpr int LONG_TILES = 32;                           // tiles of 64 keys from which on its workgroups have eight waves, and their last units are cut
 constexpr int CUT_ROUNDS = 4;                            // ... unless there are so many rounds that the last one is a small part; short ones' only if they are all there is
 constexpr int MIN_TILES = 4;                             // of a part
@@ -1198,7 +1226,8 @@ Deal deal_of(const BatchView& b, const WindowView& w)
     // the most that 32 rows look at
     const long long span = std::min((long long)b.max_pages * b.page_size, (long long)w.window + w.sinks + WAVE_ROWS / G + 1);
     const bool lengthy = (span + 63) / 64 >= LONG_TILES;
-    if (!single && (rows + 127) / 128 * b.num_kv_heads >= ROWS_UNITS) {
+    const long long least_units = std::max<long long>((rows + 127) / 128, std::min(b.num_reqs, b.total_new_tokens)) * b.num_kv_heads;
+    if (!single && least_units >= ROWS_UNITS) {
         s.rows_waves = lengthy ? 8 : 4;
         const int tile_rows = 32 * s.rows_waves, slots = 256 / s.rows_waves;
         const bool uniform = (long long)b.num_reqs * b.max_new_len == b.total_new_tokens;

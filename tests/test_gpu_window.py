@@ -198,6 +198,13 @@ def test_infinities_and_nan_reach_the_rows_that_see_them_alone(prefix, new, head
     assert not np.isfinite(_f64(out)).all() or max(new) == 1
 
 
+def test_hundreds_of_requests_with_some_tokens():
+    rng = np.random.default_rng(8)
+    new = rng.integers(0, 60, 700).tolist()
+    new[3] = 300
+    Case(rng.integers(0, 200, 700).tolist(), new, 64, 3, heads=8, kv_heads=2, seed=8, extra_rows=9).run_and_check()
+
+
 def test_scores_that_differ_by_far():
     """Scores of hundreds: the reference has to be raised on the way, and what came before vanishes."""
     for seed in range(3):
