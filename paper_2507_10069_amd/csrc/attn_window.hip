@@ -541,8 +541,10 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
         };
         // One MFMA a slice, fenced, so that the order is the one written here: the matrix pipe has an instruction in every slice, its operand
         // was read from LDS AHEAD slices before, and the softmax fills the slots between.
-        //   8 KB slices   S^T(i + 1) = K Q^T, and tile i's weights, a pair a slice: scaled, exponentials, then sums and rounding, a slice apart each
-        //   8 KB slices   O^T += V^T P^T, and the largest of the new scores
+        //   8 KB slices   S^T(i + 1) = K Q^T
+        //   8 KB slices   O^T += V^T P^T
+        // Beside both tile i's weights, two pairs in three slices: scaled, exponentials, then sums and rounding; beside the last the largest of the new scores.
+        // (With a pair a slice, done with the scores, those slices were bound by the softmax and the others by the products, and the waves of a SIMD are in step.)
         auto iteration = [&](int i, auto parity, f32x16 (&now)[KB], f32x16 (&next)[KB]) {
             constexpr int R = decltype(parity)::value, N = 8 * KB, AHEAD = 2;
             arrive(i);
@@ -595,7 +597,23 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
                 pin(sum0);
                 pin(sum1);
             };
-            scaled(std::integral_constant<int, 0>{});
+            // a pair's three steps, a slice apart, begin at slice SPREAD / 10 times its number: before they are needed, and over as many slices as may be
+            constexpr int SPREAD = KB == 2 ? 15 : 14;
+            auto soften = [&](auto n) {
+                constexpr int k = decltype(n)::value;
+                static_for<0, N>([&](auto pair) {
+                    constexpr int from = decltype(pair)::value * SPREAD / 10;
+                    if constexpr (k == from + 1) raised(pair);
+                });
+                static_for<0, N>([&](auto pair) {
+                    constexpr int from = decltype(pair)::value * SPREAD / 10;
+                    if constexpr (k == from + 2) rounded(pair);
+                });
+                static_for<0, N>([&](auto pair) {
+                    constexpr int from = decltype(pair)::value * SPREAD / 10;
+                    if constexpr (k == from) scaled(pair);
+                });
+            };
             __builtin_amdgcn_sched_barrier(0);
             static_for<0, N>([&](auto n) {
                 constexpr int k = decltype(n)::value, kb = k % KB, st = k / KB;
@@ -611,22 +629,18 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
                 // (rows shapes: in between, and past the last tile the list's last blocks again, which costs less than a branch)
                 if constexpr (!KEYS && k == 1) fetch_v(i + 1);
                 if constexpr (!KEYS && k == 3) fetch_k(i + 2);
-                raised(n);
-                if constexpr (k > 0) rounded(std::integral_constant<int, k - 1>{});
-                if constexpr (k + 1 < N) scaled(std::integral_constant<int, k + 1>{});
+                soften(n);
                 __builtin_amdgcn_sched_barrier(0);
             });
-            rounded(std::integral_constant<int, N - 1>{});
-            l += sum0 + sum1;
-            __builtin_amdgcn_sched_barrier(0);
             auto product = [&](auto n) {
                 constexpr int k = decltype(n)::value, block = k / 4, nb = k % 4;
                 if constexpr (N + k + AHEAD < 2 * N) operand[N + k + AHEAD] = read(std::integral_constant<int, N + k + AHEAD>{});
                 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
                 const u32x4 pw = {p[block >> 1][block & 1][0], p[block >> 1][block & 1][1], p[block >> 1][block & 1][2], p[block >> 1][block & 1][3]};
                 o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand[N + k], __builtin_bit_cast(bf16x8, pw), o[nb], 0, 0, 0);
+                soften(std::integral_constant<int, N + k>{});
             };
-            constexpr int FIRST = 4;                         // value products before the new scores are looked at
+            constexpr int FIRST = N / 2;                     // value products before the new scores are looked at
             static_for<0, FIRST>([&](auto n) {
                 product(n);
                 __builtin_amdgcn_sched_barrier(0);
@@ -643,6 +657,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
                 pin(most);
                 __builtin_amdgcn_sched_barrier(0);
             });
+            l += sum0 + sum1;
             top = most * c_log2;
         };
         using even = std::integral_constant<int, 0>;
