@@ -521,8 +521,10 @@ def _check_rows(batch: emm_batch, norm, rope, slots=None) -> None:
         _check_positions(batch, rope)
     if norm is not None and norm._head_dim is not None and norm._head_dim != batch.head_dim:
         raise ValueError("norm weights of %d channels, heads of %d" % (norm._head_dim, batch.head_dim))
-    if slots is not None and (str(slots.dtype) != "torch.int64" or not slots.is_contiguous() or slots.numel() < batch.total_new_tokens):
-        raise ValueError("slots are a contiguous int64 tensor, one for each of %d tokens" % batch.total_new_tokens)
+    if slots is not None:
+        import torch
+        if slots.dtype is not torch.int64 or not slots.is_contiguous() or slots.numel() < batch.total_new_tokens:     # (a dtype's name takes longer than the rest)
+            raise ValueError("slots are a contiguous int64 tensor, one for each of %d tokens" % batch.total_new_tokens)
 
 
 def emm_norm_rope(batch: emm_batch, norm: Optional[emm_qk_norm], rope: Optional[emm_rope_params], q, k, q_out, k_out, token_stride: int = 0,

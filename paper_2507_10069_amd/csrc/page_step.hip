@@ -65,7 +65,7 @@ __global__ __launch_bounds__(NT) void page_step_kernel(PageStepArgs a)
 {
     constexpr int REQS = NT * ITEMS;
     __shared__ int back_end[REQS], first_back[REQS], need_end[REQS], cu_end[REQS], len_of[REQS];
-    __shared__ int part[2][NT / 64], part2[2][NT / 64];
+    __shared__ int part[3][NT / 64], part2[2][NT / 64], odd[NT / 64];
     const int tid = threadIdx.x;
     const int ps_log2 = 4 + a.page_shift, ps = 1 << ps_log2, width = a.max_pages, n = a.num_reqs;
     const int row_slots = (int)min((long long)width << ps_log2, 1ll << 30);
@@ -82,7 +82,8 @@ __global__ __launch_bounds__(NT) void page_step_kernel(PageStepArgs a)
         held[i] = here ? a.held_from[r] : 0;
     }
     const int count = min(max(a.free_count[0], 0), a.num_pages);
-    int sums[2] = {0, 0};                                    // of back and need, of this thread's requests
+    int sums[3] = {0, 0, 0};                                 // of back, need and tokens, of this thread's requests
+    bool misfit = false;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const bool here = tid * ITEMS + i < n;
@@ -94,17 +95,27 @@ __global__ __launch_bounds__(NT) void page_step_kernel(PageStepArgs a)
         back[i] = held[i] - start[i];
         fits[i] = add[i] <= row_slots - len[i];
         if (!fits[i]) add[i] = -1;                           // (refused whatever is free)
+        misfit = misfit || !fits[i];
         const int m = max(add[i], 0);
         need[i] = ((len[i] + m + ps - 1) >> ps_log2) - ((len[i] + ps - 1) >> ps_log2);
         sums[0] = sat_add(sums[0], back[i]);
         sums[1] = sat_add(sums[1], need[i]);
+        sums[2] = sat_add(sums[2], m);
     }
-    int total[2], mine[2] = {sums[0], sums[1]};
-    scan_block<2, NT>(sums, total, part);
+    int total[3], mine[3] = {sums[0], sums[1], sums[2]};
+    __shared__ int taken_s;
+    if (tid == 0) taken_s = 0;
+    if (__builtin_amdgcn_ballot_w64(misfit) != 0) odd[tid >> 6] = 1;
+    else odd[tid >> 6] = 0;
+    scan_block<3, NT>(sums, total, part);                    // (its barrier is the one behind which the others see these)
+#pragma unroll
+    for (int k = 0; k < NT / 64; ++k) misfit = misfit || odd[k] != 0;
     const int free_now = sat_add(count, total[0]);           // pages on the stack before any is taken
 
     // ---- who is served, and the packed offsets.  Of those that need pages the served ones are the first: the sum of all up to and
     //      with them is what the stack holds.
+    // Mostly everybody is, and the offsets are the sums that there are; else they are taken again.
+    const bool all_served = !misfit && total[1] <= free_now;
     int new_len[ITEMS], ends[2] = {0, 0};                    // tokens; requests refused
     int need_at[ITEMS], back_at[ITEMS];
     {
@@ -123,16 +134,18 @@ __global__ __launch_bounds__(NT) void page_step_kernel(PageStepArgs a)
             if (!served && add[i] != 0 && tid * ITEMS + i < n) ends[1] += 1;
         }
     }
-    int total2[2], mine_new = ends[0];
-    // pages taken: the running sum at the last served request that needs some
-    int taken_here = 0;
+    int total2[2] = {total[2], 0}, mine_new = ends[0], taken = total[1];
+    if (all_served) {
+        ends[0] = sums[2];
+    } else {
+        // pages taken: the running sum at the last served request that needs some
+        int taken_here = 0;
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
-        if (need[i] > 0) taken_here = need_at[i];
-    __shared__ int taken_s;
-    if (tid == 0) taken_s = 0;
-    scan_block<2, NT>(ends, total2, part2);                  // (its barrier is the one behind which taken_s is 0)
-    if (taken_here > 0) atomicMax(&taken_s, taken_here);     // (a maximum of whole numbers: the same in any order)
+        for (int i = 0; i < ITEMS; ++i)
+            if (need[i] > 0) taken_here = need_at[i];
+        scan_block<2, NT>(ends, total2, part2);
+        if (taken_here > 0) atomicMax(&taken_s, taken_here); // (a maximum of whole numbers: the same in any order)
+    }
     {
         int at = ends[0] - mine_new;
 #pragma unroll
@@ -160,7 +173,8 @@ __global__ __launch_bounds__(NT) void page_step_kernel(PageStepArgs a)
         }
     }
     __syncthreads();
-    const int taken = taken_s, tokens = min(total2[0], a.max_tokens), left = free_now - taken;
+    if (!all_served) taken = taken_s;
+    const int tokens = min(total2[0], a.max_tokens), left = free_now - taken;
     if (blockIdx.x == 0 && tid == 0) {
         if (MODE != NO_STATE) a.free_count_out[0] = min(left, a.num_pages);
         if (MODE != STATE) {
@@ -189,28 +203,35 @@ __global__ __launch_bounds__(NT) void page_step_kernel(PageStepArgs a)
     };
     const int stride = gridDim.x * NT;
     const int pushed = min(left, a.num_pages) - count;       // pages that were given back and not taken lie on the stack
-    const int most = max(max(pushed, taken), a.max_tokens);
-    for (int x = blockIdx.x * NT + tid; x < most; x += stride) {
-        if (x < pushed) a.free_pages[count + x] = *given_back(x);
-        if (x < taken) {
+    // Whole waves of each of the three kinds, one kind after the other, so that their chains of loads run side by side.
+    auto waves = [](int n) { return (max(n, 0) + 63) & ~63; };
+    const int first_pop = waves(pushed), first_token = first_pop + waves(taken), end = first_token + a.max_tokens;
+    for (int item = blockIdx.x * NT + tid; item < end; item += stride) {
+        if (item < first_pop) {
+            if (item < pushed) a.free_pages[count + item] = *given_back(item);
+        } else if (item < first_token) {
+            const int x = item - first_pop;
+            if (x >= taken) continue;
             const int r = first_beyond(need_end, x);
             const int before = r > 0 ? need_end[r - 1] : 0;
             const int entry = ((len_of[r] + ps - 1) >> ps_log2) + x - before;
             if (entry < width) a.page_table[(long long)r * width + entry] = page_taken(x);
-        }
-        if (x < tokens) {
-            const int r = first_beyond(cu_end, x);
-            const int position = len_of[r] + x - (r > 0 ? cu_end[r - 1] : 0);
-            if (a.positions != nullptr) a.positions[x] = position;
-            if (a.slots != nullptr) {
+        } else {
+            const int x = item - first_token;
+            int position = 0;
+            int64_t slot = -1;
+            if (x < tokens) {
+                const int r = first_beyond(cu_end, x);
+                position = len_of[r] + x - (r > 0 ? cu_end[r - 1] : 0);
                 const int have = (len_of[r] + ps - 1) >> ps_log2, entry = position >> ps_log2;
-                const int page = entry < have ? a.page_table[(long long)r * width + min(entry, width - 1)]
-                                              : page_taken((r > 0 ? need_end[r - 1] : 0) + entry - have);
-                a.slots[x] = (int64_t)page * ps + (position & (ps - 1));
+                if (a.slots != nullptr) {
+                    const int page = entry < have ? a.page_table[(long long)r * width + min(entry, width - 1)]
+                                                  : page_taken((r > 0 ? need_end[r - 1] : 0) + entry - have);
+                    slot = (int64_t)page * ps + (position & (ps - 1));
+                }
             }
-        } else if (x < a.max_tokens) {
-            if (a.positions != nullptr) a.positions[x] = 0;
-            if (a.slots != nullptr) a.slots[x] = -1;
+            if (a.positions != nullptr) a.positions[x] = position;
+            if (a.slots != nullptr) a.slots[x] = slot;
         }
     }
 }
