@@ -118,19 +118,23 @@ __device__ inline float row_norm(const float (&x)[8], const float (&y)[8], float
     return norm;
 }
 
+// waves that share a token's rows
+struct Splits {
+    int n;
+    Divisor by;
+};
 enum Cache { NO_CACHE, FP8, PLAIN /* in the batch's dtype */ };
 
 // rows of a token: K heads, then (with a cache) V heads, then q heads
 template <typename T, int D, int CACHE, bool ROPE, bool NORM>
-__device__ __forceinline__ void do_rows(const BatchView& b, const RopeView& rope, const NewRows& rows, const Fp8Pools& pools, const PlainPools& plain,
-                                        const NormView& norm, int splits)
+__device__ __forceinline__ void do_rows(BatchView b, RopeView rope, NewRows rows, Fp8Pools pools, PlainPools plain, NormView norm, Splits split)
 {
     constexpr bool QUANT = CACHE == FP8, CACHED = CACHE != NO_CACHE;
     constexpr int UNITS = D / 16, ROWS = 64 / UNITS;
     __shared__ float2 turns[WAVES][D / 2];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const long long item = (long long)blockIdx.x * WAVES + wave;
-    const int t = (int)(item / splits), part = (int)(item - (long long)t * splits);
+    const int item = blockIdx.x * WAVES + wave, splits = split.n;        // (at most 2^25 and a workgroup's)
+    const int t = split.by.quotient(item), part = item - t * splits;
     if (t >= b.total_new_tokens) return;
 
     const int n_k = rows.k != nullptr ? b.num_kv_heads : 0, n_v = CACHED ? b.num_kv_heads : 0, n_q = rows.q != nullptr ? b.num_q_heads : 0;
@@ -283,7 +287,7 @@ __device__ __forceinline__ void do_rows(const BatchView& b, const RopeView& rope
 }
 
 template <typename T, int D, bool QUANT, bool ROPE>
-__global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, RopeView rope, NewRows rows, Fp8Pools pools, int splits)
+__global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, RopeView rope, NewRows rows, Fp8Pools pools, Splits splits)
 {
     do_rows<T, D, QUANT ? FP8 : NO_CACHE, ROPE, false>(b, rope, rows, pools, PlainPools{}, NormView{}, splits);
 }
@@ -291,7 +295,7 @@ __global__ __launch_bounds__(64 * WAVES) void rope_rows_kernel(BatchView b, Rope
 // With norms, a cache in the batch's dtype, or given slots
 template <typename T, int D, int CACHE, bool ROPE, bool NORM>
 __global__ __launch_bounds__(64 * WAVES) void norm_rope_rows_kernel(BatchView b, RopeView rope, NewRows rows, Fp8Pools pools, PlainPools plain,
-                                                                    NormView norm, int splits)
+                                                                    NormView norm, Splits splits)
 {
     do_rows<T, D, CACHE, ROPE, NORM>(b, rope, rows, pools, plain, norm, splits);
 }
@@ -355,14 +359,14 @@ __global__ __launch_bounds__(64 * WAVES) void kv_gather_fp8_kernel(BatchView b, 
 
 // Few tokens: a wave for each pass over a token's rows, which takes its turns by itself; many: a wave for a token.
 template <int D>
-int splits_of(const BatchView& b, const NewRows& rows, bool cached, dim3& grid)
+Splits splits_of(const BatchView& b, const NewRows& rows, bool cached, dim3& grid)
 {
     const int heads = (rows.k != nullptr ? b.num_kv_heads : 0) + (cached ? b.num_kv_heads : 0) + (rows.q != nullptr ? b.num_q_heads : 0);
     const int passes = (heads * (D / 16) + 63) / 64;
     const int splits = (long long)b.total_new_tokens * passes <= MOST_SPLIT ? passes : 1;
     const long long items = (long long)b.total_new_tokens * splits;
     grid = dim3((unsigned)((items + WAVES - 1) / WAVES));
-    return splits;
+    return {splits, divisor_of(splits)};
 }
 
 template <typename T, int D>
@@ -370,7 +374,7 @@ hipError_t launch_rows(const BatchView& b, const RopeView& rope, const NewRows& 
 {
     dim3 grid;
     const dim3 block(64 * WAVES);
-    const int splits = splits_of<D>(b, rows, pools != nullptr, grid);
+    const Splits splits = splits_of<D>(b, rows, pools != nullptr, grid);
     if (pools == nullptr) hipLaunchKernelGGL((rope_rows_kernel<T, D, false, true>), grid, block, 0, stream, b, rope, rows, Fp8Pools{}, splits);
     else if (rope.rotary_dim > 0) hipLaunchKernelGGL((rope_rows_kernel<T, D, true, true>), grid, block, 0, stream, b, rope, rows, *pools, splits);
     else hipLaunchKernelGGL((rope_rows_kernel<T, D, true, false>), grid, block, 0, stream, b, rope, rows, *pools, splits);
@@ -383,7 +387,7 @@ hipError_t launch_norm_rows(const BatchView& b, const NormView& norm, const Rope
 {
     dim3 grid;
     const dim3 block(64 * WAVES);
-    const int splits = splits_of<D>(b, rows, CACHE != NO_CACHE, grid);
+    const Splits splits = splits_of<D>(b, rows, CACHE != NO_CACHE, grid);
     const bool turns = rope.rotary_dim > 0, norms = norm.q_weight != nullptr;
     if (turns && norms) hipLaunchKernelGGL((norm_rope_rows_kernel<T, D, CACHE, true, true>), grid, block, 0, stream, b, rope, rows, fp8, plain, norm, splits);
     else if (norms) hipLaunchKernelGGL((norm_rope_rows_kernel<T, D, CACHE, false, true>), grid, block, 0, stream, b, rope, rows, fp8, plain, norm, splits);
