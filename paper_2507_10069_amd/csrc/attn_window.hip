@@ -66,6 +66,13 @@ struct Tile {
     __device__ int block(int v) const { return v + (v >= sink_blocks ? gap : 0); }
 };
 
+// How a row tile's keys are cut where the host has given it `parts` workgroups, from what a window may hold: each takes `share` of its tiles, so many at least
+// as are worth a workgroup, so that a context shorter than its window has fewer parts, and the others nothing to do and no record.
+constexpr int MIN_TILES = 4;                             // of a part: of the decode shape one of 32 keys for each wave, of the rows shape of 64
+constexpr int MIN_TILES_KEYS = 1;                        // (20 tokens of 320 11.7 us, in parts of four 13.3)
+__device__ inline int share_of(int tiles, int parts, const Divisor& by_parts, int least) { return max(by_parts.quotient(tiles + parts - 1), least); }
+__device__ inline int share_of(int tiles, int parts) { return max((tiles + parts - 1) / parts, MIN_TILES); }
+
 // The tile of `rows` rows from row0 on of a request with these lengths; false: it has no such rows.
 __device__ inline bool make_tile(const BatchView& b, const WindowLayout& L, const WindowView& w, int r, long long row0, int rows, int new_len,
                                  int prefix_len, int cu, Tile& t)
@@ -260,9 +267,11 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     const int all_tiles = (t.blocks + TB - 1) / TB;
     int t_begin = 0, t_end = all_tiles;
     if (KEYS || (SHAPE == ROWS && parts > 1)) {
-        const int share = KEYS ? L.by_parts.quotient(all_tiles + parts - 1) : (all_tiles + parts - 1) / parts;
-        t_begin = min(part * share, all_tiles);
+        const int share = KEYS ? share_of(all_tiles, parts, L.by_parts, MIN_TILES_KEYS) : share_of(all_tiles, parts);
+        t_begin = part * share;                              // (at most the tiles and a share for each part more)
+        if (t_begin >= all_tiles) return;
         t_end = min(t_begin + share, all_tiles);
+        if (share >= all_tiles) parts = 1;                   // this one does it all
     }
     const int step = KEYS ? NW : 1, t_first = KEYS ? t_begin + wave : t_begin;
     const int n_mine = t_end > t_first ? (t_end - t_first + step - 1) / step : 0;
@@ -897,8 +906,9 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attn_window_decode_kernel(AttnA
     if (!make_tile(b, L, w, slot, 0, DECODE_ROWS, min(new_len, 1), prefix_len, cu, t)) return;
     const int32_t* __restrict__ pt = b.page_table + (long long)slot * b.max_pages;
 
-    const int all_tiles = (t.blocks + TB - 1) / TB, share = L.by_parts.quotient(all_tiles + L.parts - 1);
-    const int t_begin = min(part * share, all_tiles), t_end = min(t_begin + share, all_tiles), t_first = t_begin + wave;
+    const int all_tiles = (t.blocks + TB - 1) / TB, share = share_of(all_tiles, L.parts, L.by_parts, MIN_TILES);
+    const int t_begin = part * share, t_end = min(t_begin + share, all_tiles), t_first = t_begin + wave;
+    if (t_begin >= all_tiles) return;
     const int n_mine = t_end > t_first ? (t_end - t_first + WAVES - 1) / WAVES : 0;
 
     // where this wave's blocks lie, in slabs of the pool: lane k has that of the k-th it fetches from its tile id_base on
@@ -1055,7 +1065,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void attn_window_decode_kernel(AttnA
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) sum[x] += weight[k] * *(const f32x4*)(first + k * DECODE_ROWS * REC_STRIDE + ch + 64 * x);
     }
-    if (L.parts > 1) {
+    if (share < all_tiles) {                                 // one of several parts
         float* rec = (float*)a.workspace + ((long long)(pair * L.parts + part) * DECODE_ROWS + row) * REC_STRIDE;
 #pragma unroll
         for (int x = 0; x < 2; ++x) *(f32x4*)(rec + ch + 64 * x) = sum[x];
@@ -1119,34 +1129,42 @@ __global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int unit = blockIdx.x / row_groups, row = (blockIdx.x - unit * row_groups) * WAVES + wave;
     const int slot = L.by_kv_heads.quotient(unit), kvh = unit - slot * b.num_kv_heads;
-    Tile t;
-    if (!find_tile<ROWS>(b, L, w, slot, t)) return;
-    if (t.row0 + row >= t.n_rows) return;
-    const float* rec = (const float*)a.workspace + ((long long)unit * L.parts * ROWS + row) * REC_STRIDE;
+    const float* rec = (const float*)a.workspace + ((long long)unit * L.parts * ROWS + min(row, ROWS - 1)) * REC_STRIDE;
     constexpr int STRIDE = ROWS * REC_STRIDE;
     typedef float f32x2 __attribute__((ext_vector_type(2)));
-    float top = -INFINITY, total = 0.f, x = 0.f, y = 0.f;
-    for (int k0 = 0; k0 < L.parts; k0 += 64) {
-        // lane k has the reference and the sum of part k0 + k
-        const f32x2 ml = *(const f32x2*)(rec + (long long)min(k0 + lane, L.parts - 1) * STRIDE + D);
-        const float m = k0 + lane < L.parts ? ml[0] : -INFINITY;
-        f32x2 v[AT_ONCE];
-        auto ask = [&](int k) {
+    // Records travel with the lengths that say which of them there are: what the others hold is not looked at.
+    f32x2 ml, v[AT_ONCE];
+    auto ask_sums = [&](int k0) { ml = *(const f32x2*)(rec + (long long)min(k0 + lane, L.parts - 1) * STRIDE + D); };      // lane k: reference and sum of part k0 + k
+    auto ask = [&](int k) {
 #pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) v[u] = *(const f32x2*)(rec + (long long)min(k + u, L.parts - 1) * STRIDE + 2 * lane);
-        };
-        ask(k0);
+        for (int u = 0; u < AT_ONCE; ++u) v[u] = *(const f32x2*)(rec + (long long)min(k + u, L.parts - 1) * STRIDE + 2 * lane);
+    };
+    ask_sums(0);
+    ask(0);
+    Tile t;
+    if (!find_tile<ROWS>(b, L, w, slot, t)) return;
+    if (row >= ROWS || t.row0 + row >= t.n_rows) return;
+    const int tiles = (t.blocks + 1) / 2, share = share_of(tiles, L.parts, L.by_parts, ROWS == DECODE_ROWS ? MIN_TILES : MIN_TILES_KEYS);       // (of 32 keys)
+    if (share >= tiles) return;                              // in one part: done
+    float top = -INFINITY, total = 0.f, x = 0.f, y = 0.f;
+    for (int k0 = 0; k0 * share < tiles; k0 += 64) {
+        if (k0 > 0) {
+            ask_sums(k0);
+            ask(k0);
+        }
+        const bool mine = (k0 + lane) * share < tiles;       // is there that part?
+        const float m = mine ? ml[0] : -INFINITY;
         const float most = fmaxf(top, wave_max(m));
         const float before = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - most), weight = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - most);
         top = most;
-        total = total * before + wave_sum(k0 + lane < L.parts ? weight * ml[1] : 0.f);
+        total = total * before + wave_sum(mine ? weight * ml[1] : 0.f);
         x *= before;
         y *= before;
-        for (int k = k0; k < min(k0 + 64, L.parts); k += AT_ONCE) {
+        for (int k = k0; k < k0 + 64 && k * share < tiles; k += AT_ONCE) {
             if (k > k0) ask(k);
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
-                const float w_u = k + u < L.parts ? __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(weight), (k + u - k0) & 63)) : 0.f;
+                const float w_u = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(weight), (k + u - k0) & 63));
                 x = w_u != 0.f ? fmaf(w_u, v[u][0], x) : x;
                 y = w_u != 0.f ? fmaf(w_u, v[u][1], y) : y;
             }
@@ -1178,6 +1196,9 @@ __global__ __launch_bounds__(256) void attn_window_rows_merge_kernel(AttnArgs a,
     const int unit = plan.first + plan.whole + nth, kvh = unit / tiles;
     Tile t;
     if (!lines.take(L, w, unit - kvh * tiles, -1, t)) return;
+    const int tiles_here = (t.blocks + 3) / 4, share_here = share_of(tiles_here, plan.parts);        // (of 64 keys)
+    if (share_here >= tiles_here) return;                    // in one part: done
+    const int parts = (tiles_here + share_here - 1) / share_here;
     const float* rec = Record<NW>::at(a.workspace, xcd, nth * plan.parts);
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     for (int item = (share * SUB + sub) * 256 + threadIdx.x; item < 16 * THREADS; item += plan.parts * SUB * 256) {
@@ -1187,18 +1208,18 @@ __global__ __launch_bounds__(256) void attn_window_rows_merge_kernel(AttnArgs a,
         f32x2 ml[MOST_PARTS];
 #pragma unroll
         for (int k = 0; k < MOST_PARTS; ++k)
-            if (k < plan.parts) {
+            if (k < parts) {
                 ml[k] = *(const f32x2*)(rec + (size_t)k * Record<NW>::FLOATS + 64 * THREADS + 2 * col);
                 v[k] = *(const f32x4*)(rec + (size_t)k * Record<NW>::FLOATS + item * 4);
             }
         float top = -INFINITY, total = 0.f;
 #pragma unroll
         for (int k = 0; k < MOST_PARTS; ++k)
-            if (k < plan.parts) top = fmaxf(top, ml[k][0]);
+            if (k < parts) top = fmaxf(top, ml[k][0]);
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < MOST_PARTS; ++k)
-            if (k < plan.parts) {
+            if (k < parts) {
                 const float weight = ml[k][0] != -INFINITY ? __builtin_amdgcn_exp2f(ml[k][0] - top) : 0.f;
                 total += weight * ml[k][1];
                 if (weight != 0.f) sum += weight * v[k];
@@ -1219,7 +1240,6 @@ constexpr long long STREAM_BYTES = 96ll << 20;           // of K and V, each rea
 constexpr int ROWS_UNITS = 16;                          // units of 128 rows from which the rows shape is taken
 constexpr int LONG_TILES = 32;                           // tiles of 64 keys from which on its workgroups have eight waves, and their last units are cut
 constexpr int CUT_ROUNDS = 4;                            // ... unless there are so many rounds that the last one is a small part; short ones' only if they are all there is
-constexpr int MIN_TILES = 4;                             // of a part
 
 // How a batch is dealt, from what the host knows.
 struct Deal {
@@ -1268,7 +1288,7 @@ Deal deal_of(const BatchView& b, const WindowView& w)
     s.stream = s.decode && slots * b.num_kv_heads * span * (4 * D) > STREAM_BYTES;
     // as many parts as fill the chip, each of a tile for every wave at least
     const long long tiles = (span + 31) / 32, units = (single ? slots : std::max((rows + WAVE_ROWS - 1) / WAVE_ROWS, 1ll)) * b.num_kv_heads;
-    s.L.parts = (int)std::max(1ll, std::min(COMPUTE_UNITS / units, (tiles + WAVES - 1) / WAVES));
+    s.L.parts = (int)std::max(1ll, std::min(COMPUTE_UNITS / units, (tiles + MIN_TILES - 1) / MIN_TILES));
     const long long items = slots * b.num_kv_heads * s.L.parts;
     s.L.items = (int)items;
     s.L.per_xcd = single ? 0 : (int)((items + NUM_XCD - 1) / NUM_XCD);
