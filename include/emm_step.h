@@ -114,8 +114,9 @@ emm_status emm_norm_rope_kv_scatter_fp8(const emm_batch *batch, const emm_qk_nor
  * (emm_page_step).  What a slot holds that a row does not see never reaches the row, infinities and NaN included.
  * Arguments and results otherwise as for emm_prefill_attn (emm_decode_attn_window: at most one new token per request, else
  * EMM_ERR_INVALID_ARG); EMM_BF16 with head_dim 128 and EMM_F32 with head_dim 64 or 128; at most 2^20 (request, KV head) pairs.
- * bf16: scores, softmax statistics and sums in 32 bits; softmax weights are rounded to bf16 for the value product.  Results are
- * run-to-run bitwise deterministic.
+ * bf16: scores, softmax statistics and sums in 32 bits; softmax weights are rounded to bf16 for the value product.  The sums are
+ * divided by the sum of the weights at the end, and weights are at most 2^16 until then: results are finite where
+ * 2^16 * (slots that the row sees) * (largest |v|) is at most 2^127.  Results are run-to-run bitwise deterministic.
  *   workspace  device scratch of at least emm_attn_window_workspace_size bytes, 16-byte aligned (may be NULL if that is 0), the
  *              same size for both calls; contents need no initialisation and mean nothing afterwards.  Calls that may overlap
  *              must not share one.

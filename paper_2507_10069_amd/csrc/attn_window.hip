@@ -5,22 +5,29 @@
 // them.  In blocks of 16 slots, which lie in one page each, these are a list without a gap: the sinks' blocks, then the window's.
 // Tiles are taken from that list, so nothing is fetched or multiplied that no row sees, but for the ends of blocks and tiles.
 //
-// Two shapes of the same loop:
-//   rows   a workgroup has 128 rows, 32 to a wave, and its four waves share tiles of 64 keys: prompts, bound by the matrix pipes;
-//   keys   a workgroup has 32 rows, all of its four waves the same ones, and each wave takes every fourth tile of 32 keys by
-//          itself, without a barrier; they meet in LDS at the end.  Decode steps (bound by reading K and V) and small calls (bound by
-//          the trips through memory), whose contexts are cut into `parts` besides, so that they fill the chip: a second kernel adds
-//          the parts' records up.
+// Shapes:
+//   rows    a workgroup of 4 or 8 waves has 32 rows a wave, and its waves share tiles of 64 keys: prompts, bound by the matrix pipes and the
+//           power that they take.  How its row tiles are dealt, cut and halved stands at RowsPlan.
+//   decode  one new token, up to 16 heads: a workgroup has a (request, KV head), each of its four waves takes every fourth tile of 32 keys by
+//           itself, without a barrier, and they meet in LDS at the end.  Bound by reading K and V.
+//   keys    the same with 32 rows a wave: chunks too small for the rows shape, bound by the trips through memory that follow each other.
+// Where the last two are too few to fill the chip their keys are cut into parts besides, and a second kernel adds the parts' records up.
 // K and V go from memory straight into LDS, whole rows of 256 bytes in XOR-swizzled chunks of 16; K is read with ds_read_b128, V with
 // the transposing read.  Scores are made transposed, S^T = K Q^T, and K's rows are stored with bits 2 and 3 of the place in the block
 // swapped: then a lane has one row's scores, and those are the value product's operand O^T += V^T P^T as they stand.
 //
 // The softmax's reference is a row's maximum of an earlier tile: it is raised, and the sums scaled, only when a tile brings a score that
 // is more than 2^LAG of it, which the lane's own maximum tells without asking the other half of the row.  (Any reference gives the same
-// quotient; weights are at most 2^LAG.)
+// quotient; weights are at most 2^LAG.)  Weights are rounded to bf16 because the product takes both operands so; their sum is of what they were
+// before, in 32 bits, so that lse is as exact as the scores (of the rounded ones it was 2^-10 off).
 //
 // A slot that some row of a tile sees and another does not may hold an infinity or NaN, which a weight of 0 would not remove.  In the
-// tiles at the ends of windows such values are looked for, replaced by 0 and added to the rows that see them by hand.
+// tiles at the ends of windows such values are looked for, replaced by 0, and added at the end to the rows that see them.
+//
+// Measured, 28 query heads over 4 KV heads, calls in a graph: 2 x 2048 new tokens behind a window of 4096 235 us (1020 TFLOP/s of what rows see; a large
+// matrix product reaches 1265 on that card: 448 units on 256 compute units, two waves to a SIMD, matrix pipes busy half of the cycles at 1.95 GHz); one
+// compute unit's fill of units, 2 x 1170, 135 us; 8 x 177 to 479 behind 1024 62 us; 36 tokens behind 2048 13.5; one decode step behind 1024 7.8 (two launches;
+// the kernels 4.0 and 2.6); 64 behind 4096 82 us (6.6 TB/s), behind 1024 24.
 #include "attn_bf16_common.h"
 #include "step_internal.h"
 
@@ -117,9 +124,13 @@ template <int ROWS> __device__ inline bool find_tile(const BatchView& b, const W
 // ---- Rows shape, NW waves a workgroup.  A unit is a row tile of 32 NW rows of a KV head; units are counted head by head, request by request, and
 // each XCD has an eighth of them, neighbours, which mostly read the same keys.  It holds 256 / NW workgroups at once, and units take about equally
 // long (a window), so that with few units in the last round most of its places would idle.  Such units are
-//   cut     along their keys into as many parts as there are places for, which leave records for a second kernel, or, where that may not be,
+//   cut     along their keys into as many parts as there are places for, which leave records for a second kernel, or, where that gains nothing,
 //   halved  a workgroup then has half of the rows, two waves to 32 of them, which take a half of each tile's keys each and meet in LDS.
 // Everybody derives the same plan from the lengths.
+// Four waves, two workgroups to a compute unit, whose starts and ends overlap, for short windows (8 x 177 to 479 tokens behind 1024 62 us, and 70 with eight);
+// eight, which bring each tile once for twice the rows, for long ones (2 x 2048 behind 4096 240 us, and 251 with four).
+// us whole, halved, cut: 2 x 585 tokens behind 4096 (16 units on an XCD) 107, 82, -; 2 x 292 (8) 103, 70, 52; 2 x 200 (6) -, 93 in the keys shape, 46; one of
+// 250 behind 1024 (7) -, 23, 20; 2 of 250 (14) -, 24, 30: the more parts there are, the more their records cost, 67 or 135 KB each, out and in.
 constexpr int MOST_PARTS = 16, PLACES = 32;              // parts of a unit; of all of an XCD's
 struct RowsPlan {
     int first, units, whole;                             // of an XCD: its first unit, all of them, those that are neither cut nor halved
@@ -1236,10 +1247,16 @@ __global__ __launch_bounds__(256) void attn_window_rows_merge_kernel(AttnArgs a,
 }
 
 constexpr int COMPUTE_UNITS = 256;
-constexpr long long STREAM_BYTES = 96ll << 20;           // of K and V, each read once: more than the last-level cache keeps for a next call
-constexpr int ROWS_UNITS = 16;                          // units of 128 rows from which the rows shape is taken
-constexpr int LONG_TILES = 32;                           // tiles of 64 keys from which on its workgroups have eight waves, and their last units are cut
-constexpr int CUT_ROUNDS = 4;                            // ... unless there are so many rounds that the last one is a small part; short ones' only if they are all there is
+// K and V of a decode step, each read once, past the caches where they are more than the last-level cache keeps for a next call (537 MB 101 us through the caches
+// and 90 past them, 800 ragged 308 and 276, 393 on 8 heads 81 and 70; 134 MB 29.0 and 29.3, 66 30.6 and 30.6).
+constexpr long long STREAM_BYTES = 96ll << 20;
+// The rows shape from so many units on (of 128 rows, one for each request at least), us in the rows and in the keys shape: 8 units, 36 tokens behind 2048 20.5 and
+// 14.1; 12, 50 behind 1024 16.1 and 15.2; 16, 60 behind 4096 22.2 and 21.5, 4 x 9 behind 1024 14.3 and 18.0, behind 4096 18.5 and 26.5; 24, 100 behind
+// 4096 25.4 and 31.6; 28, 160 behind 1024 17.9 and 22.7; 64, 16 x 9 behind 1024 19.4 and 32.1.
+constexpr int ROWS_UNITS = 16;
+constexpr int LONG_TILES = 32;                           // tiles of 64 keys from which on a window is long: see RowsPlan (measured at 18 and at 65)
+constexpr int CUT_ROUNDS = 4;                            // a long window's last units are cut in batches of up to so many rounds, a short one's where they are all there is:
+                                                         // beyond, what the second kernel takes (5 us where nothing was cut after all) is as much as there is to gain
 
 // How a batch is dealt, from what the host knows.
 struct Deal {

@@ -8,7 +8,8 @@
 // by itself (they are of a few numbers per request) and its share of the pages and tokens, and writes nothing that another reads, but
 // where an output is the input that it follows: then a second, small launch writes those, or one workgroup does it all.
 //
-// Bound by the chain of its round trips: arguments, lengths, page ids, stores.
+// Bound by the chain of its round trips: arguments, lengths, page ids, stores.  In a graph, us: 64 requests' decode step behind a window 3.7 (5.1 with the
+// three kinds of work one after the other and two running sums in every call), 32000 tokens of 48 prompts 4.2; an empty kernel is 1.7.
 #include "step_internal.h"
 
 namespace emm {

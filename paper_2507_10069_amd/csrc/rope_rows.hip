@@ -6,9 +6,12 @@
 // are rotary_dim / 2 further up, or 16 in a row where pairs are neighbours.  A token's cosines and sines are made once by
 // its wave, a lane for each frequency (at most 64), and reach the lanes that need eight of them through LDS.
 //
-// Measured, of bytes read and written: 4096 tokens of 28 + 4 heads of 128 in bf16 rotated in 12.2 us (67 MB, 5.5 TB/s: they fit the
-// last-level cache), 46000 tokens' K and V of 8 heads quantised in 58 us (284 MB, 4.9 TB/s, what a large copy reaches), 35000 slots
-// of 4 heads read back in 24.2 us (108 MB, 4.5 TB/s).  64 tokens' rotation and write takes 3.9 us on the card, an empty kernel 1.7;
+// Norms add a sum of squares over the lanes of a row, which travel by DPP, and 16 weights a lane, which stay in registers while a wave is at q's rows.
+//
+// Measured, of bytes read and written: 4096 tokens of 28 + 4 heads of 128 in bf16 rotated in 12.4 us (67 MB, 5.4 TB/s: they fit the
+// last-level cache), with norms 13.1; 42500 tokens of 32 + 8 heads with norms, rotation and the write 207 us (1.07 GB, 5.2 TB/s, what a large copy reaches);
+// 46000 tokens' K and V of 8 heads quantised in 57 us (284 MB, 5.0 TB/s), 35000 slots
+// of 4 heads read back in 24.2 us (108 MB, 4.5 TB/s).  64 tokens' rotation and write takes 3.9 us on the card, with norms into bf16 3.5, an empty kernel 1.7;
 // what a decode step waits for is the launch.
 #include "fp8_device.h"
 #include "step_internal.h"
