@@ -516,36 +516,42 @@ def _ref(struct):
     return None if struct is None else ctypes.byref(struct)
 
 
+def _ptrs(*tensors):
+    """Addresses of many tensors at once (0.1 us each, with a call for each 0.2: what a small call waits for is the host)."""
+    return [None if t is None else t.data_ptr() for t in tensors]
+
+
 def _check_rows(batch: emm_batch, norm, rope, slots=None) -> None:
     if rope is not None:
         _check_positions(batch, rope)
     if norm is not None and norm._head_dim is not None and norm._head_dim != batch.head_dim:
         raise ValueError("norm weights of %d channels, heads of %d" % (norm._head_dim, batch.head_dim))
-    if slots is not None:
-        import torch
-        if slots.dtype is not torch.int64 or not slots.is_contiguous() or slots.numel() < batch.total_new_tokens:     # (a dtype's name takes longer than the rest)
-            raise ValueError("slots are a contiguous int64 tensor, one for each of %d tokens" % batch.total_new_tokens)
+    if slots is not None and (slots.element_size() != 8 or slots.is_floating_point() or slots.is_complex() or not slots.is_contiguous()
+                              or slots.numel() < batch.total_new_tokens):
+        raise ValueError("slots are a contiguous int64 tensor, one for each of %d tokens" % batch.total_new_tokens)
 
 
 def emm_norm_rope(batch: emm_batch, norm: Optional[emm_qk_norm], rope: Optional[emm_rope_params], q, k, q_out, k_out, token_stride: int = 0,
                   stream=None) -> None:
     _check_rows(batch, norm, rope)
-    _check(load().emm_norm_rope(ctypes.byref(batch), _ref(norm), _ref(rope), _ptr(q), _ptr(k), token_stride, _ptr(q_out), _ptr(k_out),
-                                _stream(stream)), "emm_norm_rope")
+    q, k, q_out, k_out = _ptrs(q, k, q_out, k_out)
+    _check(load().emm_norm_rope(ctypes.byref(batch), _ref(norm), _ref(rope), q, k, token_stride, q_out, k_out, _stream(stream)), "emm_norm_rope")
 
 
 def emm_norm_rope_kv_scatter(batch: emm_batch, norm: Optional[emm_qk_norm], rope: Optional[emm_rope_params], q, k_new, v_new, q_out, k_cache, v_cache,
                              token_stride: int = 0, slots=None, stream=None) -> None:
     _check_rows(batch, norm, rope, slots)
-    _check(load().emm_norm_rope_kv_scatter(ctypes.byref(batch), _ref(norm), _ref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), token_stride, _ptr(slots),
-                                           _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream(stream)), "emm_norm_rope_kv_scatter")
+    q, k_new, v_new, slots, q_out, k_cache, v_cache = _ptrs(q, k_new, v_new, slots, q_out, k_cache, v_cache)
+    _check(load().emm_norm_rope_kv_scatter(ctypes.byref(batch), _ref(norm), _ref(rope), q, k_new, v_new, token_stride, slots, q_out, k_cache, v_cache,
+                                           _stream(stream)), "emm_norm_rope_kv_scatter")
 
 
 def emm_norm_rope_kv_scatter_fp8(batch: emm_batch, norm: Optional[emm_qk_norm], rope: Optional[emm_rope_params], q, k_new, v_new, q_out,
                                  cache: emm_fp8_cache, token_stride: int = 0, slots=None, stream=None) -> None:
     _check_rows(batch, norm, rope, slots)
-    _check(load().emm_norm_rope_kv_scatter_fp8(ctypes.byref(batch), _ref(norm), _ref(rope), _ptr(q), _ptr(k_new), _ptr(v_new), token_stride, _ptr(slots),
-                                               _ptr(q_out), ctypes.byref(cache), _stream(stream)), "emm_norm_rope_kv_scatter_fp8")
+    q, k_new, v_new, slots, q_out = _ptrs(q, k_new, v_new, slots, q_out)
+    _check(load().emm_norm_rope_kv_scatter_fp8(ctypes.byref(batch), _ref(norm), _ref(rope), q, k_new, v_new, token_stride, slots, q_out,
+                                               ctypes.byref(cache), _stream(stream)), "emm_norm_rope_kv_scatter_fp8")
 
 
 def make_page_step(*, num_reqs, page_size, num_pages, max_pages_per_req, max_tokens, window=0, sinks=0, page_table, free_pages, lens, add_lens, held_from,
@@ -579,8 +585,8 @@ def emm_attn_window_workspace_size(batch: emm_batch, window: int, sinks: int) ->
 
 
 def _attn_window(name: str, batch, window, sinks, q, k_cache, v_cache, out, lse, workspace, stream) -> None:
-    _check(getattr(load(), name)(ctypes.byref(batch), window, sinks, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(lse), _ptr(workspace),
-                                 _bytes(workspace), _stream(stream)), name)
+    _check(getattr(load(), name)(ctypes.byref(batch), window, sinks, *_ptrs(q, k_cache, v_cache, out, lse, workspace),
+                                 0 if workspace is None else workspace.nbytes, _stream(stream)), name)
 
 
 def emm_prefill_attn_window(batch: emm_batch, window: int, sinks: int, q, k_cache, v_cache, out, lse=None, workspace=None, stream=None) -> None:
