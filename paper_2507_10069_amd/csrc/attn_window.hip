@@ -19,15 +19,15 @@
 // The softmax's reference is a row's maximum of an earlier tile: it is raised, and the sums scaled, only when a tile brings a score that
 // is more than 2^LAG of it, which the lane's own maximum tells without asking the other half of the row.  (Any reference gives the same
 // quotient; weights are at most 2^LAG.)  Weights are rounded to bf16 because the product takes both operands so; their sum is of what they were
-// before, in 32 bits, so that lse is as exact as the scores (of the rounded ones it was 2^-10 off).
+// before, in 32 bits, so that lse is as exact as the scores (of the rounded ones it could be off by their half step, 2^-8).
 //
 // A slot that some row of a tile sees and another does not may hold an infinity or NaN, which a weight of 0 would not remove.  In the
 // tiles at the ends of windows such values are looked for, replaced by 0, and added at the end to the rows that see them.
 //
 // Measured, 28 query heads over 4 KV heads, calls in a graph: 2 x 2048 new tokens behind a window of 4096 235 us (1020 TFLOP/s of what rows see; a large
 // matrix product reaches 1265 on that card: 448 units on 256 compute units, two waves to a SIMD, matrix pipes busy half of the cycles at 1.95 GHz); one
-// compute unit's fill of units, 2 x 1170, 135 us; 8 x 177 to 479 behind 1024 62 us; 36 tokens behind 2048 13.5; one decode step behind 1024 7.8 (two launches;
-// the kernels 4.0 and 2.6); 64 behind 4096 82 us (6.6 TB/s), behind 1024 24.
+// compute unit's fill of units, 2 x 1170, 135 us; 8 x 177 to 479 behind 1024 62 us; 36 tokens behind 2048 13.5; one decode step behind 1024 7.7 (two launches;
+// the kernels 4.4 and 3.0 traced); 64 behind 4096 82 us (6.6 TB/s), behind 1024 24.
 #include "attn_bf16_common.h"
 #include "step_internal.h"
 
