@@ -257,11 +257,10 @@ template <int SHAPE, int NW> struct Sizes {
 };
 
 // The rows of tile t by the workgroup, or, of `parts`, part `part` of their keys, whose record is number `place` (of those that the keys shape leaves,
-// or of the XCD's).  bad_s: rows shape, keys of a tile's blocks whose V holds
-// an infinity or NaN.
+// or of the XCD's).  bad_s: rows shapes, which waves have taken an infinity or NaN of V out.
 template <int SHAPE, int NW>
 __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView& w, const WindowLayout& L, const Tile& t, int kvh, int parts, int part, int place,
-                                            unsigned char* smem, int (*bad_s)[NW])
+                                            unsigned char* smem, int* bad_s)
 {
     constexpr bool KEYS = SHAPE == Shape::KEYS, HALVED = SHAPE == Shape::HALVED;
     constexpr int TB = Sizes<SHAPE, NW>::TILE / BLK, TILE_BYTES = Sizes<SHAPE, NW>::TILE_BYTES, RING = Sizes<SHAPE, NW>::RING;
@@ -705,11 +704,11 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
     // what was not finite and taken out, to the rows that see it
     bool any = __builtin_amdgcn_ballot_w64(odd_rows != 0) != 0;
     if constexpr (!KEYS) {
-        if (lane == 0) bad_s[0][wave] = any ? 1 : 0;
+        if (lane == 0) bad_s[wave] = any ? 1 : 0;
         __syncthreads();                                     // (and the rings are free)
         any = false;
 #pragma unroll
-        for (int k = 0; k < NW; ++k) any = any || __builtin_amdgcn_readfirstlane(bad_s[0][k]) != 0;
+        for (int k = 0; k < NW; ++k) any = any || __builtin_amdgcn_readfirstlane(bad_s[k]) != 0;
     }
     if (any) {
         int* list = (int*)my_ring;                           // [waves that brought blocks][64]
@@ -1102,7 +1101,7 @@ template <int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_window_rows_kernel(AttnArgs a, WindowView w, WindowLayout L)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char smem[Sizes<ROWS, NW>::LDS];
-    __shared__ int bad_s[1][NW];
+    __shared__ int bad_s[NW];
     const BatchView& b = a.b;
     Lines<NW> lines = {b};
     const int tiles = lines.total(L), i = blockIdx.x / NUM_XCD;
@@ -1258,6 +1257,10 @@ constexpr int LONG_TILES = 32;                           // tiles of 64 keys fro
 constexpr int CUT_ROUNDS = 4;                            // a long window's last units are cut in batches of up to so many rounds, a short one's where they are all there is:
                                                          // beyond, what the second kernel takes (5 us where nothing was cut after all) is as much as there is to gain
 
+// A request that may have no token has room for a row tile all the same: so many items at most are cut (no batch of 15 requests or fewer has more), or
+// a few tokens among thousands of requests would want a workspace of gigabytes.
+constexpr long long MOST_ITEMS = 4096;
+
 // How a batch is dealt, from what the host knows.
 struct Deal {
     int rows_waves;                                      // of a workgroup of the rows shape, 0: the others
@@ -1305,7 +1308,7 @@ Deal deal_of(const BatchView& b, const WindowView& w)
     s.stream = s.decode && slots * b.num_kv_heads * span * (4 * D) > STREAM_BYTES;
     // as many parts as fill the chip, each of a tile for every wave at least
     const long long tiles = (span + 31) / 32, units = (single ? slots : std::max((rows + WAVE_ROWS - 1) / WAVE_ROWS, 1ll)) * b.num_kv_heads;
-    s.L.parts = (int)std::max(1ll, std::min(COMPUTE_UNITS / units, (tiles + MIN_TILES - 1) / MIN_TILES));
+    s.L.parts = (int)std::max(1ll, std::min({COMPUTE_UNITS / units, (tiles + MIN_TILES - 1) / MIN_TILES, MOST_ITEMS / (slots * b.num_kv_heads)}));
     const long long items = slots * b.num_kv_heads * s.L.parts;
     s.L.items = (int)items;
     s.L.per_xcd = single ? 0 : (int)((items + NUM_XCD - 1) / NUM_XCD);

@@ -205,6 +205,14 @@ def test_hundreds_of_requests_with_some_tokens():
     Case(rng.integers(0, 200, 700).tolist(), new, 64, 3, heads=8, kv_heads=2, seed=8, extra_rows=9).run_and_check()
 
 
+@pytest.mark.parametrize("idle", [14, 600, 5000])
+def test_a_few_tokens_among_many_requests(idle):
+    new = [0] * (idle // 2) + [9] + [0] * (idle - idle // 2) + [3]
+    prefix = [40] * (idle // 2) + [3000] + [0] * (idle - idle // 2) + [700]
+    case = Case(prefix, new, 2048, 4, kv_heads=1).to_device()
+    case.check(*case.run())
+
+
 def test_scores_that_differ_by_far():
     """Scores of hundreds: the reference has to be raised on the way, and what came before vanishes."""
     for seed in range(3):

@@ -160,6 +160,15 @@ def test_windows_and_workspaces():
             assert B.emm_attn_window_workspace_size(_batch(num_reqs=4, max_pages_per_req=2 ** 26), window, sinks) < 64 << 20
 
 
+def test_requests_without_tokens_take_no_parts_of_the_workspace():
+    """Few tokens among many requests: each request's room is that of one part, not of as many as would fill the chip for those with tokens.
+    Records are of 32 rows of 132 floats; 4096 of them, or one for each row tile there may be where that is more."""
+    for reqs in (15, 64, 4096, 200000, 2 ** 20):
+        b = _batch(num_reqs=reqs, num_q_heads=28, num_kv_heads=1, max_pages_per_req=600, total_new_tokens=15, max_new_len=15)
+        tiles = 15 * 28 // 32 + reqs
+        assert B.emm_attn_window_workspace_size(b, 4096, 4) <= max(4096, tiles) * 32 * 132 * 4, reqs
+
+
 def test_empty_batches_are_no_ops():
     lib, n, r = B.load(), ctypes.byref(_norm()), ctypes.byref(_rope())
     for b in (_batch(arrays=False, num_reqs=0, total_new_tokens=0, max_new_len=0), _batch(arrays=False, total_new_tokens=0, max_new_len=0)):
