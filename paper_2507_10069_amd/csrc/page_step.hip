@@ -240,10 +240,13 @@ __global__ __launch_bounds__(NT) void page_step_kernel(PageStepArgs a)
 template <int NT, int ITEMS>
 hipError_t launch(const PageStepArgs& a, bool in_place, hipStream_t stream)
 {
-    constexpr int ALONE = 4;                                 // tokens per thread up to which one workgroup does it all
+    // Where outputs are inputs one workgroup does it all up to so many tokens per thread, as the second launch costs 1.7 us and more; us of one workgroup and of
+    // many with the second launch: 8 requests' 512 tokens 3.4 and 5.0, 1024 4.6 and 5.1, 2048 6.9 and 5.1.
+    // Apart, many are never slower: 256 tokens 3.3 and 3.4, 1024 5.0 and 3.4, 8192 21.4 and 3.6.
+    constexpr int ALONE = 4;
     constexpr int MOST_GROUPS = 256;
     const int groups = (int)min(((long long)a.max_tokens + NT - 1) / NT, (long long)MOST_GROUPS);
-    if (groups <= ALONE) {
+    if (groups <= (in_place ? ALONE : 1)) {
         hipLaunchKernelGGL((page_step_kernel<NT, ITEMS, ALL>), dim3(1), dim3(NT), 0, stream, a);
     } else if (!in_place) {
         hipLaunchKernelGGL((page_step_kernel<NT, ITEMS, ALL>), dim3(groups), dim3(NT), 0, stream, a);
@@ -258,8 +261,11 @@ hipError_t launch(const PageStepArgs& a, bool in_place, hipStream_t stream)
 
 hipError_t launch_page_step(const PageStepArgs& a, bool in_place, hipStream_t stream)
 {
+    // Fewer waves meet sooner, and more requests a thread take longer; us of decode steps, outputs apart from inputs: 64 requests with 256 threads 3.2, with 1024
+    // 5.0; 300 with 256 x 4 requests 5.0, 512 x 2 4.7, 1024 x 1 5.5; 1000 5.9, 5.5, 7.1 (in place 11.4, 7.1, 6.7); 2000 with 1024 x 4 8.9, 512 x 8 11.3; 512
+    // requests' 16384 tokens 5.2, 4.9, 6.6.
     if (a.num_reqs <= 256) return launch<256, 1>(a, in_place, stream);
-    if (a.num_reqs <= 1024) return launch<1024, 1>(a, in_place, stream);
+    if (a.num_reqs <= 1024) return launch<512, 2>(a, in_place, stream);
     return launch<1024, MOST_STEP_REQS / 1024>(a, in_place, stream);
 }
 
