@@ -75,7 +75,9 @@ struct Tile {
 
 // How a row tile's keys are cut where the host has given it `parts` workgroups, from what a window may hold: each takes `share` of its tiles, so many at least
 // as are worth a workgroup, so that a context shorter than its window has fewer parts, and the others nothing to do and no record.
-constexpr int MIN_TILES = 4;                             // of a part: of the decode shape one of 32 keys for each wave, of the rows shape of 64
+// MIN_TILES: of a part: of the decode shape one of 32 keys for each wave, of the rows shape of 64.  us with 2, 4, 8, 16: one decode step behind 1024 8.7, 8.0, 8.8,
+// 10.4, behind 4096 10.0, 9.8, 9.8, 10.6; 250 tokens behind 1024 20.1, 20.0, 22.9, 21.9; 2 x 200 behind 4096 43.5, 43.2, 43.3, 45.9.
+constexpr int MIN_TILES = 4;
 constexpr int MIN_TILES_KEYS = 1;                        // (20 tokens of 320 11.7 us, in parts of four 13.3)
 __device__ inline int share_of(int tiles, int parts, const Divisor& by_parts, int least) { return max(by_parts.quotient(tiles + parts - 1), least); }
 __device__ inline int share_of(int tiles, int parts) { return max((tiles + parts - 1) / parts, MIN_TILES); }

@@ -240,7 +240,7 @@ __global__ __launch_bounds__(NT) void page_step_kernel(PageStepArgs a)
 template <int NT, int ITEMS>
 hipError_t launch(const PageStepArgs& a, bool in_place, hipStream_t stream)
 {
-    // Where outputs are inputs one workgroup does it all up to so many tokens per thread, as the second launch costs 1.7 us and more; us of one workgroup and of
+    // Where outputs are inputs one workgroup does it all up to so many tokens per thread, as the second launch costs 1.2 to 2.5 us; us of one workgroup and of
     // many with the second launch: 8 requests' 512 tokens 3.4 and 5.0, 1024 4.6 and 5.1, 2048 6.9 and 5.1.
     // Apart, many are never slower: 256 tokens 3.3 and 3.4, 1024 5.0 and 3.4, 8192 21.4 and 3.6.
     constexpr int ALONE = 4;
