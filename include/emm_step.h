@@ -112,6 +112,7 @@ emm_status emm_norm_rope_kv_scatter_fp8(const emm_batch *batch, const emm_qk_nor
  * more is the full attention.
  * Entries of the page table whose page no new token sees are not looked at, so those pages may have been given back
  * (emm_page_step).  What a slot holds that a row does not see never reaches the row, infinities and NaN included.
+ * One of them in V at a slot that the row sees makes that channel of the row infinite or NaN, whatever the slot's weight.
  * Arguments and results otherwise as for emm_prefill_attn (emm_decode_attn_window: at most one new token per request, else
  * EMM_ERR_INVALID_ARG); EMM_BF16 with head_dim 128 and EMM_F32 with head_dim 64 or 128; at most 2^20 (request, KV head) pairs.
  * bf16: scores, softmax statistics and sums in 32 bits; softmax weights are rounded to bf16 for the value product.  The sums are

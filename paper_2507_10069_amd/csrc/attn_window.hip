@@ -1133,6 +1133,7 @@ __device__ inline float wave_sum(float x)
 }
 
 // Adds the records of a row tile's parts up: a wave for a row, two channels a lane, AT_ONCE parts' rows on their way at a time.
+// A record counts if there is that part, whatever its weight: 0 times a sum that an infinity or NaN is in is NaN, as in the waves' own sums.
 constexpr int AT_ONCE = 16;
 template <int ROWS>                                      // of a record
 __global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs a, WindowView w, WindowLayout L, int row_groups)
@@ -1177,8 +1178,9 @@ __global__ __launch_bounds__(64 * WAVES) void attn_window_merge_kernel(AttnArgs 
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
                 const float w_u = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(weight), (k + u - k0) & 63));
-                x = w_u != 0.f ? fmaf(w_u, v[u][0], x) : x;
-                y = w_u != 0.f ? fmaf(w_u, v[u][1], y) : y;
+                const bool there = (k + u) * share < tiles;
+                x = there ? fmaf(w_u, v[u][0], x) : x;
+                y = there ? fmaf(w_u, v[u][1], y) : y;
             }
         }
     }
@@ -1234,7 +1236,7 @@ __global__ __launch_bounds__(256) void attn_window_rows_merge_kernel(AttnArgs a,
             if (k < parts) {
                 const float weight = ml[k][0] != -INFINITY ? __builtin_amdgcn_exp2f(ml[k][0] - top) : 0.f;
                 total += weight * ml[k][1];
-                if (weight != 0.f) sum += weight * v[k];
+                sum += weight * v[k];
             }
         const float inv = total != 0.f ? 1.f / total : 0.f;
         const int token = L.by_G.quotient(t.row0 + row);

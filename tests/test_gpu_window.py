@@ -241,3 +241,52 @@ def test_batches_without_tokens():
     case = Case([5, 6], [0, 0], 4, 0, extra_rows=4).to_device()
     out, lse = case.run()
     assert (out == 7).all() and (lse == 7).all()
+
+
+# prefix, new, window, heads, KV heads, dtype, are keys cut over workgroups, whose records a second kernel adds up?
+CUT_AND_UNCUT = [([5000], [1], 4096, 28, 4, "bf16", True),                       # decode shape
+                 ([500] * 10, [1] * 10, 400, 28, 28, "bf16", False),
+                 ([200, 60], [1, 1], 50, 28, 4, "bf16", False),
+                 ([5000], [33], 2048, 28, 4, "bf16", True),                      # keys shape
+                 ([300], [9], 60, 28, 4, "bf16", False),
+                 ([2000], [250], 1024, 28, 4, "bf16", True),                     # rows shape, four waves
+                 ([1000] * 5, [200] * 5, 900, 28, 4, "bf16", False),             # (in halves)
+                 ([1000] * 8, [200] * 8, 900, 28, 4, "bf16", False),             # (whole)
+                 ([3000], [300], 2100, 28, 4, "bf16", True),                     # eight waves
+                 ([900, 70], [1, 1], 60, 8, 2, "f32", False),
+                 ([2000], [33], 1000, 8, 2, "f32", False)]
+
+
+def _of_odd_values(prefix, new, window, heads, kv_heads, dtype, cut, far):
+    """far: the scores of the older 5/8 of a window are 522 powers of two below the others, so that its parts have a weight of 0."""
+    case = Case(prefix, new, window, 20, heads=heads, kv_heads=kv_heads, dtype=dtype, seed=len(prefix) + window)
+    case.q[:, :, 0] = 8
+    places = []
+    for c, m, r in zip(prefix, new, range(len(prefix))):
+        for s in range(c - window + 1, c + m):
+            page, place = case.slot(r, s)
+            case.k[page, :, place, 0] = -512 if far and s < c - 3 * window // 8 else 0
+        # slots that all of the request's rows see, and some
+        assert m == 1 or m < window // 4 + window // 8
+        places.append((case.slot(r, c - window + 3 * window // 8), case.slot(r, c - window + 1 + m // 2)))
+    return case, places
+
+
+@pytest.mark.parametrize("far", [False, True])
+@pytest.mark.parametrize("prefix,new,window,heads,kv_heads,dtype,cut", CUT_AND_UNCUT)
+def test_infinities_and_nan_reach_the_rows_that_see_them_however_a_call_is_cut(prefix, new, window, heads, kv_heads, dtype, cut, far):
+    """In V.  A channel is then infinite or NaN (which of them is left open: a weight that is 0 in 32 bits, times an infinity, is NaN)."""
+    case, places = _of_odd_values(prefix, new, window, heads, kv_heads, dtype, cut, far)
+    odd = torch.tensor([float("nan"), float("inf"), -float("inf")]).to(case.v.dtype)
+    for (page, place), (page2, place2) in places:
+        case.v[page, 0, place, [3, 40, 77]] = odd
+        case.v[page2, kv_heads - 1, place2, [9, 50, 127]] = odd
+    case.to_device()
+    assert (case.workspace is not None) == cut
+    out, lse = case.run(decode=max(new) == 1)
+    want, _, _ = M.window_attention(case.table, case.prefix, case.new, case.cu, _f64(case.q), _f64(case.k), _f64(case.v), case.page, window, 20, case.scale, case.rows)
+    want = torch.from_numpy(want).to(DEV)
+    odd = ~want.isfinite()
+    assert odd.any(dim=2).any(dim=1).all() and not odd.all(dim=2).any()
+    assert torch.equal(odd, ~out.isfinite())
+    case.check(torch.where(odd, want, out.double()), lse)                    # the others' values
