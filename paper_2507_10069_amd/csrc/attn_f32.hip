@@ -282,11 +282,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnArgs a, int G,
             l_all += wgt * l_s[w][my];
             acc += wgt * *(const f32x4*)&o_s[w][my][c4];
         }
-        const float inv = (l_all > 0.f) ? 1.f / l_all : 0.f;                // no keys (cross, empty cache): zero row
+        const bool any = WINDOW ? l_all != 0.f : l_all > 0.f;               // (with a window a sum of NaN makes lse NaN too, as in bf16)
+        const float inv = any ? 1.f / l_all : 0.f;                          // no keys (cross, empty cache): zero row
         const int o_row = row0 + my, o_tok = by_G.quotient(o_row);
         const long long at = (first_row + o_tok) * b.num_q_heads + kvh * G + (o_row - o_tok * G);
         *(f32x4*)((float*)a.out + at * D + ch0 + c4) = acc * inv;
-        if (a.lse != nullptr && ch0 + c4 == 0) a.lse[at] = (l_all > 0.f) ? m_all + logf(l_all) : -INFINITY;
+        if (a.lse != nullptr && ch0 + c4 == 0) a.lse[at] = any ? m_all + logf(l_all) : -INFINITY;
     }
 }
 

@@ -290,3 +290,19 @@ def test_infinities_and_nan_reach_the_rows_that_see_them_however_a_call_is_cut(p
     assert odd.any(dim=2).any(dim=1).all() and not odd.all(dim=2).any()
     assert torch.equal(odd, ~out.isfinite())
     case.check(torch.where(odd, want, out.double()), lse)                    # the others' values
+
+
+@pytest.mark.parametrize("far", [False, True])
+@pytest.mark.parametrize("prefix,new,window,heads,kv_heads,dtype,cut", CUT_AND_UNCUT)
+def test_nan_in_k_reaches_the_rows_that_see_it_however_a_call_is_cut(prefix, new, window, heads, kv_heads, dtype, cut, far):
+    """Their scores are NaN: so are the rows, and lse."""
+    case, places = _of_odd_values(prefix, new, window, heads, kv_heads, dtype, cut, far)
+    for (page, place), (page2, place2) in places:
+        case.k[page, 0, place, 5] = float("nan")
+        case.k[page2, 0, place2, 6] = float("nan")
+    case.to_device()
+    out, lse = case.run(decode=max(new) == 1)
+    want, want_lse, _ = M.window_attention(case.table, case.prefix, case.new, case.cu, _f64(case.q), _f64(case.k), _f64(case.v), case.page, window, 20, case.scale, case.rows)
+    assert np.isnan(want).any() and not np.isnan(want).all()
+    assert np.array_equal(np.isnan(want_lse), np.isnan(_f64(lse)))
+    case.check(out, lse)
