@@ -526,8 +526,7 @@ def _check_rows(batch: emm_batch, norm, rope, slots=None) -> None:
         _check_positions(batch, rope)
     if norm is not None and norm._head_dim is not None and norm._head_dim != batch.head_dim:
         raise ValueError("norm weights of %d channels, heads of %d" % (norm._head_dim, batch.head_dim))
-    if slots is not None and (slots.element_size() != 8 or slots.is_floating_point() or slots.is_complex() or not slots.is_contiguous()
-                              or slots.numel() < batch.total_new_tokens):
+    if slots is not None and (str(slots.dtype) != "torch.int64" or not slots.is_contiguous() or slots.numel() < batch.total_new_tokens):
         raise ValueError("slots are a contiguous int64 tensor, one for each of %d tokens" % batch.total_new_tokens)
 
 

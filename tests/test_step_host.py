@@ -264,3 +264,15 @@ def test_model_of_the_step_keeps_every_page_once():
         table, free, count, lens, held = np.array(w["page_table"]), np.array(w["free_pages"]), w["free_count_out"][0], w["lens_out"], w["held_out"]
         own = [table[r, e] for r in range(n) for e in list(range(min(1, -(-lens[r] // page)))) + list(range(max(1, held[r]), -(-lens[r] // page)))]
         assert sorted(own + list(free[:count])) == list(range(pages)), step
+
+
+def test_slots_are_signed_64_bit_numbers():
+    import torch
+    if not hasattr(torch, "uint64"):                         # pragma: no cover
+        pytest.skip("no unsigned 64-bit tensors")
+    norm = B.make_qk_norm(torch.ones(128), torch.ones(128), eps=1e-6)
+    slots = torch.zeros(20, dtype=torch.uint64)
+    with pytest.raises(ValueError):
+        B.emm_norm_rope_kv_scatter(_batch(), norm, None, None, None, None, None, None, None, slots=slots)
+    with pytest.raises(ValueError):
+        B.emm_norm_rope_kv_scatter_fp8(_batch(), norm, None, None, None, None, None, B.emm_fp8_cache(), slots=slots)
