@@ -97,8 +97,8 @@ __device__ inline float row_sum(float x)
     return x;
 }
 
-// 1 / sqrt(mean(x^2) + eps) of a row, of which this lane holds 16 channels.  Squares of |x| from 1.8e19 on pass the range of 32 bits:
-// such a row is taken again in units of 2^70, so that the squares of all finite values add up to less than 2^124.
+// 1 / sqrt(mean(x^2) + eps) of a row, of which this lane holds 16 channels.  Squares of |x| from 1.8e19 on pass the range of 32 bits, or their mean
+// with an eps near its end: such a row is taken again in units of 2^70, so that the squares of all finite values add up to less than 2^124.
 template <int LANES>
 __device__ inline float row_norm(const float (&x)[8], const float (&y)[8], float eps)
 {
@@ -112,9 +112,9 @@ __device__ inline float row_norm(const float (&x)[8], const float (&y)[8], float
         }
         return row_sum<LANES>(a + c);
     };
-    const float sum = squares(1.0f);
-    float norm = __builtin_amdgcn_rsqf(fmaf(sum, MEAN, eps));
-    if (!(sum < __builtin_inff())) {
+    const float mean = fmaf(squares(1.0f), MEAN, eps);
+    float norm = __builtin_amdgcn_rsqf(mean);
+    if (!(mean < __builtin_inff())) {
         constexpr float UNIT = 0x1p-70f;
         norm = __builtin_amdgcn_rsqf(fmaf(squares(UNIT), MEAN, eps * UNIT * UNIT)) * UNIT;
     }

@@ -344,6 +344,19 @@ def test_rows_of_any_magnitude(magnitude, eps, dtype):
     rows.near(_f64(k_out), rows.exact(rows.k, 1))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("magnitude,eps", [(1e18, 3.4e38), (3e18, 3.38e38), (1.0, 3.4e38), (1e30, 3.4e38)])
+def test_eps_near_the_end_of_the_range(magnitude, eps, d, dtype):
+    """The mean of squares and eps are each below 2^128, their sum is not."""
+    rows = Rows([3], [9], dtype=dtype, d=d, magnitude=magnitude, seed=6)
+    rows.descriptors(True, 0, "half", 0, eps)
+    q_out, k_out = torch.empty_like(rows.q), torch.empty_like(rows.k)
+    B.emm_norm_rope(rows.batch, rows.norm, None, rows.q, rows.k, q_out, k_out)
+    rows.near(_f64(q_out), rows.exact(rows.q, 0))
+    rows.near(_f64(k_out), rows.exact(rows.k, 1))
+
+
 def test_a_row_with_nan_leaves_the_others():
     rows = Rows([3], [9])
     rows.descriptors(True, 128, "half", 0, 1e-6)
