@@ -24,10 +24,11 @@
 // A slot that some row of a tile sees and another does not may hold an infinity or NaN, which a weight of 0 would not remove.  In the
 // tiles at the ends of windows such values are looked for, replaced by 0, and added at the end to the rows that see them.
 //
-// Measured, 28 query heads over 4 KV heads, calls in a graph: 2 x 2048 new tokens behind a window of 4096 235 us (1020 TFLOP/s of what rows see; a large
-// matrix product reaches 1265 on that card: 448 units on 256 compute units, two waves to a SIMD, matrix pipes busy half of the cycles at 1.95 GHz); one
-// compute unit's fill of units, 2 x 1170, 135 us; 8 x 177 to 479 behind 1024 62 us; 36 tokens behind 2048 13.5; one decode step behind 1024 7.7 (two launches;
-// the kernels 4.4 and 3.0 traced); 64 behind 4096 82 us (6.6 TB/s), behind 1024 24.
+// Measured, 28 query heads over 4 KV heads, calls in a graph: 2 x 2048 new tokens behind a window of 4096 232 to 244 us by card (990 to 1040 TFLOP/s of what rows
+// see, where matrix products of 8192 and 16384 reach 1265 and 1375: 448 units on 256 compute units, two waves to a SIMD, matrix pipes busy half of the cycles at 1.95 GHz;
+// from rest the clock dips, and calls in a row take 250, then up to 312, and settle after about a hundred); one compute unit's fill of units, 2 x 1170, 135 us;
+// 8 x 177 to 479 behind 1024 62 to 66 us; 36 tokens behind 2048 13.4; one decode step behind 1024 7.7 (two launches; the kernels 4.4 and 3.1 traced); 64 behind 4096
+// 83 us (6.5 TB/s), behind 1024 24.
 #include "attn_bf16_common.h"
 #include "step_internal.h"
 
@@ -131,8 +132,12 @@ template <int ROWS> __device__ inline bool find_tile(const BatchView& b, const W
 // Everybody derives the same plan from the lengths.
 // Four waves, two workgroups to a compute unit, whose starts and ends overlap, for short windows (8 x 177 to 479 tokens behind 1024 62 us, and 70 with eight);
 // eight, which bring each tile once for twice the rows, for long ones (2 x 2048 behind 4096 240 us, and 251 with four).
-// us whole, halved, cut: 2 x 585 tokens behind 4096 (16 units on an XCD) 107, 82, -; 2 x 292 (8) 103, 70, 52; 2 x 200 (6) -, 93 in the keys shape, 46; one of
-// 250 behind 1024 (7) -, 23, 20; 2 of 250 (14) -, 24, 30: the more parts there are, the more their records cost, 67 or 135 KB each, out and in.
+// us whole, halved, cut, of units that are left over on an XCD (the more parts there are, the more their records cost, 67 or 135 KB each, out and in):
+//   eight waves, behind 4096: 3 units 92, 62, 31; 8 95, 67, 51; 10 (3 parts) 96, 70, 60; 13 (2) 97, 75, 76; 16 (2) 100, 84, 83; behind 32 others: 5 219, 199, 170; 13
+//     224, 207, 204.  So they are cut from two parts on.
+//   four waves, behind 1024: 5 units 25, 22, 18.6; 8 (4 parts) 25, 22, 20.5; 10 (3) 24.8, 22.6, 22.8; 13 (2) 25, 23, 26; 16 (2) 25.5, 23.7, 26.9; behind 64 others: 13 65, 62.5,
+//     64.5; behind 1900: 7 37, 33, 23; 10 38, 33.2, 27.6; 13 39, 34, 33.  So from four parts on (three are worth it behind long windows alone).
+//   24 and 32 units of four waves, with no others, would be quicker whole, 26.7 and 28.5, than halved, 30.0 and 32.6; behind others it was not timed.
 constexpr int MOST_PARTS = 16, PLACES = 32;              // parts of a unit; of all of an XCD's
 struct RowsPlan {
     int first, units, whole;                             // of an XCD: its first unit, all of them, those that are neither cut nor halved
@@ -147,7 +152,7 @@ template <int NW> __device__ inline RowsPlan rows_plan(const WindowLayout& L, in
     const int full = p.units / SLOTS * SLOTS, rem = p.units - full;
     p.whole = rem <= SLOTS / 2 ? full : p.units;
     p.parts = rem > 0 && rem <= SLOTS / 2 ? min(PLACES / rem, L.most_parts) : 0;
-    if (p.parts < (NW == 8 ? 2 : 4)) p.parts = 0;        // fewer are no quicker than halves, which leave no records
+    if (p.parts < (NW == 8 ? 2 : 4)) p.parts = 0;        // fewer are hardly ever quicker than halves, which leave no records
     return p;
 }
 // a part's record: per thread 64 sums, in groups of four, then m, l
@@ -401,8 +406,11 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& a, const WindowView&
 
     const float c_log2 = b.softmax_scale * LOG2E;
     float m = -INFINITY, l = 0.f;                            // reference (times log2 e); sum of this lane's weights
-    // Lane n: which rows of V that this wave brought of the n-th tile looked at held what is not finite, 16 bits a block.  (Tiles looked at hold a slot that some
-    // rows see and others do not: at most 31 + 2 blocks' at either end of a window, and one at the sinks' end.)
+    // Lane n: which rows of V that this wave brought of the n-th tile looked at held what is not finite, 16 bits a block.  Tiles looked at hold a slot that some
+    // rows see and others do not.  A tile's rows are of at most as many tokens, so that such slots lie in ROWS / 16 + 1 blocks at either end of a window, and in one
+    // at the sinks' end, and n blocks in a row touch (n + 2 TB - 2) / TB tiles at most: 12 of eight waves (11 are reached), 8 of four, 6 of the keys shape.
+    constexpr int MOST_LOOKED = 2 * (((KEYS ? 1 : NW) * WAVE_ROWS / BLK + 2 + 2 * TB - 2) / TB);
+    static_assert(MOST_LOOKED <= 64, "a lane for each tile that is looked at");
     int odd_rows = 0, looked = 0;
     f32x16 o[4];
 #pragma unroll
@@ -1257,7 +1265,10 @@ constexpr long long STREAM_BYTES = 96ll << 20;
 // 14.1; 12, 50 behind 1024 16.1 and 15.2; 16, 60 behind 4096 22.2 and 21.5, 4 x 9 behind 1024 14.3 and 18.0, behind 4096 18.5 and 26.5; 24, 100 behind
 // 4096 25.4 and 31.6; 28, 160 behind 1024 17.9 and 22.7; 64, 16 x 9 behind 1024 19.4 and 32.1.
 constexpr int ROWS_UNITS = 16;
-constexpr int LONG_TILES = 32;                           // tiles of 64 keys from which on a window is long: see RowsPlan (measured at 18 and at 65)
+// Tiles of 64 keys from which on a window is long: see RowsPlan.  us with four and with eight waves, each with its way to cut: 8 x 400 tokens behind 1024 (17 tiles) 78
+// and 86, 1500 (24) 104 and 102, 2048 (33) 126 and 122, 4096 (65) 218 and 208; 2 x 2048 82 and 83, 112 and 108, 139 and 135, 255 and 245; 2 x 585 behind 1500 42 and
+// 47, 2048 51 and 53, 4096 90 and 83; one of 250 21.8 and 24.8, 24.1 and 25.6, 33.7 and 33.3.
+constexpr int LONG_TILES = 32;
 constexpr int CUT_ROUNDS = 4;                            // a long window's last units are cut in batches of up to so many rounds, a short one's where they are all there is:
                                                          // beyond, what the second kernel takes (5 us where nothing was cut after all) is as much as there is to gain
 

@@ -9,7 +9,7 @@
 // where an output is the input that it follows: then a second, small launch writes those, or one workgroup does it all.
 //
 // Bound by the chain of its round trips: arguments, lengths, page ids, stores.  In a graph, us: 64 requests' decode step behind a window 3.7 (5.1 with the
-// three kinds of work one after the other and two running sums in every call), 32000 tokens of 48 prompts 4.2; an empty kernel is 1.7.
+// three kinds of work one after the other and two running sums in every call; without a window 3.1), 32000 tokens of 48 prompts 4.2, in place 6.3; an empty kernel is 1.7.
 #include "step_internal.h"
 
 namespace emm {
@@ -261,7 +261,7 @@ hipError_t launch(const PageStepArgs& a, bool in_place, hipStream_t stream)
 
 hipError_t launch_page_step(const PageStepArgs& a, bool in_place, hipStream_t stream)
 {
-    // Fewer waves meet sooner, and more requests a thread take longer; us of decode steps, outputs apart from inputs: 64 requests with 256 threads 3.2, with 1024
+    // Fewer waves meet sooner, and more requests a thread take longer; us of decode steps without a window, outputs apart from inputs: 64 requests with 256 threads 3.2, with 1024
     // 5.0; 300 with 256 x 4 requests 5.0, 512 x 2 4.7, 1024 x 1 5.5; 1000 5.9, 5.5, 7.1 (in place 11.4, 7.1, 6.7); 2000 with 1024 x 4 8.9, 512 x 8 11.3; 512
     // requests' 16384 tokens 5.2, 4.9, 6.6.
     if (a.num_reqs <= 256) return launch<256, 1>(a, in_place, stream);

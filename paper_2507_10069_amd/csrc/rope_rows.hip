@@ -9,9 +9,10 @@
 // Norms add a sum of squares over the lanes of a row, which travel by DPP, and 16 weights a lane, which stay in registers while a wave is at q's rows.
 //
 // Measured, of bytes read and written: 4096 tokens of 28 + 4 heads of 128 in bf16 rotated in 12.4 us (67 MB, 5.4 TB/s: they fit the
-// last-level cache), with norms 13.1; 42500 tokens of 32 + 8 heads with norms, rotation and the write 207 us (1.07 GB, 5.2 TB/s, what a large copy reaches);
+// last-level cache), with norms 13.1; 42500 tokens of 32 + 8 heads with norms, rotation and the write 207 us (1.07 GB, 5.2 TB/s, what a large copy reaches),
+// into the 8-bit cache 190 (0.98 GB, 5.2 TB/s), with heads of 64 108 (0.54 GB, 4.9 TB/s), 4096 such tokens normed and rotated 9.9;
 // 46000 tokens' K and V of 8 heads quantised in 57 us (284 MB, 5.0 TB/s), 35000 slots
-// of 4 heads read back in 24.2 us (108 MB, 4.5 TB/s).  64 tokens' rotation and write takes 3.9 us on the card, with norms into bf16 3.5, an empty kernel 1.7;
+// of 4 heads read back in 24.2 us (108 MB, 4.5 TB/s).  64 tokens' rotation and write takes 3.9 us on the card, with norms into bf16 3.5, into 8 bits 3.9, an empty kernel 1.7;
 // what a decode step waits for is the launch.
 #include "fp8_device.h"
 #include "step_internal.h"
